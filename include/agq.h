@@ -497,6 +497,101 @@ int agq_stack_forward(const agq_block *blocks, int n_blocks, const int64_t *keep
  * [m]) receives the tokens left after each stage.  0 <= beta < 1, 1 <= m <= 1024.  */
 int agq_cascade_keep(int64_t S, double beta, int m, int64_t *keep_out);
 
+/* ---- Serving: a paged key/value cache in 8 bits, and attention for prompts and for generated tokens.
+ *
+ * The projections of generation read every weight once per step (agq_gemm_w4a8 and the others with few rows); these
+ * calls are what lies between them.  A step is: agq_kv_map (which pages and slots the step's new tokens get), per layer
+ * agq_kv_append (rotary embedding, keys and values into the cache on Eq.2's 8-bit grid, the step's exponent per page and
+ * head instead of per layer), then agq_attn_packed for prompts (fp16 keys and values as they came from the projections)
+ * or agq_attn_kv for generated tokens (everything from the cache).
+ *
+ * Conventions of these calls: fp16 tensors are [tokens, heads, D] with a leading dimension ("ld", elements, a multiple
+ * of 8, at least heads * D) between tokens, so q, k and v may be parts of one projection's output; fp16 tensors,
+ * caches, rope tables and workspaces are 16-byte aligned, int32 arrays 4-byte.  D = 64 or 128.  Hq % Hkv == 0: query
+ * head h reads key head h / (Hq / Hkv).  page = tokens of a page: 16, 32, 64 or 128.  `cu` arrays hold B + 1 offsets in
+ * ascending order; sequence b is tokens cu[b] .. cu[b+1] - 1 of the packed tensor, and rows that belong to no sequence
+ * (padding behind the last one) are neither read nor written.  Offsets, lengths, page numbers and slots live on the
+ * device and are never trusted with an address: whatever lies outside the tensors is left out.  Every call enqueues
+ * kernels only, may be captured, and needs nothing cleared.  A call with no tokens is a no-op (agq_kv_map: it still
+ * gives back pages).                                                                                                 */
+
+/* The cache of one layer.  Entry (token, d) of page p and head h is the code k[p, h, token, d] with the scale
+ * 2^k_exp[p, h]; values lie transposed inside a page, v[p, h, d, token], scale 2^v_exp[p, h].  All pages of a cache lie
+ * in one allocation; n_pages * page < 2^31.  HOST struct, read before a call returns.                                */
+typedef struct agq_kv_cache {
+    int8_t *k;              /* int8 [n_pages, Hkv, page, D]                          */
+    int8_t *v;              /* int8 [n_pages, Hkv, D, page]                          */
+    int8_t *k_exp, *v_exp;  /* int8 [n_pages, Hkv]                                   */
+    int64_t n_pages, Hkv, D, page;
+} agq_kv_cache;
+
+/* Pages, slots and positions of one step from the requests' lengths, on the device in one launch.
+ * kv_len [B]: tokens that request b has in the cache; n_new [B]: tokens that it gets in this step, or -1: it is
+ * finished, its pages go back and its length becomes 0.  block_table [B, max_pages] (updated): the page numbers of
+ * request b, entry j for its tokens j * page .. (j+1) * page - 1; entries behind its pages mean nothing.
+ * The free pages are a ring: free_ring [n_pages] (updated) and free_state = {head, count}; pages are taken at head, in
+ * the order of requests and tokens, and given back behind the last one in the same order.  To begin with: free_ring =
+ * 0 .. n_pages - 1 in any order, free_state = {0, n_pages}, kv_len = 0.
+ * Out: kv_len_out [B] (the lengths after the step), cu_new [B+1] (offsets of the requests' new tokens, finished
+ * requests have none), pos [T], slot [T] (token t goes to token slot % page of page slot / page; T >= the sum of the
+ * new tokens; rows behind them get pos 0, slot -1), free_state_out, and *status: 0; or the number of free pages that
+ * are missing; or -1 (a negative length, n_new < -1, a request longer than max_pages * page, more than T tokens, an
+ * impossible free_state).  With a status other than 0 the step is left out: lengths, table, ring and state stay as they
+ * are, cu_new is all 0 and every slot -1, so that calls which follow do nothing.
+ * kv_len_out and free_state_out must not overlap kv_len and free_state (AGQ_EINVAL): a loop swaps two of each.
+ * B <= 2^20; max_pages * page < 2^31; pos and slot may be NULL when T == 0.                                          */
+int agq_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int64_t page, int32_t *block_table,
+               int64_t max_pages, int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T,
+               int32_t *kv_len_out, int32_t *cu_new, int32_t *pos, int32_t *slot, int32_t *free_state_out,
+               int32_t *status, void *stream);
+
+/* A step's keys and values into the cache, with the rotary embedding on the way (as in agq_rope_quantize: pairs
+ * (i, i + D/2), float64 arithmetic, rounded once to fp16; positions are clamped into the tables).
+ * slot [T]: as agq_kv_map writes it.  A token whose slot is negative or not in the cache is left out: nothing of it is
+ * read or written.  Codes: Eq.2 on the signed 8-bit grid with the step 2^e, e that of the page and head:
+ *   e = the smallest e with max|x| <= 127 * 2^e over the tokens that this call writes there (infinities count as 2^16,
+ *       all zeros as 2^-30's e), but not below the page's present e if earlier tokens lie in front of them (slot % page
+ *       of the first one > 0); the codes of those are then divided by 2^(e - present e), halves to the even code.
+ * Tokens of the call in one page have to be consecutive, in the order of their slots, and no slot twice, as agq_kv_map
+ * makes them; otherwise the contents of that page (of no other memory) are unspecified.  Bytes of the page behind them
+ * stay as they are.
+ * k, v: fp16 [T, Hkv, D].  q (may be NULL with q_out NULL, Hq = 0): fp16 [T, Hq, D], rotated into q_out.  k_out (may be
+ * NULL): the rotated keys in fp16, for agq_attn_packed.  q_out and k_out may be q and k themselves.
+ * rope_cos, rope_sin [P, D/2] float32 and pos [T]; all three NULL: no rotation (q and k_out must be NULL then).        */
+int agq_kv_append(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, const void *v_f16, int64_t ldv, int64_t T,
+                  const int32_t *slot, const void *q_f16, int64_t ldq, int64_t Hq, const int32_t *pos,
+                  const float *rope_cos, const float *rope_sin, int64_t P, void *q_out_f16, int64_t ldqo,
+                  void *k_out_f16, int64_t ldko, void *stream);
+
+/* Attention over packed prompts, fp16 in and out, in one pass over the keys:
+ *   o[i,h] = sum_j softmax_j( scale * q[i,h] . k[j,h'] ) v[j,h'],   h' = h / (Hq / Hkv)
+ * over the keys j of the query's own sequence; causal != 0: query i of n sees keys j <= i + (m - n) of m, so the last
+ * query sees the last key (n < m: the queries are the later part of the prompt; n > m: the first queries see nothing).
+ * A row that sees no key is 0.  Keys and values that a row does not see do not reach it, infinities and NaN included.
+ * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D]; cu_q, cu_k [B+1].  scale > 0, usually 1 / sqrt(D).
+ * Scores, maxima, sums and the accumulated output are fp32; a probability is rounded to fp16 (by 2^-11 of it at
+ * most) for the product with v; the output is rounded once.                                                            */
+int agq_attn_packed(const void *q_f16, int64_t ldq, int64_t Tq, int64_t Hq, const void *k_f16, int64_t ldk,
+                    const void *v_f16, int64_t ldv, int64_t Tk, int64_t Hkv, int64_t D, const int32_t *cu_q,
+                    const int32_t *cu_k, int64_t B, int causal, float scale, void *o_f16, int64_t ldo, void *stream);
+
+/* Attention of each request's newest tokens over its pages: the same sum over the cache, for the n = cu_q[b+1] -
+ * cu_q[b] tokens that are the last of the request's kv_len[b] (kv_len counts them: agq_kv_append comes first; it is
+ * agq_kv_map's kv_len_out).  Always causal: token i of n sees the first kv_len - n + i + 1 tokens.  n = 1 is plain
+ * generation; a few tokens (a draft to be checked) share one pass over the cache; a prompt's part works as well.
+ * max_q, max_kv: the largest n and kv_len as the program knows them.  They choose how the work is dealt out (and so the
+ * workspace); larger lengths are computed all the same.  Lengths beyond max_pages * page are cut to it, and tokens of a
+ * page number outside the cache are left out.
+ * q, o: fp16 [T, Hq, D].  workspace: agq_attn_kv_workspace_bytes (may be 0; NULL then): partial results where the keys
+ * of a request are shared by several workgroups; contents are scratch.  Hq / Hkv <= 1024; B <= 65535.
+ * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32; a probability (times its page's
+ * scale) is rounded to fp16 for the product with v: by 2^-11 of it at most, down to 2^-29 of the row's largest.         */
+size_t agq_attn_kv_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t B, int64_t max_q, int64_t max_kv);
+int agq_attn_kv(const agq_kv_cache *cache, const void *q_f16, int64_t ldq, int64_t T, int64_t Hq, const int32_t *cu_q,
+                const int32_t *kv_len, int64_t B, const int32_t *block_table, int64_t max_pages, int64_t max_q,
+                int64_t max_kv, float scale, void *o_f16, int64_t ldo, void *workspace, size_t workspace_bytes,
+                void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,7 +6,9 @@ is no CPU fallback: if the library has not been built, loading raises."""
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -60,6 +62,12 @@ SIGNATURES = {
     "agq_block_calibrate": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
     "agq_cascade_keep": (_int, [_i64, ctypes.c_double, _int, _vp]),
     "agq_stack_workspace_bytes": (_sz, [_vp, _int, _i64, _vp]),
+    "agq_kv_map": (_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "agq_kv_append": (_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "agq_attn_packed": (_int, [_vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _int, ctypes.c_float, _vp,
+                               _i64, _vp]),
+    "agq_attn_kv_workspace_bytes": (_sz, [_i64] * 7),
+    "agq_attn_kv": (_int, [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_float, _vp, _i64, _vp, _sz, _vp]),
     "agq_stack_forward": (_int, [_vp, _int, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
 }
 
@@ -550,3 +558,146 @@ def cascade_keep(S: int, beta: float, m: int) -> list:
     out = (ctypes.c_int64 * m)()
     _ok(lib().agq_cascade_keep(S, beta, m, ctypes.cast(out, _vp)), "agq_cascade_keep")
     return list(out)
+
+
+# ------------------------------------------------------------------ serving: the paged 8-bit cache and its attentions
+#
+# Tensors of tokens are fp16 [T, heads, D] with any distance between tokens; the caches int8 [n_pages, Hkv, page, D] (keys)
+# and [n_pages, Hkv, D, page] (values) with int8 exponents [n_pages, Hkv].  The calls below look at types, shapes and
+# layouts (a ValueError before anything is enqueued); what lies on the device is checked there.
+
+def _heads(t, name):
+    """(tokens, heads, D, elements between tokens) of a fp16 [T, heads, D] tensor"""
+    T, H, D = t.shape
+    ld, sh, sd = t.stride()
+    if t.dtype is not torch.float16 or (T and (sd != 1 or (H > 1 and sh != D))):
+        raise ValueError("%s: fp16 [tokens, heads, D] with contiguous heads is wanted" % name)
+    return T, H, D, (ld if T > 1 else max(ld, H * D) if ld % 8 == 0 else H * D)
+
+
+def _ints(n, **tensors):
+    for name, t in tensors.items():
+        if t.dtype is not torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
+            raise ValueError("%s: a contiguous int32 tensor%s is wanted" % (name, "" if n is None else " of %d values" % n))
+
+
+def _kv_cache(k_cache, v_cache, k_exp, v_exp):
+    """struct agq_kv_cache as eight 8-byte values"""
+    n_pages, Hkv, page, D = k_cache.shape
+    if (v_cache.shape != (n_pages, Hkv, D, page) or k_exp.shape != (n_pages, Hkv) or v_exp.shape != (n_pages, Hkv)
+            or not (k_cache.dtype is v_cache.dtype is k_exp.dtype is v_exp.dtype is torch.int8)
+            or not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_exp.is_contiguous() and v_exp.is_contiguous())):
+        raise ValueError("cache: contiguous int8 k [n_pages, Hkv, page, D], v [n_pages, Hkv, D, page], exponents [n_pages, Hkv] are wanted")
+    return (_i64 * 8)(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), n_pages, Hkv, D, page), Hkv, D
+
+
+class KvStep(NamedTuple):
+    """What kv_map says about a step (device int32 tensors): the lengths after it [B], the offsets of the requests' new
+    tokens [B+1], position and slot of every token [T], the ring's state [2], and the status [1]."""
+    kv_len: torch.Tensor
+    cu_new: torch.Tensor
+    pos: torch.Tensor
+    slot: torch.Tensor
+    free_state: torch.Tensor
+    status: torch.Tensor
+
+
+def kv_map(kv_len, n_new, block_table, page, free_ring, free_state, T, out: KvStep | None = None) -> KvStep:
+    """agq_kv_map: pages, slots and positions of one step; block_table [B, max_pages] and free_ring [n_pages] are updated.
+    out: a KvStep to write into (not the one whose kv_len and free_state are passed in: a loop swaps two)."""
+    B, max_pages = block_table.shape
+    _ints(B, kv_len=kv_len, n_new=n_new)
+    _ints(None, block_table=block_table, free_ring=free_ring)
+    _ints(2, free_state=free_state)
+    if out is None:
+        buf = torch.empty(2 * B + 4 + 2 * T, dtype=torch.int32, device=kv_len.device)
+        out = KvStep(*buf.split([B, B + 1, T, T, 2, 1]))
+    else:
+        _ints(B, kv_len=out.kv_len)
+        _ints(T, pos=out.pos, slot=out.slot)
+        if out.cu_new.numel() != B + 1 or out.free_state.numel() != 2:
+            raise ValueError("out: a KvStep of another batch")
+    _ok(lib().agq_kv_map(kv_len.data_ptr(), n_new.data_ptr(), B, page, block_table.data_ptr(), max_pages, free_ring.data_ptr(),
+                         free_ring.numel(), free_state.data_ptr(), T, out.kv_len.data_ptr(), out.cu_new.data_ptr(), out.pos.data_ptr(),
+                         out.slot.data_ptr(), out.free_state.data_ptr(), out.status.data_ptr(), _stream()), "agq_kv_map")
+    return out
+
+
+def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope_cos=None, rope_sin=None, q_out=None, k_out=None):
+    """agq_kv_append: a step's keys and values into the cache.  With rope tables (float32 [P, D/2]) and pos the keys, and
+    the queries if given, are rotated first: returns (rotated q or None, rotated k), else (None, None)."""
+    cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
+    T, Hk, Dk, ldk = _heads(k, "k")
+    Tv, Hv, Dv, ldv = _heads(v, "v")
+    if (Hk, Dk) != (Hkv, D) or (Tv, Hv, Dv) != (T, Hkv, D):
+        raise ValueError("k and v: [T, %d, %d] as the cache has it is wanted" % (Hkv, D))
+    _ints(T, slot=slot)
+    P = Hq = ldq = ldqo = ldko = 0
+    if rope_cos is not None:
+        _ints(T, pos=pos)
+        P = rope_cos.shape[0]
+        if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is torch.float32) \
+                or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
+            raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
+        k_out = torch.empty((T, Hkv, D), dtype=torch.float16, device=k.device) if k_out is None else k_out
+        To, Ho, Do, ldko = _heads(k_out, "k_out")
+        if (To, Ho, Do) != (T, Hkv, D):
+            raise ValueError("k_out: k's shape is wanted")
+    elif q is not None or k_out is not None or pos is not None:
+        raise ValueError("q, k_out and pos go with rope tables")
+    if q is not None:
+        Tq, Hq, Dq, ldq = _heads(q, "q")
+        q_out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device) if q_out is None else q_out
+        To, Ho, Do, ldqo = _heads(q_out, "q_out")
+        if (Tq, Dq) != (T, D) or (To, Ho, Do) != (T, Hq, D):
+            raise ValueError("q and q_out: [T, Hq, D] is wanted")
+    _ok(lib().agq_kv_append(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, slot.data_ptr(), _ptr(q), ldq, Hq, _ptr(pos), _ptr(rope_cos),
+                            _ptr(rope_sin), P, _ptr(q_out) if q is not None else None, ldqo, _ptr(k_out), ldko, _stream()), "agq_kv_append")
+    return (q_out if q is not None else None), k_out
+
+
+def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None):
+    """agq_attn_packed: attention of packed sequences; q fp16 [Tq, Hq, D], k and v [Tk, Hkv, D], cu_q, cu_k int32 [B+1].
+    Rows of o that belong to no sequence are not written."""
+    Tq, Hq, D, ldq = _heads(q, "q")
+    Tk, Hkv, Dk, ldk = _heads(k, "k")
+    Tv, Hv, Dv, ldv = _heads(v, "v")
+    B = cu_q.numel() - 1
+    _ints(B + 1, cu_q=cu_q, cu_k=cu_k)
+    if Dk != D or (Tv, Hv, Dv) != (Tk, Hkv, D):
+        raise ValueError("k and v: [Tk, Hkv, %d] are wanted" % D)
+    o = torch.empty((Tq, Hq, D), dtype=torch.float16, device=q.device) if o is None else o
+    To, Ho, Do, ldo = _heads(o, "o")
+    if (To, Ho, Do) != (Tq, Hq, D):
+        raise ValueError("o: q's shape is wanted")
+    _ok(lib().agq_attn_packed(q.data_ptr(), ldq, Tq, Hq, k.data_ptr(), ldk, v.data_ptr(), ldv, Tk, Hkv, D, cu_q.data_ptr(), cu_k.data_ptr(),
+                              B, 1 if causal else 0, 1.0 / math.sqrt(D) if scale is None else scale, o.data_ptr(), ldo, _stream()),
+        "agq_attn_packed")
+    return o
+
+
+def attn_kv_workspace_bytes(T, Hq, Hkv, D, B, max_q, max_kv) -> int:
+    return lib().agq_attn_kv_workspace_bytes(T, Hq, Hkv, D, B, max_q, max_kv)
+
+
+def attn_kv(q, cu_q, kv_len, block_table, k_cache, v_cache, k_exp, v_exp, max_q, max_kv, scale=None, o=None, workspace=None):
+    """agq_attn_kv: each request's newest tokens (q fp16 [T, Hq, D], cu_q int32 [B+1]) over its kv_len [B] tokens of the
+    cache.  max_q, max_kv: the largest number of new tokens and of tokens in the cache, as the program knows them."""
+    cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
+    T, Hq, Dq, ldq = _heads(q, "q")
+    B, max_pages = block_table.shape
+    _ints(B, kv_len=kv_len)
+    _ints(B + 1, cu_q=cu_q)
+    _ints(None, block_table=block_table)
+    if Dq != D:
+        raise ValueError("q: [T, Hq, %d] as the cache has it is wanted" % D)
+    o = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device) if o is None else o
+    To, Ho, Do, ldo = _heads(o, "o")
+    if (To, Ho, Do) != (T, Hq, D):
+        raise ValueError("o: q's shape is wanted")
+    if workspace is None:
+        workspace = _scratch(lib().agq_attn_kv_workspace_bytes(T, Hq, Hkv, D, B, max_q, max_kv), q.device)
+    _ok(lib().agq_attn_kv(cache, q.data_ptr(), ldq, T, Hq, cu_q.data_ptr(), kv_len.data_ptr(), B, block_table.data_ptr(), max_pages, max_q,
+                          max_kv, 1.0 / math.sqrt(D) if scale is None else scale, o.data_ptr(), ldo, _ptr(workspace),
+                          0 if workspace is None else workspace.nbytes, _stream()), "agq_attn_kv")
+    return o

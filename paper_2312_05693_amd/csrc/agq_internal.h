@@ -370,3 +370,61 @@ int agq_launch_swiglu(const void *gate, const void *up, void *out, int64_t n, vo
 int agq_launch_swiglu_rows(const void *gate, const void *up, void *out, int64_t rows, int64_t F, const AgqCodes &codes, void *stream);
 int agq_launch_add(const void *a, const void *b, void *out, int64_t n, void *stream);
 int agq_read_i32(const int32_t *dev, int32_t *host, int n, void *stream);
+
+// ---- serving (agq_kv.hip, agq_attn_kv.hip, agq_attn_packed.hip, agq_serve_api.cpp)
+struct AgqKvAppend {
+    int8_t *k_cache, *v_cache, *k_exp, *v_exp;
+    int64_t n_pages, Hkv, D;
+    int page;
+    const void *q, *k, *v;
+    void *q_out, *k_out;
+    int64_t ldq, ldk, ldv, ldqo, ldko, T, Hq, P;
+    const int32_t *pos, *slot;
+    const float *rope_cos, *rope_sin;
+};
+struct AgqAttnPacked {
+    const void *q, *k, *v;
+    void *o;
+    int64_t ldq, ldk, ldv, ldo, Tq, Tk, Hq, Hkv, D, B;
+    const int32_t *cu_q, *cu_k;
+    int causal;
+    float scale;
+};
+struct AgqAttnKv {
+    const int8_t *k_cache, *v_cache, *k_exp, *v_exp;
+    int64_t n_pages, Hkv, D;
+    int page;
+    const void *q;
+    void *o;
+    int64_t ldq, ldo, T, Hq, B, max_pages, max_q;
+    const int32_t *cu_q, *kv_len, *block_table;
+    float scale;
+};
+// How attention over the cache is dealt out: 16 * tiles rows (new tokens x query heads of a key head) per workgroup,
+// row_tiles workgroups over the rows, splits over the keys with split_keys keys each (a multiple of 64).
+struct AgqKvSplit {
+    int tiles, row_tiles, splits, split_keys;
+};
+static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv) {
+    const int64_t rows = max_q * (Hq / Hkv), fill = 768;
+    AgqKvSplit s;
+    s.tiles = rows <= 16 ? 1 : 2;
+    const int64_t row_tiles = (rows + 16 * s.tiles - 1) / (16 * s.tiles);
+    s.row_tiles = (int)(row_tiles < 1 ? 1 : row_tiles > 1024 ? 1024 : row_tiles);
+    const int64_t groups = B * Hkv * s.row_tiles, most = (max_kv + 511) / 512;
+    int64_t splits = groups < 1 ? 1 : fill / groups;
+    splits = splits > most ? most : splits;
+    splits = splits < 1 ? 1 : splits;
+    int64_t keys = (max_kv + splits - 1) / splits;
+    keys = (keys + 255) / 256 * 256;
+    s.split_keys = (int)(keys < 256 ? 256 : keys);
+    s.splits = (int)((max_kv + s.split_keys - 1) / s.split_keys);
+    if (s.splits < 1) s.splits = 1;
+    return s;
+}
+int agq_launch_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int page, int32_t *block_table, int64_t max_pages,
+                      int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T, int32_t *kv_len_out, int32_t *cu_new,
+                      int32_t *pos, int32_t *slot, int32_t *free_state_out, int32_t *status, void *stream);
+int agq_launch_kv_append(const AgqKvAppend &p, void *stream);
+int agq_launch_attn_packed(const AgqAttnPacked &p, void *stream);
+int agq_launch_attn_kv(const AgqAttnKv &p, const AgqKvSplit &sp, void *workspace, void *stream);
