@@ -15,10 +15,12 @@ typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -1e30f;      // the maximum of no keys
-constexpr float kUp = 1024.0f;       // 2^10: probabilities in the second product
-constexpr int kRows = 128, kKeys = 64;
+constexpr float kUpLog2 = 10.0f;     // probabilities are 2^10 times what they are, in sum and product alike
+constexpr float kSlack = 5.0f;       // how far a score may lie above the row's reference, in powers of two
+constexpr int kRows = 128;
 
 struct PackedArgs {
     const _Float16 *q, *k, *v;
@@ -55,16 +57,16 @@ __device__ __forceinline__ Tile tile_of(const PackedArgs &a, int idx, int rows) 
         if (over) {
             const int src = __ffsll((long long)over) - 1;
             Tile t;
-            t.b = b0 + src;
-            t.q0 = __shfl(q0, src);
-            t.n = __shfl(n, src);
-            const int last = __shfl(before + up, src) - 1;       // the sequence's last tile is its number 0
+            t.b = __builtin_amdgcn_readfirstlane(b0 + src);
+            t.q0 = __builtin_amdgcn_readlane(q0, src);
+            t.n = __builtin_amdgcn_readlane(n, src);
+            const int last = __builtin_amdgcn_readlane(before + up, src) - 1;       // the sequence's last tile is its number 0
             t.row = (last - idx) * rows;
             t.k0 = min(max(a.cu_k[t.b], 0), a.Tk);
             t.m = max(min(max(a.cu_k[t.b + 1], 0), a.Tk) - t.k0, 0);
             return t;
         }
-        before += __shfl(up, 63);
+        before += __builtin_amdgcn_readlane(up, 63);
     }
     Tile t = {};
     t.b = -1;
@@ -73,17 +75,53 @@ __device__ __forceinline__ Tile tile_of(const PackedArgs &a, int idx, int rows) 
 
 // four keys of one column of a [key][d] tile in LDS: lanes 4 r + c of a group of sixteen name row r's columns 4 c .. 4 c + 3,
 // lane j receives column j of the four rows
-__device__ __forceinline__ short4_t read_tr(const _Float16 *p) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)p);
+__device__ __forceinline__ short4_t read_tr(uint32_t at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)(uintptr_t)at);
+}
+__device__ __forceinline__ half8_t read_lds(uint32_t at) {
+    return *(const __attribute__((address_space(3))) half8_t *)(uintptr_t)at;
 }
 
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void unroll(F &&f) {
+    if constexpr (I < N) {
+        f(Int<I>{});
+        unroll<N, I + 1>(f);
+    }
+}
+
+// At most VM of this wavefront's copies may still fly (they return in order), its LDS reads are done; then meet the others.
+template <int VM>
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | 0x70);   // vmcnt(VM) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Keys go by in sub-tiles of 32.  In step u the scores of sub-tile u + 1 and the product with the values of sub-tile u - 1 run on
+// the matrix cores while the vector ALU turns the scores of sub-tile u into probabilities: three independent pieces of
+// work, dealt out one matrix instruction at a time.  Copies into LDS run two steps ahead (rings of three).
+// Rows' reference: a probability is 2^(c s - off); off is raised to the row's maximum (less 10) only when a score is five
+// above it, so the accumulators are seldom rescaled and a weight stays below 2^15.
 template <int D>
-__global__ __launch_bounds__(256) void attn_packed_kernel(const PackedArgs a) {
-    constexpr int KS = D / 16, DT = D / 32, CH = D / 8;            // steps of the first product, row tiles of the second, 16-byte pieces of a row
-    constexpr int LOADS = kKeys * CH / 256;
-    __shared__ __attribute__((aligned(16))) _Float16 ks[kKeys * D], vs[kKeys * D];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 31, h = lane >> 5;
-    const int head = blockIdx.x % a.Hq, kv = head / a.group;
+__global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a) {
+    constexpr int KS = D / 16, DT = D / 32;                        // matrix instructions for a sub-tile's scores; d tiles of the output
+    constexpr int PIECES = D / 8, ROW = D * 2, SUB = 32 * ROW;     // 16-byte pieces and bytes of a row, bytes of a sub-tile
+    constexpr int COPIES = SUB / 4096;                             // a wavefront's copies (1 KiB each) of a sub-tile
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[6 * SUB];       // keys' ring, values' ring
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // heads that share keys go to one XCD (workgroups go around the eight of them)
+    int head = blockIdx.x % a.Hq;
+    if (a.Hq % 8 == 0) head = (head & 7) * (a.Hq >> 3) + (head >> 3);
+    const int kv = head / a.group;
     const Tile tl = tile_of(a, blockIdx.x / a.Hq, kRows);
     if (tl.b < 0) return;
     const int row = tl.row + wave * 32 + i;                        // the lane's query
@@ -99,124 +137,230 @@ __global__ __launch_bounds__(256) void attn_packed_kernel(const PackedArgs a) {
     }
     const int past = tl.m - tl.n;                                  // query r sees keys up to past + r
     const int seen = a.causal ? min(past + row + 1, tl.m) : tl.m;
-    const int rows_here = min(tl.n - tl.row, kRows);
-    const int all_keys = a.causal ? min(past + tl.row + rows_here, tl.m) : tl.m;              // keys that some row of the workgroup sees
-    const int wave_keys = a.causal ? min(past + tl.row + wave * 32 + 32, tl.m) : tl.m;        // ... of the wavefront
-    const int wave_all = a.causal ? past + tl.row + wave * 32 + 1 : tl.m;                     // keys that every row of it sees
+    const int last_row = min(tl.n - tl.row, kRows) - 1;            // of the workgroup's rows
+    const int all_keys = a.causal ? min(past + tl.row + last_row + 1, tl.m) : tl.m;                                 // that some row sees
+    const int wave_last = min(last_row, wave * 32 + 31);
+    const int wave_keys = wave * 32 > last_row ? 0 : a.causal ? min(past + tl.row + wave_last + 1, tl.m) : tl.m;    // some row of the wavefront
+    const int wave_all = a.causal ? min(past + tl.row + wave * 32 + 1, tl.m) : tl.m;                                // every row of it
+    const int steps = (max(all_keys, 0) + 31) >> 5, mine = (max(wave_keys, 0) + 31) >> 5, whole = max(wave_all, 0) >> 5;
+
+    // copies: lane l of a wavefront's copy j brings the piece that belongs at place l of 1 KiB.  Sixteen lanes read LDS at a time,
+    // 256 bytes: a row's pieces are permuted by the row so that the sixteen rows (keys) or the four rows of 64 bytes (values) of a
+    // read meet every bank once.
+    const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
     const _Float16 *kbase = a.k + (int64_t)tl.k0 * a.ldk + kv * D, *vbase = a.v + (int64_t)tl.k0 * a.ldv + kv * D;
-
-    float M = kNone, l = 0.0f;
-    float16_t o[DT];
+    auto key_place = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
+    auto value_place = [](int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; };
+    uint32_t k_off[COPIES], v_off[COPIES];
+    auto offsets = [&](int limit) {                                // rows from `limit` on are replaced by the last one
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = float16_t{};
-
-    uint4 kr[LOADS], vr[LOADS];
-    auto load = [&](int key0) {
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int it = j * 256 + tid, r = key0 + it / CH, c = it % CH;
-            // rows behind the sequence are not read: another sequence's, or nobody's
-            kr[j] = vr[j] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < tl.m) {
-                kr[j] = *reinterpret_cast<const uint4 *>(kbase + (int64_t)r * a.ldk + c * 8);
-                vr[j] = *reinterpret_cast<const uint4 *>(vbase + (int64_t)r * a.ldv + c * 8);
-            }
+        for (int j = 0; j < COPIES; ++j) {
+            const int r = (wave * COPIES + j) * (64 / PIECES) + lane / PIECES, at = lane % PIECES, from = min(r, limit - 1);
+            k_off[j] = (uint32_t)(from * (int)a.ldk + (at ^ key_place(r)) * 8) * 2;
+            v_off[j] = (uint32_t)(from * (int)a.ldv + (at ^ value_place(r)) * 8) * 2;
         }
     };
-    if (all_keys > 0) load(0);
-    for (int key0 = 0; key0 < all_keys; key0 += kKeys) {
-        __syncthreads();
-        bool odd = false;                       // an infinity or NaN among the thread's values
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int it = j * 256 + tid, r = it / CH, c = it % CH;
-            *reinterpret_cast<uint4 *>(ks + r * D + ((c ^ (r & 7)) * 8)) = kr[j];
-            *reinterpret_cast<uint4 *>(vs + r * D + ((c ^ ((r & 3) * (D == 128 ? 4 : 2))) * 8)) = vr[j];
-            const uint32_t w[4] = {vr[j].x, vr[j].y, vr[j].z, vr[j].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= (w[e] & 0x7C00u) == 0x7C00u || (w[e] & 0x7C000000u) == 0x7C000000u;
-        }
-        // Such values under the mask must not reach the rows that do not see them (0 times an infinity is NaN); they go in by
-        // the slow way below, and only in tiles that the mask cuts
-        const bool slow = __syncthreads_or(odd) && key0 + kKeys > (a.causal ? past + tl.row + 1 : tl.m);
-        if (key0 + kKeys < all_keys) load(key0 + kKeys);
-        if (key0 >= wave_keys) continue;
+    offsets(32);
+    int k_next = 0, v_next = 0;                                    // sub-tiles to be copied next
+    uint32_t k_slot = 0, v_slot = 0;
+    const uint32_t part = wave * (COPIES * 1024);
+    auto copy_k = [&] {                                            // behind the last one: the last one again, into a slot nobody reads
+        const int u = min(k_next, steps - 1);
+        if (u * 32 + 32 > tl.m) offsets(tl.m - u * 32);
+        const _Float16 *src = kbase + (int64_t)(u * 32) * a.ldk;
+        lds_dma16_s<0, 0>(k_off[0], src, base + k_slot + part);
+        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(k_off[COPIES - 1], src, base + k_slot + part);
+        ++k_next;
+        k_slot = k_slot == 2 * SUB ? 0 : k_slot + SUB;
+    };
+    auto copy_v = [&] {
+        const int u = min(v_next, steps - 1);
+        if (u * 32 + 32 > tl.m) offsets(tl.m - u * 32);
+        else if (k_next * 32 > tl.m) offsets(32);
+        const _Float16 *src = vbase + (int64_t)(u * 32) * a.ldv;
+        lds_dma16_s<0, 0>(v_off[0], src, base + 3 * SUB + v_slot + part);
+        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(v_off[COPIES - 1], src, base + 3 * SUB + v_slot + part);
+        ++v_next;
+        v_slot = v_slot == 2 * SUB ? 0 : v_slot + SUB;
+    };
 
-        float16_t s[2] = {};
+    // operand reads: piece 2 st + h of row i; columns 32 d .. + 31 of rows 16 st + 8 e + 4 h .. + 3
+    const uint32_t k_lane = (uint32_t)(i * ROW) + (uint32_t)((h ^ key_place(i)) << 4);
+    const int tr_row = 4 * h + ((lane & 15) >> 2), tr_col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+    const uint32_t v_lane = (uint32_t)(tr_row * ROW) + (uint32_t)(((tr_col >> 3) ^ value_place(tr_row)) << 4) + (tr_col & 7) * 2;
+    auto read_k = [&](uint32_t at, int st) { return read_lds(at ^ (uint32_t)(st << 5)); };
+    auto read_v = [&](uint32_t at, int d, int st) {
+        union {
+            short4_t s[2];
+            half8_t v;
+        } f;
+        f.s[0] = read_tr((at ^ (uint32_t)(d << 6)) + st * 16 * ROW);
+        f.s[1] = read_tr((at ^ (uint32_t)(d << 6)) + st * 16 * ROW + 8 * ROW);
+        return f.v;
+    };
+
+    const float c = a.scale;
+    float off = kNone, l = 0.0f;
+    float16_t o[DT], s0 = {}, s1 = {};
+    half8_t p0[2] = {}, p1[2] = {};
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+    for (int d = 0; d < DT; ++d) o[d] = float16_t{};
+    const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
+
+    auto top_of = [&](const float16_t &s) {
+        float t[4];
 #pragma unroll
-            for (int st = 0; st < KS; ++st) {
-                const int r = half * 32 + i;
-                const half8_t kf = *reinterpret_cast<const half8_t *>(ks + r * D + (((st * 2 + h) ^ (r & 7)) * 8));
-                s[half] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[st], s[half], 0, 0, 0);
+        for (int r = 0; r < 4; ++r) t[r] = fmaxf(fmaxf(fmaxf(s[4 * r], s[4 * r + 1]), s[4 * r + 2]), s[4 * r + 3]);
+        const float x = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        return fmaxf(x, __shfl_xor(x, 32));
+    };
+    auto weigh = [&](const float16_t &s, half8_t (&p)[2], int g) {   // scores 2 g and 2 g + 1
+        const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * g], c, -off)), (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * g + 1], c, -off))};
+        p[g >> 2][2 * (g & 3)] = w.x;
+        p[g >> 2][2 * (g & 3) + 1] = w.y;
+        l = __builtin_amdgcn_fdot2(w, ones, l, false);
+    };
+
+    uint32_t k_rd = 0, v_rd = 0;                                   // slots of sub-tiles u + 1 and u - 1
+
+    // every step that has something at the mask, at the beginning or at the end
+    auto scores = [&](float16_t &s) {
+        const uint32_t at = base + k_rd + k_lane;
+        s = float16_t{};
+#pragma unroll
+        for (int st = 0; st < KS; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_k(at, st), q[st], s, 0, 0, 0);
+    };
+    auto step_plain = [&](int u) {                                 // scores in s0, probabilities of the sub-tile before in p1
+        if (u + 1 < mine) scores(s1);
+        if (u > 0 && u - 1 < mine) {
+            const uint32_t at = base + 3 * SUB + v_rd + v_lane;
+            // values under the mask must not reach the rows that do not see them (0 times an infinity is NaN): infinities and
+            // NaN are left out of the product and added where they are seen
+            const bool cut = u > whole;
+            uint32_t odd = 0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    half8_t v = read_v(at, d, st);
+                    if (cut) {
+                        uint4_t w = __builtin_bit_cast(uint4_t, v);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t x = ((w[e] & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((w[e] & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
+                            odd |= x;
+                            w[e] &= ~x;
+                        }
+                        v = __builtin_bit_cast(half8_t, w);
+                    }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p1[st], o[d], 0, 0, 0);
+                }
+            if (cut && __any(odd)) {
+                for (int r = 0; r < 32 && (u - 1) * 32 + r < seen; ++r)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int col = d * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+                            const _Float16 x = *(const __attribute__((address_space(3))) _Float16 *)(uintptr_t)(
+                                base + 3 * SUB + v_rd + r * ROW + (((col >> 3) ^ value_place(r)) << 4) + (col & 7) * 2);
+                            if ((__builtin_bit_cast(uint16_t, x) & 0x7C00u) == 0x7C00u) o[d][e] += (float)x;
+                        }
             }
-        const bool masked = key0 + kKeys > wave_all;
-        float top = kNone;
+        }
+        if (u < mine) {
+            if (u >= whole) {
+                const int left = seen - u * 32 - 4 * h;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float x = s[half][r] * a.scale;
-                const int key = key0 + half * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                if (masked) x = key < seen ? x : -INFINITY;
-                s[half][r] = x;
-                top = fmaxf(top, x);
+                for (int r = 0; r < 16; ++r) s0[r] = 8 * (r >> 2) + (r & 3) < left ? s0[r] : -INFINITY;
             }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > M)) {
-            const float to = fmaxf(M, top), f = __builtin_amdgcn_exp2f(M - to);
-            M = to;
+            const float top = top_of(s0), over = fmaf(top, c, -off);
+            if (__any(over > kSlack + kUpLog2)) {
+                const float to = over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off, f = __builtin_amdgcn_exp2f(off - to);
+                off = to;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] *= f;
+            }
+#pragma unroll
+            for (int g = 0; g < 8; ++g) weigh(s0, p1, g);
+        }
+        s0 = s1;
+    };
+
+    // the others: sub-tiles u and u - 1 seen whole, u + 1 there
+    auto step_full = [&](float16_t &s, float16_t &s_next, half8_t (&p)[2], const half8_t (&p_before)[2]) {
+        const uint32_t at_k = base + k_rd + k_lane, at_v = base + 3 * SUB + v_rd + v_lane;
+        half8_t kf[KS], vf[2 * DT];
+        constexpr int AHEAD = 3;
+        unroll<AHEAD>([&](auto n) {
+            kf[n.value] = read_k(at_k, n.value);
+            vf[n.value] = read_v(at_v, n.value % DT, n.value / DT);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        const float top = top_of(s), over = fmaf(top, c, -off);
+        float f = 1.0f;
+        const bool raise = __any(over > kSlack + kUpLog2);
+        if (raise) {
+            const float to = over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off;
+            f = __builtin_amdgcn_exp2f(off - to);
+            off = to;
             l *= f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        unroll<KS>([&](auto n) {                                   // KS == 2 DT
+            constexpr int N = n.value;
+            if constexpr (N == 0) s_next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[0], q[0], float16_t{}, 0, 0, 0);
+            else s_next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[N], q[N], s_next, 0, 0, 0);
+            if constexpr (N + AHEAD < KS) kf[N + AHEAD] = read_k(at_k, N + AHEAD);
+            weigh(s, p, N * 8 / KS);
+            __builtin_amdgcn_sched_barrier(0);
+            o[N % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[N], p_before[N / DT], o[N % DT], 0, 0, 0);
+            if constexpr (N + AHEAD < KS) vf[N + AHEAD] = read_v(at_v, (N + AHEAD) % DT, (N + AHEAD) / DT);
+            if constexpr (KS == 4) weigh(s, p, 2 * N + 1);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (raise) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= f;
         }
-        half8_t p[4];
-        float sum = 0.0f;
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float w = __builtin_amdgcn_exp2f(s[half][r] - M);
-                sum += w;
-                p[half * 2 + (r >> 3)][r & 7] = (_Float16)(w * kUp);
+    };
+
+    if (steps > 0) {
+        copy_k();                                                  // sub-tiles 0, 1 and 2 of the keys, 0 of the values
+        copy_k();
+        copy_k();
+        copy_v();
+        meet<3 * COPIES>();
+        if (mine > 0) scores(s0);
+        // Between two steps: keys' sub-tile u + 1 and values' u - 1 have landed (what the step before requested may fly), and
+        // nobody reads the slots of keys' u and values' u - 2 any more, which the next ones get.
+        auto turn = [&](int u) {
+            meet<2 * COPIES>();
+            k_rd = k_rd == 2 * SUB ? 0 : k_rd + SUB;
+            if (u > 1) v_rd = v_rd == 2 * SUB ? 0 : v_rd + SUB;
+            copy_k();
+            copy_v();
+        };
+        const int full = min(whole, mine - 1);                     // steps 1 .. full - 1 are full ones
+        for (int u = 0; u <= steps;) {
+            if (u >= 1 && u + 1 < full) {
+                turn(u);
+                step_full(s0, s1, p0, p1);
+                turn(u + 1);
+                step_full(s1, s0, p1, p0);
+                u += 2;
+            } else {
+                turn(u);
+                step_plain(u);
+                ++u;
             }
-        l += sum;
-        // O^T += V^T P^T; the lane's keys of step st: 16 st + 8 (e / 4) + 4 h + e % 4
-        const int tr_row = 4 * h + ((lane & 15) >> 2), tr_col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                short4_t part[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = st * 16 + e * 8 + tr_row, col = d * 32 + tr_col;
-                    part[e] = read_tr(vs + r * D + (((col >> 3) ^ ((r & 3) * (D == 128 ? 4 : 2))) * 8) + (col & 7));
-                }
-                short vfr[8] = {part[0].x, part[0].y, part[0].z, part[0].w, part[1].x, part[1].y, part[1].z, part[1].w};
-                half8_t vf = __builtin_bit_cast(half8_t, vfr);
-                if (slow) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) vf[e] = (((uint16_t)vfr[e]) & 0x7C00u) == 0x7C00u ? (_Float16)0.0f : vf[e];
-                }
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[st], o[d], 0, 0, 0);
-            }
-        if (slow) {
-            for (int r = 0; r < kKeys && key0 + r < seen; ++r)
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int col = d * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-                        const _Float16 x = vs[r * D + (((col >> 3) ^ ((r & 3) * (D == 128 ? 4 : 2))) * 8) + (col & 7)];
-                        if ((__builtin_bit_cast(uint16_t, x) & 0x7C00u) == 0x7C00u) o[d][e] += (float)x;
-                    }
         }
+        __builtin_amdgcn_s_waitcnt(0x70);                          // the last copies have landed before the LDS is given back
     }
     l += __shfl_xor(l, 32);
     if (!on) return;
-    const float f = l == 0.0f ? 0.0f : 1.0f / (l * kUp);
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
     _Float16 *dst = a.o + (int64_t)(tl.q0 + row) * a.ldo + head * D + 4 * h;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
