@@ -6,22 +6,24 @@
 // second product, O^T = V^T P^T, wants from that lane: the probabilities never leave their registers.  Which key a tile's
 // row stands for is free, so the keys are dealt out such that a lane's sixteen are neighbours: its bytes of V (kept [D, token]
 // in a page) are one load, and so is its piece of a key.  Nothing goes through LDS but the join of the wavefronts.
-// Codes become fp16 exactly (1024 + code + 128 - 1152); a page's scale of K is a factor of the scores.  Its scale of V is
-// added to the exponent: the weight of key j is w = 2^(s_j + e_v - M), M the running maximum of s_j + e_v, so the products of
+// A page's scale of K is a factor of the scores.  Its scale of V is added to the exponent: the weight of key j is w = 2^(s_j + e_v - M), M the running maximum of s_j + e_v, so the products of
 // pages with different scales add up in one accumulator, and the softmax's sum is that of w 2^-e_v.  w goes into the product
 // as fp16 times 2^15: down to 2^-29 of the largest weight it has all eleven bits (off by 2^-11 of it at most, and as often up
 // as down); sums, maxima and accumulators are fp32.
 #include "agq_device.h"
 #include "agq_internal.h"
 
+#include <type_traits>
+
 namespace {
 
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -1e30f;       // the maximum of no keys
-constexpr float kUp = 32768.0f;       // 2^15: weights in the second product
+constexpr float kUpLog2 = 15.0f;      // weights are 2^15 times what they are, in sums and product alike
 
 struct KvArgs {
     const _Float16 *q;
@@ -35,18 +37,23 @@ struct KvArgs {
     int T, B, Hq, Hkv, group, page_log2, n_pages, splits, split_keys, row_tiles;
 };
 
-// four codes -> four fp16
-__device__ __forceinline__ void widen4(uint32_t w, half2_t &a, half2_t &b) {
-    const uint32_t u = w ^ 0x80808080u;
-    const half2_t off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-    a = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
-    b = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
+// Eight codes of K as fp16: code + 128 is the low byte of a half, a subnormal, 2^-24 times itself; three instructions for
+// four codes.  The factor and 128 times the row's sum of q come out of the score, which is off by the roundings of a sum
+// 128 times |q|_1 in size for it, as if every code were that large.
+__device__ __forceinline__ half8_t widen_k(uint32_t w0, uint32_t w1) {
+    const uint32_t u0 = w0 ^ 0x80808080u, u1 = w1 ^ 0x80808080u;
+    const uint4_t h = {__builtin_amdgcn_perm(0u, u0, 0x0c010c00u), __builtin_amdgcn_perm(0u, u0, 0x0c030c02u),
+                       __builtin_amdgcn_perm(0u, u1, 0x0c010c00u), __builtin_amdgcn_perm(0u, u1, 0x0c030c02u)};
+    return __builtin_bit_cast(half8_t, h);
 }
-__device__ __forceinline__ half8_t widen8(uint32_t w0, uint32_t w1) {
-    half2_t a, b, c, d;
-    widen4(w0, a, b);
-    widen4(w1, c, d);
-    return half8_t{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+constexpr float kCode = 16777216.0f;  // 2^24
+// Eight codes of V as fp16, exactly: 1024 + (code + 128) - 1152.  (K's form would leave an error of 128 times the rounding
+// of the weights' sum in an output whose values are all small.)
+__device__ __forceinline__ half8_t widen_v(uint32_t w0, uint32_t w1) {
+    const uint32_t u0 = w0 ^ 0x80808080u, u1 = w1 ^ 0x80808080u;
+    const uint4_t h = {__builtin_amdgcn_perm(0x64646464u, u0, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, u0, 0x04030402u),
+                       __builtin_amdgcn_perm(0x64646464u, u1, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, u1, 0x04030402u)};
+    return __builtin_bit_cast(half8_t, h) - (_Float16)1152.0f;
 }
 
 // how many workgroups share the keys of a request of L tokens
@@ -66,25 +73,31 @@ __device__ __forceinline__ Request request_of(const KvArgs &a, int b) {
 // One workgroup of NW wavefronts: NQ tiles of sixteen rows of one key head of one request, over one split of its keys;
 // the wavefronts take the chunks of 64 keys in turn.
 template <int D, int NQ, int NW>
-__global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
-    constexpr int KH = D / 64, DT = D / 16, ROWS = 16 * NQ;
-    __shared__ __attribute__((aligned(16))) float join[NW * 16 * D];
+__global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
+    constexpr int KH = D / 64, DT = D / 16, ROWS = 16 * NQ, PAD = D + 4;
+    __shared__ __attribute__((aligned(16))) float join[NW * 16 * PAD];
     __shared__ float2 ml[NW * ROWS];                                      // maxima and sums
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    unsigned id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int tile0 = id % a.row_tiles;
-    id /= a.row_tiles;
-    const int head = id % a.Hkv, b = id / a.Hkv;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int head = blockIdx.x, b = blockIdx.y, split = a.row_tiles == 1 ? blockIdx.z : blockIdx.z / a.row_tiles;
+    const int tile0 = blockIdx.z - split * a.row_tiles;
+    // The request's numbers and the first chunks' page numbers are requested together.  Pages: of the keys that the lane loads
+    // ((i / 4) * 16 + 4 t + i % 4 for tile t), and of those it owns; what the table says behind the last key does not
+    // matter: the mask keeps it out.
+    const int32_t *table = a.table + (int64_t)b * a.max_pages;
+    const int page1 = (1 << a.page_log2) - 1, k0 = split * a.split_keys, c0 = (k0 >> 6) + wave;
+    auto page_of = [&](int key) { return table[min(key >> a.page_log2, (int)a.max_pages - 1)]; };
+    auto inside = [&](int p) { return (unsigned)p < (unsigned)a.n_pages; };
+    int first[4] = {page_of(c0 * 64 + (i >> 2) * 16), page_of(c0 * 64 + g * 16), page_of((c0 + NW) * 64 + (i >> 2) * 16), page_of((c0 + NW) * 64 + g * 16)};
     const Request rq = request_of(a, b);
     const int ns = splits_of(rq.L, a.split_keys, a.splits), rows = rq.n * a.group;
     if (split >= ns) return;
-    const int32_t *table = a.table + (int64_t)b * a.max_pages;
 
+    const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
     for (int tile = tile0; tile * ROWS < rows; tile += a.row_tiles) {
         // the rows' queries as the second operand of the first product: lane (row i, group g) holds d = 64 h + 16 g + 0..15
         half8_t q[NQ][KH][2];
+        float q128[NQ];            // 128 times the sum of the row
         int seen[NQ];              // keys that the lane's row sees
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -99,13 +112,22 @@ __global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
                     q[n][h][s] = *reinterpret_cast<const half8_t *>(src + 64 * h + 8 * s);
                     if (!on) q[n][h][s] = half8_t{};
                 }
+            float sum = 0.0f;
+#pragma unroll
+            for (int h = 0; h < KH; ++h)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{q[n][h][s][e], q[n][h][s][e + 1]}, ones, sum, false);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            q128[n] = 128.0f * sum;
         }
         const int t_first = tile * ROWS / a.group, t_last = min(tile * ROWS + ROWS, rows) - 1;
         const int all_see = rq.L - rq.n + t_first + 1;                    // keys that every row of the tile sees
-        const int k0 = split * a.split_keys;
         const int k1 = min(split == ns - 1 ? rq.L : k0 + a.split_keys, rq.L - rq.n + t_last / a.group + 1);
 
-        float M[NQ], l[NQ];
+        float M[NQ], l[NQ];                                               // maximum, sum of w 2^-e_v
         float4_t o[NQ][DT];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -113,27 +135,31 @@ __global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[n][d] = float4_t{};
         }
-        for (int c = (k0 >> 6) + wave; c * 64 < k1; c += NW) {
-            // pages: of the keys that the lane loads ((i / 4) * 16 + 4 t + i % 4 for tile t), and of those that it owns
-            auto page_of = [&](int key) {
-                const int at = key >> a.page_log2;
-                const int p = key < rq.L ? table[at] : -1;
-                return (unsigned)p < (unsigned)a.n_pages ? p : -1;
-            };
-            const int page1 = (1 << a.page_log2) - 1;
-            const int key_k = c * 64 + (i >> 2) * 16, key_v = c * 64 + g * 16;
-            const int pk = page_of(key_k), pv = page_of(key_v);
-            const int8_t *kp = a.kc + ((((int64_t)max(pk, 0) * a.Hkv + head) << a.page_log2) + (key_k & page1) + (i & 3)) * D + 16 * g;
-            const int8_t *vp = a.vc + (((int64_t)max(pv, 0) * a.Hkv + head) << a.page_log2) * D + (key_v & page1);
-            uint4 kraw[4][KH], vraw[DT];
+        // The chunk's bytes: requested a chunk ahead, each as soon as the registers of the one before are free; its page numbers two
+        // chunks ahead.  Loads return in the order of their requests: page numbers and scales come before the keys, so that
+        // nothing waits for the values but their product.
+        uint4 kraw[4][KH], vraw[DT];
+        int ek = 0, ev = 0, pk1, pv1;                                       // scales of this chunk; page numbers of the next one
+        bool there = true;                                                  // the lane's keys have a page
+        auto load_k = [&](int c) {
+            const int64_t at = (int64_t)(inside(pv1) ? pv1 : 0) * a.Hkv + head;
+            ek = a.ke[at], ev = a.ve[at];
+            const int8_t *src = a.kc + ((((int64_t)(inside(pk1) ? pk1 : 0) * a.Hkv + head) << a.page_log2) + ((c * 64 + (i >> 2) * 16) & page1) + (i & 3)) * D + 16 * g;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int h = 0; h < KH; ++h) kraw[t][h] = *reinterpret_cast<const uint4 *>(kp + t * 4 * D + h * 64);
+                for (int h = 0; h < KH; ++h) kraw[t][h] = *reinterpret_cast<const uint4 *>(src + t * 4 * D + h * 64);
+        };
+        auto load_v = [&](int c) {
+            const int8_t *src = a.vc + ((((int64_t)(inside(pv1) ? pv1 : 0) * a.Hkv + head) * D + i) << a.page_log2) + ((c * 64 + g * 16) & page1);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) vraw[d] = *reinterpret_cast<const uint4 *>(vp + ((int64_t)(d * 16 + i) << a.page_log2));
-            const int64_t e_at = (int64_t)max(pv, 0) * a.Hkv + head;
-            const int ek = min(max((int)a.ke[e_at], -64), 64), ev = min(max((int)a.ve[e_at], -64), 64);
+            for (int d = 0; d < DT; ++d) vraw[d] = *reinterpret_cast<const uint4 *>(src + (d * 16 << a.page_log2));
+        };
+        auto chunk = [&](int c, auto more_tag) {
+            constexpr bool more = decltype(more_tag)::value;
+            const int key_v = c * 64 + g * 16;
+            int pk2, pv2;
+            if constexpr (more) pk2 = page_of((c + 2 * NW) * 64 + (i >> 2) * 16), pv2 = page_of((c + 2 * NW) * 64 + g * 16);
 
             float4_t s[NQ][4];
 #pragma unroll
@@ -142,26 +168,32 @@ __global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
                 for (int n = 0; n < NQ; ++n) s[n][t] = float4_t{};
 #pragma unroll
                 for (int h = 0; h < KH; ++h) {
-                    const half8_t a0 = widen8(kraw[t][h].x, kraw[t][h].y), a1 = widen8(kraw[t][h].z, kraw[t][h].w);
+                    const half8_t a0 = widen_k(kraw[t][h].x, kraw[t][h].y), a1 = widen_k(kraw[t][h].z, kraw[t][h].w);
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) {
                         s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, q[n][h][0], s[n][t], 0, 0, 0);
                         s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, q[n][h][1], s[n][t], 0, 0, 0);
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);               // the fp16 form of a tile only lives that long
             }
-            const float sk = __builtin_amdgcn_ldexpf(a.scale, ek), sv = (float)ev, inv = __builtin_amdgcn_ldexpf(1.0f, -ev);
-            const bool masked = c * 64 + 64 > all_see || __any(pv < 0);
+            const int e_k = min(max(ek, -64), 64), e_v = min(max(ev, -64), 64);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more) load_k(c + NW);
+            __builtin_amdgcn_sched_barrier(0);
+            const float sk = __builtin_amdgcn_ldexpf(a.scale, e_k), sv = (float)e_v, inv = __builtin_amdgcn_ldexpf(1.0f, -e_v);
+            const bool masked = c * 64 + 64 > all_see || __any(!there);
             half8_t p[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 float x[16], top = kNone;
-                const int left = pv < 0 ? 0 : seen[n] - key_v;            // of the lane's sixteen keys, those that its row sees
+                const float sk24 = sk * kCode, base = fmaf(-sk, q128[n], sv);
+                const int left = there ? seen[n] - key_v : 0;             // of the lane's sixteen keys, those that its row sees
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        float y = fmaf(s[n][t][r], sk, sv);
+                        float y = fmaf(s[n][t][r], sk24, base);
                         if (masked) y = t * 4 + r < left ? y : -INFINITY;
                         x[t * 4 + r] = y;
                         top = fmaxf(top, y);
@@ -175,24 +207,45 @@ __global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
 #pragma unroll
                     for (int d = 0; d < DT; ++d) o[n][d] *= f;
                 }
+                const float off = M[n] - kUpLog2;
                 float sum = 0.0f;
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const float w = __builtin_amdgcn_exp2f(x[k] - M[n]);
-                    sum += w;
-                    p[n][k >> 3][k & 7] = (_Float16)(w * kUp);
+                for (int k = 0; k < 16; k += 2) {
+                    const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(x[k] - off), (_Float16)__builtin_amdgcn_exp2f(x[k + 1] - off)};
+                    sum = __builtin_amdgcn_fdot2(w, ones, sum, false);
+                    p[n][k >> 3][k & 7] = w.x;
+                    p[n][k >> 3][(k & 7) + 1] = w.y;
                 }
                 l[n] = fmaf(sum, inv, l[n]);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const half8_t a0 = widen8(vraw[d].x, vraw[d].y), a1 = widen8(vraw[d].z, vraw[d].w);
+                const half8_t a0 = widen_v(vraw[d].x, vraw[d].y), a1 = widen_v(vraw[d].z, vraw[d].w);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
                     o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, p[n][0], o[n][d], 0, 0, 0);
                     o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, p[n][1], o[n][d], 0, 0, 0);
                 }
+                if (d % 2) __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more) {
+                load_v(c + NW);
+                there = inside(pv1);
+                pk1 = pk2, pv1 = pv2;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int c = c0;
+        if (c * 64 < k1) {
+            pk1 = first[0], pv1 = first[1];
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(c);
+            load_v(c);
+            there = inside(pv1);
+            pk1 = first[2], pv1 = first[3];
+            for (; (c + NW) * 64 < k1; c += NW) chunk(c, std::true_type{});
+            chunk(c, std::false_type{});
         }
         // the lane groups' sums, then the wavefronts
 #pragma unroll
@@ -208,7 +261,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
             for (int w = 0; w < NW; ++w) most = fmaxf(most, ml[w * ROWS + n * 16 + i].x);
             const float f = __builtin_amdgcn_exp2f(M[n] - most);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) *reinterpret_cast<float4_t *>(join + (wave * 16 + i) * D + d * 16 + g * 4) = o[n][d] * f;
+            for (int d = 0; d < DT; ++d) *reinterpret_cast<float4_t *>(join + (wave * 16 + i) * PAD + d * 16 + g * 4) = o[n][d] * f;
             __syncthreads();
             for (int it = threadIdx.x; it < 16 * (D / 4); it += NW * 64) {
                 const int rr = it / (D / 4), d = it % (D / 4) * 4, r = tile * ROWS + n * 16 + rr;
@@ -219,11 +272,11 @@ __global__ __launch_bounds__(NW * 64) void attn_kv_kernel(const KvArgs a) {
                 for (int w = 0; w < NW; ++w) {
                     const float2 m = ml[w * ROWS + n * 16 + rr];
                     sum += m.y * __builtin_amdgcn_exp2f(m.x - top);
-                    acc += *reinterpret_cast<const float4_t *>(join + (w * 16 + rr) * D + d);
+                    acc += *reinterpret_cast<const float4_t *>(join + (w * 16 + rr) * PAD + d);
                 }
                 const int t = rq.first + r / a.group, h = head * a.group + r % a.group;
                 if (ns == 1) {
-                    const float f1 = sum == 0.0f ? 0.0f : 1.0f / (sum * kUp);
+                    const float f1 = sum == 0.0f ? 0.0f : 1.0f / sum;
                     _Float16 y[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) y[j] = (_Float16)(acc[j] * f1);
@@ -245,28 +298,55 @@ __global__ __launch_bounds__(256) void attn_kv_join_kernel(const KvArgs a) {
     const Request rq = request_of(a, blockIdx.y);
     const int ns = splits_of(rq.L, a.split_keys, a.splits), lane = threadIdx.x & 63;
     if (ns == 1) return;
+    constexpr int W = D / 64, AHEAD = 8;
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rq.n * a.Hq; r += gridDim.x * 4) {
         const int64_t row0 = (int64_t)rq.first * a.Hq + r, step = (int64_t)a.T * a.Hq;
-        float top = kNone;
-        for (int s = 0; s < ns; ++s) top = fmaxf(top, a.part_ml[row0 + s * step].x);
-        float sum = 0.0f, acc[D / 64] = {};
-        for (int s = 0; s < ns; ++s) {
-            const float2 ml = a.part_ml[row0 + s * step];
-            const float f = __builtin_amdgcn_exp2f(ml.x - top);
-            sum += ml.y * f;
+        // the splits' maxima and sums, one lane each (in rounds of 64), then their outputs, eight loads at a time
+        float top = kNone, sum = 0.0f, acc[W] = {};
+        for (int s0 = 0; s0 < ns; s0 += 64) {
+            const bool on = s0 + lane < ns;
+            const float2 ml = on ? a.part_ml[row0 + (s0 + lane) * step] : make_float2(kNone, 0.0f);
+            float most = ml.x;
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) acc[j] += a.part[(row0 + s * step) * D + lane * (D / 64) + j] * f;
+            for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+            const float to = fmaxf(top, most), f0 = __builtin_amdgcn_exp2f(top - to), f = on ? __builtin_amdgcn_exp2f(ml.x - to) : 0.0f;
+            float part = ml.y * f;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) part += __shfl_xor(part, m);
+            sum = sum * f0 + part;
+            top = to;
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[j] *= f0;
+            const int here = min(ns - s0, 64);
+            for (int s = 0; s < here; s += AHEAD) {
+                float x[AHEAD][W], w[AHEAD];
+#pragma unroll
+                for (int e = 0; e < AHEAD; ++e) {
+                    const float *src = a.part + (row0 + (s0 + min(s + e, here - 1)) * step) * D + lane * W;
+#pragma unroll
+                    for (int j = 0; j < W; ++j) x[e][j] = src[j];
+                    w[e] = s + e < here ? __shfl(f, min(s + e, 63)) : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) acc[j] = fmaf(x[e][j], w[e], acc[j]);
+            }
         }
-        const float f = sum == 0.0f ? 0.0f : 1.0f / (sum * kUp);
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
         const int t = rq.first + r / a.Hq, h = r % a.Hq;
+        _Float16 y[W];
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) a.o[(int64_t)t * a.ldo + h * D + lane * (D / 64) + j] = (_Float16)(acc[j] * f);
+        for (int j = 0; j < W; ++j) y[j] = (_Float16)(acc[j] * f);
+        _Float16 *dst = a.o + (int64_t)t * a.ldo + h * D + lane * W;
+        if constexpr (W == 2) *reinterpret_cast<uint32_t *>(dst) = __builtin_bit_cast(uint32_t, y);
+        else *dst = y[0];
     }
 }
 
 template <int D, int NQ, int NW>
 int launch(const KvArgs &a, hipStream_t st) {
-    attn_kv_kernel<D, NQ, NW><<<dim3((unsigned)((int64_t)a.B * a.Hkv * a.row_tiles * a.splits)), NW * 64, 0, st>>>(a);
+    attn_kv_kernel<D, NQ, NW><<<dim3((unsigned)a.Hkv, (unsigned)a.B, (unsigned)(a.row_tiles * a.splits)), NW * 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 

@@ -406,18 +406,15 @@ struct AgqKvSplit {
     int tiles, row_tiles, splits, split_keys;
 };
 static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv) {
-    const int64_t rows = max_q * (Hq / Hkv), fill = 768;
+    const int64_t rows = max_q * (Hq / Hkv);
     AgqKvSplit s;
     s.tiles = rows <= 16 ? 1 : 2;
     const int64_t row_tiles = (rows + 16 * s.tiles - 1) / (16 * s.tiles);
     s.row_tiles = (int)(row_tiles < 1 ? 1 : row_tiles > 1024 ? 1024 : row_tiles);
-    const int64_t groups = B * Hkv * s.row_tiles, most = (max_kv + 511) / 512;
-    int64_t splits = groups < 1 ? 1 : fill / groups;
-    splits = splits > most ? most : splits;
-    splits = splits < 1 ? 1 : splits;
-    int64_t keys = (max_kv + splits - 1) / splits;
+    const int64_t groups = B * Hkv * s.row_tiles;
+    int64_t keys = max_kv / 64 * groups / (2048 / 64);
     keys = (keys + 255) / 256 * 256;
-    s.split_keys = (int)(keys < 256 ? 256 : keys);
+    s.split_keys = (int)(keys < 512 ? 512 : keys > 1 << 30 ? 1 << 30 : keys);
     s.splits = (int)((max_kv + s.split_keys - 1) / s.split_keys);
     if (s.splits < 1) s.splits = 1;
     return s;
