@@ -6,8 +6,8 @@ is no CPU fallback: if the library has not been built, loading raises."""
 from __future__ import annotations
 
 import ctypes
-import math
 import os
+import struct
 from typing import NamedTuple
 
 import torch
@@ -564,31 +564,45 @@ def cascade_keep(S: int, beta: float, m: int) -> list:
 #
 # Tensors of tokens are fp16 [T, heads, D] with any distance between tokens; the caches int8 [n_pages, Hkv, page, D] (keys)
 # and [n_pages, Hkv, D, page] (values) with int8 exponents [n_pages, Hkv].  The calls below look at types, shapes and
-# layouts (a ValueError before anything is enqueued); what lies on the device is checked there.
+# layouts (a ValueError before anything is enqueued); what lies on the device is checked there.  A generation step is
+# short launches, so they do it in few Python steps (structs packed as bytes, new_empty, one look per tensor).
+
+_f16, _i8, _i32, _f32 = torch.float16, torch.int8, torch.int32, torch.float32
+_pack_cache = struct.Struct("8q").pack
+
 
 def _heads(t, name):
     """(tokens, heads, D, elements between tokens) of a fp16 [T, heads, D] tensor"""
     T, H, D = t.shape
     ld, sh, sd = t.stride()
-    if t.dtype is not torch.float16 or (T and (sd != 1 or (H > 1 and sh != D))):
+    if t.dtype is not _f16 or (T and (sd != 1 or (sh != D and H != 1))):
         raise ValueError("%s: fp16 [tokens, heads, D] with contiguous heads is wanted" % name)
-    return T, H, D, (ld if T > 1 else max(ld, H * D) if ld % 8 == 0 else H * D)
+    return T, H, D, (ld if T > 1 else H * D)
 
 
-def _ints(n, **tensors):
-    for name, t in tensors.items():
-        if t.dtype is not torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
-            raise ValueError("%s: a contiguous int32 tensor%s is wanted" % (name, "" if n is None else " of %d values" % n))
+def _like(t, shape, name):
+    """elements between the tokens of a fp16 tensor of this shape"""
+    T, H, D, ld = _heads(t, name)
+    if (T, H, D) != shape:
+        raise ValueError("%s: %s is wanted" % (name, list(shape)))
+    return ld
+
+
+def _ints(t, n, name):
+    """the address of a contiguous int32 tensor of n values"""
+    if t.dtype is not _i32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: a contiguous int32 tensor of %d values is wanted" % (name, n))
+    return t.data_ptr()
 
 
 def _kv_cache(k_cache, v_cache, k_exp, v_exp):
-    """struct agq_kv_cache as eight 8-byte values"""
+    """struct agq_kv_cache as bytes, key heads, D"""
     n_pages, Hkv, page, D = k_cache.shape
     if (v_cache.shape != (n_pages, Hkv, D, page) or k_exp.shape != (n_pages, Hkv) or v_exp.shape != (n_pages, Hkv)
-            or not (k_cache.dtype is v_cache.dtype is k_exp.dtype is v_exp.dtype is torch.int8)
+            or not (k_cache.dtype is v_cache.dtype is k_exp.dtype is v_exp.dtype is _i8)
             or not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_exp.is_contiguous() and v_exp.is_contiguous())):
         raise ValueError("cache: contiguous int8 k [n_pages, Hkv, page, D], v [n_pages, Hkv, D, page], exponents [n_pages, Hkv] are wanted")
-    return (_i64 * 8)(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), n_pages, Hkv, D, page), Hkv, D
+    return _pack_cache(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), n_pages, Hkv, D, page), Hkv, D
 
 
 class KvStep(NamedTuple):
@@ -606,20 +620,17 @@ def kv_map(kv_len, n_new, block_table, page, free_ring, free_state, T, out: KvSt
     """agq_kv_map: pages, slots and positions of one step; block_table [B, max_pages] and free_ring [n_pages] are updated.
     out: a KvStep to write into (not the one whose kv_len and free_state are passed in: a loop swaps two)."""
     B, max_pages = block_table.shape
-    _ints(B, kv_len=kv_len, n_new=n_new)
-    _ints(None, block_table=block_table, free_ring=free_ring)
-    _ints(2, free_state=free_state)
-    if out is None:
-        buf = torch.empty(2 * B + 4 + 2 * T, dtype=torch.int32, device=kv_len.device)
-        out = KvStep(*buf.split([B, B + 1, T, T, 2, 1]))
+    n_pages = free_ring.numel()
+    if out is None:                                # one allocation, cut into the six
+        buf = kv_len.new_empty(2 * B + 2 * T + 4)
+        out = KvStep._make(buf.split_with_sizes([B, B + 1, T, T, 2, 1]))
+        p = buf.data_ptr()
+        to = (p, p + 4 * B, p + 8 * B + 4, p + 8 * B + 4 * T + 4, p + 8 * B + 8 * T + 4, p + 8 * B + 8 * T + 12)
     else:
-        _ints(B, kv_len=out.kv_len)
-        _ints(T, pos=out.pos, slot=out.slot)
-        if out.cu_new.numel() != B + 1 or out.free_state.numel() != 2:
-            raise ValueError("out: a KvStep of another batch")
-    _ok(lib().agq_kv_map(kv_len.data_ptr(), n_new.data_ptr(), B, page, block_table.data_ptr(), max_pages, free_ring.data_ptr(),
-                         free_ring.numel(), free_state.data_ptr(), T, out.kv_len.data_ptr(), out.cu_new.data_ptr(), out.pos.data_ptr(),
-                         out.slot.data_ptr(), out.free_state.data_ptr(), out.status.data_ptr(), _stream()), "agq_kv_map")
+        to = [_ints(t, n, "out." + name) for t, n, name in zip(out, (B, B + 1, T, T, 2, 1), KvStep._fields)]
+    _ok(lib().agq_kv_map(_ints(kv_len, B, "kv_len"), _ints(n_new, B, "n_new"), B, page, _ints(block_table, B * max_pages, "block_table"),
+                         max_pages, _ints(free_ring, n_pages, "free_ring"), n_pages, _ints(free_state, 2, "free_state"), T, *to, _stream()),
+        "agq_kv_map")
     return out
 
 
@@ -627,33 +638,36 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     """agq_kv_append: a step's keys and values into the cache.  With rope tables (float32 [P, D/2]) and pos the keys, and
     the queries if given, are rotated first: returns (rotated q or None, rotated k), else (None, None)."""
     cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
-    T, Hk, Dk, ldk = _heads(k, "k")
-    Tv, Hv, Dv, ldv = _heads(v, "v")
-    if (Hk, Dk) != (Hkv, D) or (Tv, Hv, Dv) != (T, Hkv, D):
-        raise ValueError("k and v: [T, %d, %d] as the cache has it is wanted" % (Hkv, D))
-    _ints(T, slot=slot)
+    T = k.shape[0]
+    ldk, ldv = _like(k, (T, Hkv, D), "k"), _like(v, (T, Hkv, D), "v")
     P = Hq = ldq = ldqo = ldko = 0
+    pos_p = cos_p = sin_p = q_p = qo_p = ko_p = None
     if rope_cos is not None:
-        _ints(T, pos=pos)
         P = rope_cos.shape[0]
-        if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is torch.float32) \
+        if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is _f32) \
                 or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
             raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
-        k_out = torch.empty((T, Hkv, D), dtype=torch.float16, device=k.device) if k_out is None else k_out
-        To, Ho, Do, ldko = _heads(k_out, "k_out")
-        if (To, Ho, Do) != (T, Hkv, D):
-            raise ValueError("k_out: k's shape is wanted")
+        pos_p, cos_p, sin_p = _ints(pos, T, "pos"), rope_cos.data_ptr(), rope_sin.data_ptr()
+        if k_out is None:
+            k_out, ldko = k.new_empty(T, Hkv, D), Hkv * D
+        else:
+            ldko = _like(k_out, (T, Hkv, D), "k_out")
+        ko_p = k_out.data_ptr()
+        if q is not None:
+            Hq = q.shape[1]
+            ldq = _like(q, (T, Hq, D), "q")
+            if q_out is None:
+                q_out, ldqo = q.new_empty(T, Hq, D), Hq * D
+            else:
+                ldqo = _like(q_out, (T, Hq, D), "q_out")
+            q_p, qo_p = q.data_ptr(), q_out.data_ptr()
     elif q is not None or k_out is not None or pos is not None:
         raise ValueError("q, k_out and pos go with rope tables")
-    if q is not None:
-        Tq, Hq, Dq, ldq = _heads(q, "q")
-        q_out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device) if q_out is None else q_out
-        To, Ho, Do, ldqo = _heads(q_out, "q_out")
-        if (Tq, Dq) != (T, D) or (To, Ho, Do) != (T, Hq, D):
-            raise ValueError("q and q_out: [T, Hq, D] is wanted")
-    _ok(lib().agq_kv_append(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, slot.data_ptr(), _ptr(q), ldq, Hq, _ptr(pos), _ptr(rope_cos),
-                            _ptr(rope_sin), P, _ptr(q_out) if q is not None else None, ldqo, _ptr(k_out), ldko, _stream()), "agq_kv_append")
-    return (q_out if q is not None else None), k_out
+    if q is None and q_out is not None:
+        raise ValueError("q_out goes with q")
+    _ok(lib().agq_kv_append(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, _ints(slot, T, "slot"), q_p, ldq, Hq, pos_p, cos_p, sin_p, P, qo_p,
+                            ldqo, ko_p, ldko, _stream()), "agq_kv_append")
+    return q_out, k_out
 
 
 def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None):
@@ -661,18 +675,17 @@ def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None):
     Rows of o that belong to no sequence are not written."""
     Tq, Hq, D, ldq = _heads(q, "q")
     Tk, Hkv, Dk, ldk = _heads(k, "k")
-    Tv, Hv, Dv, ldv = _heads(v, "v")
-    B = cu_q.numel() - 1
-    _ints(B + 1, cu_q=cu_q, cu_k=cu_k)
-    if Dk != D or (Tv, Hv, Dv) != (Tk, Hkv, D):
-        raise ValueError("k and v: [Tk, Hkv, %d] are wanted" % D)
-    o = torch.empty((Tq, Hq, D), dtype=torch.float16, device=q.device) if o is None else o
-    To, Ho, Do, ldo = _heads(o, "o")
-    if (To, Ho, Do) != (Tq, Hq, D):
-        raise ValueError("o: q's shape is wanted")
-    _ok(lib().agq_attn_packed(q.data_ptr(), ldq, Tq, Hq, k.data_ptr(), ldk, v.data_ptr(), ldv, Tk, Hkv, D, cu_q.data_ptr(), cu_k.data_ptr(),
-                              B, 1 if causal else 0, 1.0 / math.sqrt(D) if scale is None else scale, o.data_ptr(), ldo, _stream()),
-        "agq_attn_packed")
+    if Dk != D:
+        raise ValueError("q and k: the same D is wanted")
+    ldv = _like(v, (Tk, Hkv, D), "v")
+    n = cu_q.numel()
+    if o is None:
+        o, ldo = q.new_empty(Tq, Hq, D), Hq * D
+    else:
+        ldo = _like(o, (Tq, Hq, D), "o")
+    _ok(lib().agq_attn_packed(q.data_ptr(), ldq, Tq, Hq, k.data_ptr(), ldk, v.data_ptr(), ldv, Tk, Hkv, D, _ints(cu_q, n, "cu_q"),
+                              _ints(cu_k, n, "cu_k"), n - 1, 1 if causal else 0, D ** -0.5 if scale is None else scale, o.data_ptr(), ldo,
+                              _stream()), "agq_attn_packed")
     return o
 
 
@@ -685,19 +698,18 @@ def attn_kv(q, cu_q, kv_len, block_table, k_cache, v_cache, k_exp, v_exp, max_q,
     cache.  max_q, max_kv: the largest number of new tokens and of tokens in the cache, as the program knows them."""
     cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
     T, Hq, Dq, ldq = _heads(q, "q")
-    B, max_pages = block_table.shape
-    _ints(B, kv_len=kv_len)
-    _ints(B + 1, cu_q=cu_q)
-    _ints(None, block_table=block_table)
     if Dq != D:
         raise ValueError("q: [T, Hq, %d] as the cache has it is wanted" % D)
-    o = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device) if o is None else o
-    To, Ho, Do, ldo = _heads(o, "o")
-    if (To, Ho, Do) != (T, Hq, D):
-        raise ValueError("o: q's shape is wanted")
+    B, max_pages = block_table.shape
+    if o is None:
+        o, ldo = q.new_empty(T, Hq, D), Hq * D
+    else:
+        ldo = _like(o, (T, Hq, D), "o")
     if workspace is None:
-        workspace = _scratch(lib().agq_attn_kv_workspace_bytes(T, Hq, Hkv, D, B, max_q, max_kv), q.device)
-    _ok(lib().agq_attn_kv(cache, q.data_ptr(), ldq, T, Hq, cu_q.data_ptr(), kv_len.data_ptr(), B, block_table.data_ptr(), max_pages, max_q,
-                          max_kv, 1.0 / math.sqrt(D) if scale is None else scale, o.data_ptr(), ldo, _ptr(workspace),
+        need = lib().agq_attn_kv_workspace_bytes(T, Hq, Hkv, D, B, max_q, max_kv)
+        workspace = k_cache.new_empty(need) if need else None
+    _ok(lib().agq_attn_kv(cache, q.data_ptr(), ldq, T, Hq, _ints(cu_q, B + 1, "cu_q"), _ints(kv_len, B, "kv_len"), B,
+                          _ints(block_table, B * max_pages, "block_table"), max_pages, max_q, max_kv, D ** -0.5 if scale is None else scale,
+                          o.data_ptr(), ldo, None if workspace is None else workspace.data_ptr(),
                           0 if workspace is None else workspace.nbytes, _stream()), "agq_attn_kv")
     return o
