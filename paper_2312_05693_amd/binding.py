@@ -582,10 +582,11 @@ def _heads(t, name):
 
 def _like(t, shape, name):
     """elements between the tokens of a fp16 tensor of this shape"""
-    T, H, D, ld = _heads(t, name)
-    if (T, H, D) != shape:
-        raise ValueError("%s: %s is wanted" % (name, list(shape)))
-    return ld
+    ld, sh, sd = t.stride()
+    T, H, D = shape
+    if t.shape != shape or t.dtype is not _f16 or (T and (sd != 1 or (sh != D and H != 1))):
+        raise ValueError("%s: fp16 %s with contiguous heads is wanted" % (name, list(shape)))
+    return ld if T > 1 else H * D
 
 
 def _ints(t, n, name):
@@ -638,8 +639,9 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     """agq_kv_append: a step's keys and values into the cache.  With rope tables (float32 [P, D/2]) and pos the keys, and
     the queries if given, are rotated first: returns (rotated q or None, rotated k), else (None, None)."""
     cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
-    T = k.shape[0]
-    ldk, ldv = _like(k, (T, Hkv, D), "k"), _like(v, (T, Hkv, D), "v")
+    T = slot.numel()
+    shape = T, Hkv, D
+    ldk, ldv = _like(k, shape, "k"), _like(v, shape, "v")
     P = Hq = ldq = ldqo = ldko = 0
     pos_p = cos_p = sin_p = q_p = qo_p = ko_p = None
     if rope_cos is not None:
@@ -651,7 +653,7 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
         if k_out is None:
             k_out, ldko = k.new_empty(T, Hkv, D), Hkv * D
         else:
-            ldko = _like(k_out, (T, Hkv, D), "k_out")
+            ldko = _like(k_out, shape, "k_out")
         ko_p = k_out.data_ptr()
         if q is not None:
             Hq = q.shape[1]

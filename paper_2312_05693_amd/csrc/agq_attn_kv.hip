@@ -70,12 +70,12 @@ __device__ __forceinline__ Request request_of(const KvArgs &a, int b) {
     return {q0, q1 - q0, (int)min((int64_t)max(a.kv_len[b], 0), cap)};
 }
 
-// One workgroup of NW wavefronts: NQ tiles of sixteen rows of one key head of one request, over one split of its keys;
+// One workgroup of NW wavefronts (four or eight): NQ tiles of sixteen rows of one key head of one request, over one split of its keys;
 // the wavefronts take the chunks of 64 keys in turn.
 template <int D, int NQ, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
     constexpr int KH = D / 64, DT = D / 16, ROWS = 16 * NQ, PAD = D + 4;
-    __shared__ __attribute__((aligned(16))) float join[NW * 16 * PAD];
+    __shared__ __attribute__((aligned(16))) float join[4 * 16 * PAD];
     __shared__ float2 ml[NW * ROWS];                                      // maxima and sums
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -186,18 +186,21 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
             half8_t p[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                float x[16], top = kNone;
-                const float sk24 = sk * kCode, base = fmaf(-sk, q128[n], sv);
-                const int left = there ? seen[n] - key_v : 0;             // of the lane's sixteen keys, those that its row sees
+                if (masked) {
+                    asm volatile("");                                     // a branch, not selects in every chunk
+                    const int left = there ? seen[n] - key_v : 0;         // of the lane's sixteen keys, those that its row sees
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][t][r] = t * 4 + r < left ? s[n][t][r] : -INFINITY;
+                }
+                float top = -INFINITY;                                    // the sixteen have one page and so one scale
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float y = fmaf(s[n][t][r], sk24, base);
-                        if (masked) y = t * 4 + r < left ? y : -INFINITY;
-                        x[t * 4 + r] = y;
-                        top = fmaxf(top, y);
-                    }
+                    for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][t][r]);
+                const float sk24 = sk * kCode, base = fmaf(-sk, q128[n], sv);
+                top = fmaf(top, sk24, base);
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 if (__any(top > M[n])) {
@@ -207,11 +210,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
 #pragma unroll
                     for (int d = 0; d < DT; ++d) o[n][d] *= f;
                 }
-                const float off = M[n] - kUpLog2;
+                const float off = base - (M[n] - kUpLog2);
                 float sum = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(x[k] - off), (_Float16)__builtin_amdgcn_exp2f(x[k + 1] - off)};
+                    const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][k & 3], sk24, off)),
+                                       (_Float16)__builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][(k & 3) + 1], sk24, off))};
                     sum = __builtin_amdgcn_fdot2(w, ones, sum, false);
                     p[n][k >> 3][k & 7] = w.x;
                     p[n][k >> 3][(k & 7) + 1] = w.y;
@@ -261,19 +265,32 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
             for (int w = 0; w < NW; ++w) most = fmaxf(most, ml[w * ROWS + n * 16 + i].x);
             const float f = __builtin_amdgcn_exp2f(M[n] - most);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) *reinterpret_cast<float4_t *>(join + (wave * 16 + i) * PAD + d * 16 + g * 4) = o[n][d] * f;
+            for (int d = 0; d < DT; ++d) o[n][d] *= f;
+            float4_t *mine = reinterpret_cast<float4_t *>(join + ((wave & 3) * 16 + i) * PAD + g * 4);
+            if constexpr (NW == 8) {                                      // the upper four into the lower four
+                if (wave >= 4)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) mine[d * 4] = o[n][d];
+                __syncthreads();
+                if (wave < 4)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] += mine[d * 4];
+            }
+            if (wave < 4)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) mine[d * 4] = o[n][d];
             __syncthreads();
             for (int it = threadIdx.x; it < 16 * (D / 4); it += NW * 64) {
                 const int rr = it / (D / 4), d = it % (D / 4) * 4, r = tile * ROWS + n * 16 + rr;
                 if (r >= rows) continue;
                 float top = kNone, sum = 0.0f;
                 for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w * ROWS + n * 16 + rr].x);
-                float4_t acc = {};
                 for (int w = 0; w < NW; ++w) {
                     const float2 m = ml[w * ROWS + n * 16 + rr];
                     sum += m.y * __builtin_amdgcn_exp2f(m.x - top);
-                    acc += *reinterpret_cast<const float4_t *>(join + (w * 16 + rr) * PAD + d);
                 }
+                float4_t acc = {};
+                for (int w = 0; w < 4; ++w) acc += *reinterpret_cast<const float4_t *>(join + (w * 16 + rr) * PAD + d);
                 const int t = rq.first + r / a.group, h = head * a.group + r % a.group;
                 if (ns == 1) {
                     const float f1 = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -366,9 +383,9 @@ int agq_launch_attn_kv(const AgqAttnKv &p, const AgqKvSplit &sp, void *workspace
     hipStream_t st = (hipStream_t)stream;
     int err;
     if (p.D == 128)
-        err = sp.tiles == 1 ? launch<128, 1, 4>(a, st) : launch<128, 2, 4>(a, st);
+        err = sp.tiles == 2 ? launch<128, 2, 4>(a, st) : sp.waves == 8 ? launch<128, 1, 8>(a, st) : launch<128, 1, 4>(a, st);
     else
-        err = sp.tiles == 1 ? launch<64, 1, 4>(a, st) : launch<64, 2, 4>(a, st);
+        err = sp.tiles == 2 ? launch<64, 2, 4>(a, st) : sp.waves == 8 ? launch<64, 1, 8>(a, st) : launch<64, 1, 4>(a, st);
     if (err || a.splits == 1) return err;
     const int64_t rows = p.max_q * p.Hq;
     const dim3 grid((unsigned)(rows < 4 * 1024 ? (rows + 3) / 4 : 1024), (unsigned)p.B);

@@ -400,10 +400,18 @@ struct AgqAttnKv {
     const int32_t *cu_q, *kv_len, *block_table;
     float scale;
 };
-// How attention over the cache is dealt out: 16 * tiles rows (new tokens x query heads of a key head) per workgroup,
-// row_tiles workgroups over the rows, splits over the keys with split_keys keys each (a multiple of 64).
+// How attention over the cache is dealt out: 16 * tiles rows (new tokens x query heads of a key head) and `waves` wavefronts
+// per workgroup, row_tiles workgroups over the rows, splits over the keys with split_keys keys each (a multiple of 64), and
+// with more than one a second launch that joins them.  groups = workgroups without a split.  Measured in a replayed graph (32
+// query heads on 8 key heads, D = 128, B requests x tokens):
+//   one workgroup of eight wavefronts per CU or less, and few keys: no split, as its launch costs more than it saves (8 x 500 7.5 us;
+//     1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against 17.6, 32 x 2000 24.3 against 28.2
+//   a request's keys on eight workgroups or more: eight wavefronts each, 1024 keys at least (1 x 30000 19.0 us against 21.2 with four and
+//     512; 4 x 131072 192.6 against 202)
+//   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 27.5 us against 32.7
+//     with eight, 128 x 16..4096 46.6 against 56.3)
 struct AgqKvSplit {
-    int tiles, row_tiles, splits, split_keys;
+    int tiles, row_tiles, splits, split_keys, waves;
 };
 static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv) {
     const int64_t rows = max_q * (Hq / Hkv);
@@ -412,11 +420,23 @@ static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_
     const int64_t row_tiles = (rows + 16 * s.tiles - 1) / (16 * s.tiles);
     s.row_tiles = (int)(row_tiles < 1 ? 1 : row_tiles > 1024 ? 1024 : row_tiles);
     const int64_t groups = B * Hkv * s.row_tiles;
-    int64_t keys = max_kv / 64 * groups / (2048 / 64);
-    keys = (keys + 255) / 256 * 256;
-    s.split_keys = (int)(keys < 512 ? 512 : keys > 1 << 30 ? 1 << 30 : keys);
-    s.splits = (int)((max_kv + s.split_keys - 1) / s.split_keys);
-    if (s.splits < 1) s.splits = 1;
+    if (s.tiles == 1 && groups <= 256 && max_kv <= (groups > 128 ? 4096 : 1024)) {
+        s.waves = 8, s.splits = 1, s.split_keys = 1 << 30;
+        return s;
+    }
+    auto split = [&](int64_t least, int64_t fill) {          // about `fill` workgroups: 2048 of them at most for one request
+        int64_t keys = max_kv / 64 * groups / (fill / 64);
+        keys = (keys + 255) / 256 * 256;
+        s.split_keys = (int)(keys < least ? least : keys > 1 << 30 ? 1 << 30 : keys);
+        s.splits = (int)((max_kv + s.split_keys - 1) / s.split_keys);
+        if (s.splits < 1) s.splits = 1;
+    };
+    s.waves = 8;
+    split(1024, 512);
+    if (s.tiles == 2 || s.splits < 8) {
+        s.waves = 4;
+        split(512, 2048);
+    }
     return s;
 }
 int agq_launch_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int page, int32_t *block_table, int64_t max_pages,
