@@ -148,40 +148,40 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     // 256 bytes: a row's pieces are permuted by the row so that the sixteen rows (keys) or the four rows of 64 bytes (values) of a
     // read meet every bank once.
     const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
-    const _Float16 *kbase = a.k + (int64_t)tl.k0 * a.ldk + kv * D, *vbase = a.v + (int64_t)tl.k0 * a.ldv + kv * D;
     auto key_place = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
     auto value_place = [](int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; };
     uint32_t k_off[COPIES], v_off[COPIES];
-    auto offsets = [&](int limit) {                                // rows from `limit` on are replaced by the last one
+    auto offsets = [&](uint32_t (&at)[COPIES], int ld, auto place, int rows) {     // rows behind the last one are replaced by it
 #pragma unroll
         for (int j = 0; j < COPIES; ++j) {
-            const int r = (wave * COPIES + j) * (64 / PIECES) + lane / PIECES, at = lane % PIECES, from = min(r, limit - 1);
-            k_off[j] = (uint32_t)(from * (int)a.ldk + (at ^ key_place(r)) * 8) * 2;
-            v_off[j] = (uint32_t)(from * (int)a.ldv + (at ^ value_place(r)) * 8) * 2;
+            const int r = (wave * COPIES + j) * (64 / PIECES) + lane / PIECES;
+            at[j] = (uint32_t)(min(r, rows - 1) * ld + ((lane % PIECES) ^ place(r)) * 8) * 2;
         }
     };
-    offsets(32);
+    offsets(k_off, (int)a.ldk, key_place, 32);
+    offsets(v_off, (int)a.ldv, value_place, 32);
+    const int cut = tl.m % 32 ? tl.m >> 5 : -1;                    // the sub-tile that ends behind the sequence
+    const int64_t k_step = a.ldk * 64, v_step = a.ldv * 64;        // bytes
+    const uint8_t *k_src = reinterpret_cast<const uint8_t *>(a.k + (int64_t)tl.k0 * a.ldk + kv * D);
+    const uint8_t *v_src = reinterpret_cast<const uint8_t *>(a.v + (int64_t)tl.k0 * a.ldv + kv * D);
     int k_next = 0, v_next = 0;                                    // sub-tiles to be copied next
-    uint32_t k_slot = 0, v_slot = 0;
-    const uint32_t part = wave * (COPIES * 1024);
+    uint32_t k_slot = base + wave * (COPIES * 1024), v_slot = k_slot + 3 * SUB;
+    const uint32_t k_end = k_slot + 2 * SUB, v_end = v_slot + 2 * SUB;
     auto copy_k = [&] {                                            // behind the last one: the last one again, into a slot nobody reads
-        const int u = min(k_next, steps - 1);
-        if (u * 32 + 32 > tl.m) offsets(tl.m - u * 32);
-        const _Float16 *src = kbase + (int64_t)(u * 32) * a.ldk;
-        lds_dma16_s<0, 0>(k_off[0], src, base + k_slot + part);
-        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(k_off[COPIES - 1], src, base + k_slot + part);
+        if (k_next == cut) offsets(k_off, (int)a.ldk, key_place, tl.m & 31);
+        lds_dma16_s<0, 0>(k_off[0], k_src, k_slot);
+        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(k_off[COPIES - 1], k_src, k_slot);
+        k_src += k_next < steps - 1 ? k_step : 0;
         ++k_next;
-        k_slot = k_slot == 2 * SUB ? 0 : k_slot + SUB;
+        k_slot = k_slot == k_end ? k_end - 2 * SUB : k_slot + SUB;
     };
     auto copy_v = [&] {
-        const int u = min(v_next, steps - 1);
-        if (u * 32 + 32 > tl.m) offsets(tl.m - u * 32);
-        else if (k_next * 32 > tl.m) offsets(32);
-        const _Float16 *src = vbase + (int64_t)(u * 32) * a.ldv;
-        lds_dma16_s<0, 0>(v_off[0], src, base + 3 * SUB + v_slot + part);
-        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(v_off[COPIES - 1], src, base + 3 * SUB + v_slot + part);
+        if (v_next == cut) offsets(v_off, (int)a.ldv, value_place, tl.m & 31);
+        lds_dma16_s<0, 0>(v_off[0], v_src, v_slot);
+        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(v_off[COPIES - 1], v_src, v_slot);
+        v_src += v_next < steps - 1 ? v_step : 0;
         ++v_next;
-        v_slot = v_slot == 2 * SUB ? 0 : v_slot + SUB;
+        v_slot = v_slot == v_end ? v_end - 2 * SUB : v_slot + SUB;
     };
 
     // operand reads: piece 2 st + h of row i; columns 32 d .. + 31 of rows 16 st + 8 e + 4 h .. + 3
@@ -207,18 +207,21 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     for (int d = 0; d < DT; ++d) o[d] = float16_t{};
     const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
 
+    auto max3 = [](float x, float y, float z) { return fmaxf(fmaxf(x, y), z); };
     auto top_of = [&](const float16_t &s) {
-        float t[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) t[r] = fmaxf(fmaxf(fmaxf(s[4 * r], s[4 * r + 1]), s[4 * r + 2]), s[4 * r + 3]);
-        const float x = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-        return fmaxf(x, __shfl_xor(x, 32));
+        const float t0 = max3(s[0], s[1], s[2]), t1 = max3(s[3], s[4], s[5]), t2 = max3(s[6], s[7], s[8]), t3 = max3(s[9], s[10], s[11]);
+        const uint32_t x = __float_as_uint(max3(max3(t0, t1, s[15]), max3(t2, t3, s[14]), max3(s[12], s[13], t0)));
+        const auto both = __builtin_amdgcn_permlane32_swap(x, x, false, false);      // the other sixteen keys of the query
+        return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
     };
     auto weigh = [&](const float16_t &s, half8_t (&p)[2], int g) {   // scores 2 g and 2 g + 1
         const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * g], c, -off)), (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * g + 1], c, -off))};
-        p[g >> 2][2 * (g & 3)] = w.x;
-        p[g >> 2][2 * (g & 3) + 1] = w.y;
-        l = __builtin_amdgcn_fdot2(w, ones, l, false);
+        uint32_t bits = __builtin_bit_cast(uint32_t, w);
+        asm volatile("" : "+v"(bits));                             // here, beside the matrix instructions, not where p is used
+        uint4_t all = __builtin_bit_cast(uint4_t, p[g >> 2]);
+        all[g & 3] = bits;
+        p[g >> 2] = __builtin_bit_cast(half8_t, all);
+        l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, bits), ones, l, false);
     };
 
     uint32_t k_rd = 0, v_rd = 0;                                   // slots of sub-tiles u + 1 and u - 1
