@@ -9,6 +9,8 @@
 #include "agq_device.h"
 #include "agq_internal.h"
 
+#include <type_traits>
+
 namespace {
 
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
@@ -107,7 +109,8 @@ __device__ __forceinline__ void meet() {
 
 // Keys go by in sub-tiles of 32.  In step u the scores of sub-tile u + 1 and the product with the values of sub-tile u - 1 run on
 // the matrix cores while the vector ALU turns the scores of sub-tile u into probabilities: three independent pieces of
-// work, dealt out one matrix instruction at a time.  Copies into LDS run two steps ahead (rings of three).
+// work, dealt out one matrix instruction at a time.  The wavefronts meet every two steps; copies into LDS run two ahead (rings
+// of four).
 // Rows' reference: a probability is 2^(c s - off); off is raised to the row's maximum (less 10) only when a score is five
 // above it, so the accumulators are seldom rescaled and a weight stays below 2^15.
 template <int D>
@@ -115,7 +118,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     constexpr int KS = D / 16, DT = D / 32;                        // matrix instructions for a sub-tile's scores; d tiles of the output
     constexpr int PIECES = D / 8, ROW = D * 2, SUB = 32 * ROW;     // 16-byte pieces and bytes of a row, bytes of a sub-tile
     constexpr int COPIES = SUB / 4096;                             // a wavefront's copies (1 KiB each) of a sub-tile
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[6 * SUB];       // keys' ring, values' ring
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[8 * SUB];       // keys' ring, values' ring
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // heads that share keys go to one XCD (workgroups go around the eight of them)
@@ -165,29 +168,28 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     const uint8_t *k_src = reinterpret_cast<const uint8_t *>(a.k + (int64_t)tl.k0 * a.ldk + kv * D);
     const uint8_t *v_src = reinterpret_cast<const uint8_t *>(a.v + (int64_t)tl.k0 * a.ldv + kv * D);
     int k_next = 0, v_next = 0;                                    // sub-tiles to be copied next
-    uint32_t k_slot = base + wave * (COPIES * 1024), v_slot = k_slot + 3 * SUB;
-    const uint32_t k_end = k_slot + 2 * SUB, v_end = v_slot + 2 * SUB;
+    const uint32_t part = base + wave * (COPIES * 1024);
     auto copy_k = [&] {                                            // behind the last one: the last one again, into a slot nobody reads
         if (k_next == cut) offsets(k_off, (int)a.ldk, key_place, tl.m & 31);
-        lds_dma16_s<0, 0>(k_off[0], k_src, k_slot);
-        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(k_off[COPIES - 1], k_src, k_slot);
+        const uint32_t to = part + (k_next & 3) * SUB;
+        lds_dma16_s<0, 0>(k_off[0], k_src, to);
+        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(k_off[COPIES - 1], k_src, to);
         k_src += k_next < steps - 1 ? k_step : 0;
         ++k_next;
-        k_slot = k_slot == k_end ? k_end - 2 * SUB : k_slot + SUB;
     };
     auto copy_v = [&] {
         if (v_next == cut) offsets(v_off, (int)a.ldv, value_place, tl.m & 31);
-        lds_dma16_s<0, 0>(v_off[0], v_src, v_slot);
-        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(v_off[COPIES - 1], v_src, v_slot);
+        const uint32_t to = part + (4 + (v_next & 3)) * SUB;
+        lds_dma16_s<0, 0>(v_off[0], v_src, to);
+        if constexpr (COPIES == 2) lds_dma16_s<1024, 0>(v_off[COPIES - 1], v_src, to);
         v_src += v_next < steps - 1 ? v_step : 0;
         ++v_next;
-        v_slot = v_slot == v_end ? v_end - 2 * SUB : v_slot + SUB;
     };
 
     // operand reads: piece 2 st + h of row i; columns 32 d .. + 31 of rows 16 st + 8 e + 4 h .. + 3
-    const uint32_t k_lane = (uint32_t)(i * ROW) + (uint32_t)((h ^ key_place(i)) << 4);
+    const uint32_t k_lane = base + (uint32_t)(i * ROW) + (uint32_t)((h ^ key_place(i)) << 4);
     const int tr_row = 4 * h + ((lane & 15) >> 2), tr_col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-    const uint32_t v_lane = (uint32_t)(tr_row * ROW) + (uint32_t)(((tr_col >> 3) ^ value_place(tr_row)) << 4) + (tr_col & 7) * 2;
+    const uint32_t v_lane = base + 4 * SUB + (uint32_t)(tr_row * ROW) + (uint32_t)(((tr_col >> 3) ^ value_place(tr_row)) << 4) + (tr_col & 7) * 2;
     auto read_k = [&](uint32_t at, int st) { return read_lds(at ^ (uint32_t)(st << 5)); };
     auto read_v = [&](uint32_t at, int d, int st) {
         union {
@@ -224,19 +226,19 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, bits), ones, l, false);
     };
 
-    uint32_t k_rd = 0, v_rd = 0;                                   // slots of sub-tiles u + 1 and u - 1
+    auto slot = [](int u) { return (uint32_t)(u & 3) * SUB; };
 
     // every step that has something at the mask, at the beginning or at the end
-    auto scores = [&](float16_t &s) {
-        const uint32_t at = base + k_rd + k_lane;
+    auto scores = [&](int u, float16_t &s) {
+        const uint32_t at = k_lane + slot(u);
         s = float16_t{};
 #pragma unroll
         for (int st = 0; st < KS; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_k(at, st), q[st], s, 0, 0, 0);
     };
-    auto step_plain = [&](int u) {                                 // scores in s0, probabilities of the sub-tile before in p1
-        if (u + 1 < mine) scores(s1);
+    auto step_plain = [&](int u) __attribute__((always_inline)) {                                 // scores in s0, probabilities of the sub-tile before in p1
+        if (u + 1 < mine) scores(u + 1, s1);
         if (u > 0 && u - 1 < mine) {
-            const uint32_t at = base + 3 * SUB + v_rd + v_lane;
+            const uint32_t at = v_lane + slot(u - 1);
             // values under the mask must not reach the rows that do not see them (0 times an infinity is NaN): infinities and
             // NaN are left out of the product and added where they are seen
             const bool cut = u > whole;
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
                         for (int e = 0; e < 16; ++e) {
                             const int col = d * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
                             const _Float16 x = *(const __attribute__((address_space(3))) _Float16 *)(uintptr_t)(
-                                base + 3 * SUB + v_rd + r * ROW + (((col >> 3) ^ value_place(r)) << 4) + (col & 7) * 2);
+                                base + 4 * SUB + slot(u - 1) + r * ROW + (((col >> 3) ^ value_place(r)) << 4) + (col & 7) * 2);
                             if ((__builtin_bit_cast(uint16_t, x) & 0x7C00u) == 0x7C00u) o[d][e] += (float)x;
                         }
             }
@@ -291,72 +293,90 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         s0 = s1;
     };
 
-    // the others: sub-tiles u and u - 1 seen whole, u + 1 there
-    auto step_full = [&](float16_t &s, float16_t &s_next, half8_t (&p)[2], const half8_t (&p_before)[2]) {
-        const uint32_t at_k = base + k_rd + k_lane, at_v = base + 3 * SUB + v_rd + v_lane;
-        half8_t kf[KS], vf[2 * DT];
-        constexpr int AHEAD = 3;
+    // the others: sub-tiles u and u - 1 seen whole, u + 1 there.  The first fragments of a step are read at the end of the one
+    // before it (in `fr`) unless the wavefronts meet in between.
+    constexpr int AHEAD = 3;
+    struct Fragments {
+        half8_t k[KS + AHEAD], v[KS + AHEAD];                      // KS == 2 DT: as many products with values
+    };
+    auto first_reads = [&](int u, Fragments &fr) {
         unroll<AHEAD>([&](auto n) {
-            kf[n.value] = read_k(at_k, n.value);
-            vf[n.value] = read_v(at_v, n.value % DT, n.value / DT);
+            fr.k[n.value] = read_k(k_lane + slot(u + 1), n.value);
+            fr.v[n.value] = read_v(v_lane + slot(u - 1), n.value % DT, n.value / DT);
         });
-        __builtin_amdgcn_sched_barrier(0);
-        const float top = top_of(s), over = fmaf(top, c, -off);
-        float f = 1.0f;
-        const bool raise = __any(over > kSlack + kUpLog2);
-        if (raise) {
-            const float to = over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off;
-            f = __builtin_amdgcn_exp2f(off - to);
-            off = to;
-            l *= f;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        unroll<KS>([&](auto n) {                                   // KS == 2 DT
-            constexpr int N = n.value;
-            if constexpr (N == 0) s_next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[0], q[0], float16_t{}, 0, 0, 0);
-            else s_next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[N], q[N], s_next, 0, 0, 0);
-            if constexpr (N + AHEAD < KS) kf[N + AHEAD] = read_k(at_k, N + AHEAD);
-            weigh(s, p, N * 8 / KS);
-            __builtin_amdgcn_sched_barrier(0);
-            o[N % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[N], p_before[N / DT], o[N % DT], 0, 0, 0);
-            if constexpr (N + AHEAD < KS) vf[N + AHEAD] = read_v(at_v, (N + AHEAD) % DT, (N + AHEAD) / DT);
-            if constexpr (KS == 4) weigh(s, p, 2 * N + 1);
+    };
+    auto step_full = [&](int u, float16_t &s, float16_t &s_next, half8_t (&p)[2], const half8_t (&p_before)[2], Fragments &fr, auto more_tag) {
+        constexpr bool MORE = decltype(more_tag)::value;           // the next step follows at once
+        const uint32_t at_k = k_lane + slot(u + 1), at_v = v_lane + slot(u - 1), next_k = k_lane + slot(u + 2), next_v = v_lane + slot(u);
+        float f = 1.0f, over = 0.0f, top = 0.0f;
+        bool raise = false;
+        unroll<2 * KS>([&](auto n) {
+            constexpr int N = n.value / 2, R = N + AHEAD;
+            if constexpr (n.value % 2 == 0) {
+                if constexpr (N == 0) s_next = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr.k[0], q[0], float16_t{}, 0, 0, 0);
+                else s_next = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr.k[N], q[N], s_next, 0, 0, 0);
+                if constexpr (R < KS) fr.k[R] = read_k(at_k, R);
+                else if constexpr (MORE) fr.k[R] = read_k(next_k, R - KS);
+            } else {
+                o[N % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr.v[N], p_before[N / DT], o[N % DT], 0, 0, 0);
+                if constexpr (R < KS) fr.v[R] = read_v(at_v, R % DT, R / DT);
+                else if constexpr (MORE) fr.v[R] = read_v(next_v, (R - KS) % DT, (R - KS) / DT);
+            }
+            // the vector ALU's share: the maximum, the reference, then two scores at a time
+            if constexpr (n.value == 0) top = top_of(s);
+            if constexpr (n.value == 1) {
+                over = fmaf(top, c, -off);
+                raise = __any(over > kSlack + kUpLog2);
+                const float to = over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off;
+                f = __builtin_amdgcn_exp2f(off - to);
+                off = to;
+                l *= f;
+            }
+            constexpr int FROM = KS == 8 ? 2 : 1, DONE = (n.value - FROM) * 8 / (2 * KS - 1 - FROM), NEXT = (n.value + 1 - FROM) * 8 / (2 * KS - 1 - FROM);
+            if constexpr (n.value >= FROM) {
+#pragma unroll
+                for (int g = DONE; g < (NEXT < 8 ? NEXT : 8); ++g) weigh(s, p, g);
+            }
             __builtin_amdgcn_sched_barrier(0);
         });
         if (raise) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= f;
         }
+        if constexpr (MORE) unroll<AHEAD>([&](auto n) { fr.k[n.value] = fr.k[KS + n.value], fr.v[n.value] = fr.v[KS + n.value]; });
     };
 
     if (steps > 0) {
-        copy_k();                                                  // sub-tiles 0, 1 and 2 of the keys, 0 of the values
+        copy_k();
         copy_k();
         copy_k();
         copy_v();
-        meet<3 * COPIES>();
-        if (mine > 0) scores(s0);
-        // Between two steps: keys' sub-tile u + 1 and values' u - 1 have landed (what the step before requested may fly), and
-        // nobody reads the slots of keys' u and values' u - 2 any more, which the next ones get.
-        auto turn = [&](int u) {
-            meet<2 * COPIES>();
-            k_rd = k_rd == 2 * SUB ? 0 : k_rd + SUB;
-            if (u > 1) v_rd = v_rd == 2 * SUB ? 0 : v_rd + SUB;
+        meet<2 * COPIES + COPIES>();
+        if (mine > 0) scores(0, s0);
+        const int full = min(whole, mine - 1);                     // steps 1 .. full - 1 are full ones
+        // Between two pairs of steps: keys' sub-tiles u + 1, u + 2 and values' u - 1, u have landed, and nobody reads the slots
+        // any more that the next ones (keys' up to u + 4, values' up to u + 2) get.
+        auto turn = [&]() __attribute__((always_inline)) {
+            meet<0>();
+            copy_k();
             copy_k();
             copy_v();
+            copy_v();
         };
-        const int full = min(whole, mine - 1);                     // steps 1 .. full - 1 are full ones
-        for (int u = 0; u <= steps;) {
-            if (u >= 1 && u + 1 < full) {
-                turn(u);
-                step_full(s0, s1, p0, p1);
-                turn(u + 1);
-                step_full(s1, s0, p1, p0);
-                u += 2;
-            } else {
-                turn(u);
-                step_plain(u);
-                ++u;
+        int u = 0;
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {                     // the first pair plain, then the full ones, then the rest
+            for (const int end = part == 0 ? 1 : steps + 1; u < end; u += 2) {
+                turn();
+#pragma unroll 1
+                for (int e = 0; e < 2; ++e) step_plain(u + e);
+            }
+            for (; u + 1 < full; u += 2) {
+                turn();
+                Fragments fr;
+                first_reads(u, fr);
+                step_full(u, s0, s1, p0, p1, fr, std::true_type{});
+                step_full(u + 1, s1, s0, p1, p0, fr, std::false_type{});
             }
         }
         __builtin_amdgcn_s_waitcnt(0x70);                          // the last copies have landed before the LDS is given back
