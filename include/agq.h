@@ -568,12 +568,16 @@ int agq_kv_append(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, con
  * over the keys j of the query's own sequence; causal != 0: query i of n sees keys j <= i + (m - n) of m, so the last
  * query sees the last key (n < m: the queries are the later part of the prompt; n > m: the first queries see nothing).
  * A row that sees no key is 0.  Keys and values that a row does not see do not reach it, infinities and NaN included.
- * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D]; cu_q, cu_k [B+1].  scale > 0, usually 1 / sqrt(D).
+ * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D], ldk and ldv at most 2^24; cu_q, cu_k [B+1].  scale > 0, usually
+ * 1 / sqrt(D).  workspace: agq_attn_packed_workspace_bytes (0, and NULL, unless there are few queries and many keys):
+ * partial results where workgroups share the keys of a tile of queries; contents are scratch.
  * Scores, maxima, sums and the accumulated output are fp32; a probability is rounded to fp16 (by 2^-11 of it at
  * most) for the product with v; the output is rounded once.                                                            */
+size_t agq_attn_packed_workspace_bytes(int64_t Tq, int64_t Hq, int64_t Tk, int64_t Hkv, int64_t D, int64_t B);
 int agq_attn_packed(const void *q_f16, int64_t ldq, int64_t Tq, int64_t Hq, const void *k_f16, int64_t ldk,
                     const void *v_f16, int64_t ldv, int64_t Tk, int64_t Hkv, int64_t D, const int32_t *cu_q,
-                    const int32_t *cu_k, int64_t B, int causal, float scale, void *o_f16, int64_t ldo, void *stream);
+                    const int32_t *cu_k, int64_t B, int causal, float scale, void *o_f16, int64_t ldo, void *workspace,
+                    size_t workspace_bytes, void *stream);
 
 /* Attention of each request's newest tokens over its pages: the same sum over the cache, for the n = cu_q[b+1] -
  * cu_q[b] tokens that are the last of the request's kv_len[b] (kv_len counts them: agq_kv_append comes first; it is

@@ -64,8 +64,9 @@ SIGNATURES = {
     "agq_stack_workspace_bytes": (_sz, [_vp, _int, _i64, _vp]),
     "agq_kv_map": (_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "agq_kv_append": (_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "agq_attn_packed_workspace_bytes": (_sz, [_i64] * 6),
     "agq_attn_packed": (_int, [_vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _int, ctypes.c_float, _vp,
-                               _i64, _vp]),
+                               _i64, _vp, _sz, _vp]),
     "agq_attn_kv_workspace_bytes": (_sz, [_i64] * 7),
     "agq_attn_kv": (_int, [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_float, _vp, _i64, _vp, _sz, _vp]),
     "agq_stack_forward": (_int, [_vp, _int, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
@@ -672,7 +673,11 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     return q_out, k_out
 
 
-def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None):
+def attn_packed_workspace_bytes(Tq, Hq, Tk, Hkv, D, B) -> int:
+    return lib().agq_attn_packed_workspace_bytes(Tq, Hq, Tk, Hkv, D, B)
+
+
+def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None, workspace=None):
     """agq_attn_packed: attention of packed sequences; q fp16 [Tq, Hq, D], k and v [Tk, Hkv, D], cu_q, cu_k int32 [B+1].
     Rows of o that belong to no sequence are not written."""
     Tq, Hq, D, ldq = _heads(q, "q")
@@ -685,9 +690,13 @@ def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None):
         o, ldo = q.new_empty(Tq, Hq, D), Hq * D
     else:
         ldo = _like(o, (Tq, Hq, D), "o")
+    if workspace is None:
+        need = lib().agq_attn_packed_workspace_bytes(Tq, Hq, Tk, Hkv, D, n - 1)
+        workspace = cu_q.new_empty(need >> 2) if need else None
     _ok(lib().agq_attn_packed(q.data_ptr(), ldq, Tq, Hq, k.data_ptr(), ldk, v.data_ptr(), ldv, Tk, Hkv, D, _ints(cu_q, n, "cu_q"),
                               _ints(cu_k, n, "cu_k"), n - 1, 1 if causal else 0, D ** -0.5 if scale is None else scale, o.data_ptr(), ldo,
-                              _stream()), "agq_attn_packed")
+                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream()),
+        "agq_attn_packed")
     return o
 
 

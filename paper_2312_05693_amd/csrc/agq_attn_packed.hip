@@ -17,7 +17,9 @@ typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -1e30f;      // the maximum of no keys
 constexpr float kUpLog2 = 10.0f;     // probabilities are 2^10 times what they are, in sum and product alike
@@ -29,8 +31,10 @@ struct PackedArgs {
     _Float16 *o;
     const int32_t *cu_q, *cu_k;
     int64_t ldq, ldk, ldv, ldo;
+    float *part;                     // [split][token][query head][D]: outputs before the division
+    float2 *part_ml;                 // [split][token][query head]: reference and sum
     float scale;                     // log2(e) times the softmax's factor
-    int Tq, Tk, B, Hq, group, causal;
+    int Tq, Tk, B, Hq, group, causal, splits, split_steps;
 };
 
 struct Tile {
@@ -73,6 +77,15 @@ __device__ __forceinline__ Tile tile_of(const PackedArgs &a, int idx, int rows) 
     Tile t = {};
     t.b = -1;
     return t;
+}
+
+// sub-tiles of 32 keys that some row of the tile sees, and the workgroups that share them
+__device__ __forceinline__ int steps_of(const PackedArgs &a, const Tile &t) {
+    const int last = min(t.row + kRows, t.n) - 1;
+    return (max(a.causal ? min(t.m - t.n + last + 1, t.m) : t.m, 0) + 31) >> 5;
+}
+__device__ __forceinline__ int splits_of(const PackedArgs &a, const Tile &t) {
+    return a.splits == 1 ? 1 : min(max((steps_of(a, t) + a.split_steps - 1) / a.split_steps, 1), a.splits);
 }
 
 // four keys of one column of a [key][d] tile in LDS: lanes 4 r + c of a group of sixteen name row r's columns 4 c .. 4 c + 3,
@@ -125,8 +138,13 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     int head = blockIdx.x % a.Hq;
     if (a.Hq % 8 == 0) head = (head & 7) * (a.Hq >> 3) + (head >> 3);
     const int kv = head / a.group;
-    const Tile tl = tile_of(a, blockIdx.x / a.Hq, kRows);
+    Tile tl = tile_of(a, blockIdx.x / a.Hq, kRows);
     if (tl.b < 0) return;
+    const int ns = splits_of(a, tl);                               // workgroups that share the tile's keys
+    if ((int)blockIdx.y >= ns) return;
+    const int key0 = blockIdx.y * a.split_steps * 32;              // the first of this one's
+    tl.k0 += key0;
+    tl.m -= key0;
     const int row = tl.row + wave * 32 + i;                        // the lane's query
     const bool on = row < tl.n;
     half8_t q[KS];
@@ -145,7 +163,9 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     const int wave_last = min(last_row, wave * 32 + 31);
     const int wave_keys = wave * 32 > last_row ? 0 : a.causal ? min(past + tl.row + wave_last + 1, tl.m) : tl.m;    // some row of the wavefront
     const int wave_all = a.causal ? min(past + tl.row + wave * 32 + 1, tl.m) : tl.m;                                // every row of it
-    const int steps = (max(all_keys, 0) + 31) >> 5, mine = (max(wave_keys, 0) + 31) >> 5, whole = max(wave_all, 0) >> 5;
+    const int there = (max(all_keys, 0) + 31) >> 5;
+    const int steps = (int)blockIdx.y == ns - 1 ? there : min(there, a.split_steps);
+    const int mine = min((max(wave_keys, 0) + 31) >> 5, steps), whole = max(wave_all, 0) >> 5;
 
     // copies: lane l of a wavefront's copy j brings the piece that belongs at place l of 1 KiB.  Sixteen lanes read LDS at a time,
     // 256 bytes: a row's pieces are permuted by the row so that the sixteen rows (keys) or the four rows of 64 bytes (values) of a
@@ -201,8 +221,9 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         return f.v;
     };
 
-    const float c = a.scale;
-    float off = kNone, l = 0.0f;
+    float c = a.scale, off = kNone, l = 0.0f;
+    if constexpr (D == 64) asm("" : "+v"(c));                      // a scalar operand takes the ALU half as long again, which bounds this one (1 %)
+                                            // products with a scalar operand take the ALU half as long again
     float16_t o[DT], s0 = {}, s1 = {};
     half8_t p0[2] = {}, p1[2] = {};
 #pragma unroll
@@ -382,34 +403,110 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         __builtin_amdgcn_s_waitcnt(0x70);                          // the last copies have landed before the LDS is given back
     }
     l += __shfl_xor(l, 32);
-    if (!on) return;
+    // Out by way of LDS (each wavefront 8 KiB of it, pieces of 16 bytes permuted by the row), so that whole rows are stored: as
+    // they lie in the registers, a store would have 16 or 32 bytes of each of 32 rows.
+    __syncthreads();
+    const uint32_t mine_lds = base + wave * 8192;
+    auto rows_out = [&](auto bytes_tag, auto &&store) {
+        constexpr int BYTES = decltype(bytes_tag)::value, N = BYTES / 16;      // of a row
+        const int r0 = lane / N, p = lane % N;
+#pragma unroll
+        for (int r = 0; r < 32; r += 64 / N) {
+            const uint32_t at = mine_lds + (r + r0) * BYTES + ((p ^ (BYTES == 256 ? (r + r0) & 15 : ((r + r0) >> 1) & 7)) << 4);
+            const uint4_t x = *(const __attribute__((address_space(3))) uint4_t *)(uintptr_t)at;
+            if (tl.row + wave * 32 + r + r0 < tl.n) store(tl.q0 + tl.row + wave * 32 + r + r0, p, x);
+        }
+    };
+    if (ns > 1) {
+        const int64_t at0 = (int64_t)blockIdx.y * a.Tq;
+        if (h == 0 && on) a.part_ml[(at0 + tl.q0 + row) * a.Hq + head] = make_float2(off, l);
+#pragma unroll
+        for (int d = 0; d < DT; d += 2) {
+#pragma unroll
+            for (int dd = 0; dd < 2; ++dd)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float4_t x = {o[d + dd][e * 4], o[d + dd][e * 4 + 1], o[d + dd][e * 4 + 2], o[d + dd][e * 4 + 3]};
+                    *(__attribute__((address_space(3))) float4_t *)(uintptr_t)(mine_lds + i * 256 + (((dd * 8 + e * 2 + h) ^ (i & 15)) << 4)) = x;
+                }
+            rows_out(Int<256>{}, [&](int t, int p, uint4_t x) { *reinterpret_cast<uint4_t *>(a.part + ((at0 + t) * a.Hq + head) * D + d * 32 + p * 4) = x; });
+        }
+        return;
+    }
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
-    _Float16 *dst = a.o + (int64_t)(tl.q0 + row) * a.ldo + head * D + 4 * h;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            _Float16 y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = (_Float16)(o[d][e * 4 + j] * f);
-            *reinterpret_cast<uint2 *>(dst + d * 32 + e * 8) = __builtin_bit_cast(uint2, y);
+            const half2_t lo = {(_Float16)(o[d][e * 4] * f), (_Float16)(o[d][e * 4 + 1] * f)}, hi = {(_Float16)(o[d][e * 4 + 2] * f), (_Float16)(o[d][e * 4 + 3] * f)};
+            const uint2_t x = {__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            *(__attribute__((address_space(3))) uint2_t *)(uintptr_t)(mine_lds + i * ROW + (((d * 4 + e) ^ key_place(i)) << 4) + h * 8) = x;
         }
+    rows_out(Int<ROW>{}, [&](int t, int p, uint4_t x) { *reinterpret_cast<uint4_t *>(a.o + (int64_t)t * a.ldo + head * D + p * 8) = x; });
+}
+
+// The workgroups of a tile joined: the same tiles and heads, D / 4 lanes to a row, 1024 / D rows to a workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void attn_packed_join_kernel(const PackedArgs a) {
+    constexpr int LANES = D / 4, AHEAD = 8;
+    const int head = blockIdx.x % a.Hq;
+    const Tile tl = tile_of(a, blockIdx.x / a.Hq, kRows);
+    if (tl.b < 0) return;
+    const int ns = splits_of(a, tl), r = blockIdx.y * (256 / LANES) + threadIdx.x / LANES;
+    if (ns == 1 || tl.row + r >= tl.n) return;
+    const int d = threadIdx.x % LANES * 4;
+    const int64_t step = (int64_t)a.Tq * a.Hq, t = tl.q0 + tl.row + r, at = t * a.Hq + head;
+    float most = kNone, sum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s = 0; s < ns; s += AHEAD) {
+        float2 ml[AHEAD];
+        float4 x[AHEAD];
+        float to = most;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const int64_t from = at + min(s + e, ns - 1) * step;
+            ml[e] = a.part_ml[from];
+            x[e] = *reinterpret_cast<const float4 *>(a.part + from * D + d);
+        }
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) to = fmaxf(to, ml[e].x);
+        const float f0 = __builtin_amdgcn_exp2f(most - to);
+        most = to;
+        sum *= f0;
+        acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const float f = s + e < ns ? __builtin_amdgcn_exp2f(ml[e].x - to) : 0.0f;
+            sum = fmaf(ml[e].y, f, sum);
+            acc.x = fmaf(x[e].x, f, acc.x), acc.y = fmaf(x[e].y, f, acc.y), acc.z = fmaf(x[e].z, f, acc.z), acc.w = fmaf(x[e].w, f, acc.w);
+        }
+    }
+    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const _Float16 y[4] = {(_Float16)(acc.x * f), (_Float16)(acc.y * f), (_Float16)(acc.z * f), (_Float16)(acc.w * f)};
+    *reinterpret_cast<uint2 *>(a.o + t * a.ldo + head * D + d) = __builtin_bit_cast(uint2, y);
+}
+
+template <int D>
+int launch(const PackedArgs &a, hipStream_t st) {
+    const unsigned groups = (unsigned)(agq_packed_tiles(a.Tq, a.B) * a.Hq);
+    attn_packed_kernel<D><<<dim3(groups, (unsigned)a.splits), 256, 0, st>>>(a);
+    const int err = (int)hipGetLastError();
+    if (err || a.splits == 1) return err;
+    attn_packed_join_kernel<D><<<dim3(groups, kRows * D / 1024), 256, 0, st>>>(a);
+    return (int)hipGetLastError();
 }
 
 }  // namespace
 
-int agq_launch_attn_packed(const AgqAttnPacked &p, void *stream) {
+int agq_launch_attn_packed(const AgqAttnPacked &p, const AgqPackedSplit &sp, void *workspace, void *stream) {
     PackedArgs a;
     a.q = (const _Float16 *)p.q, a.k = (const _Float16 *)p.k, a.v = (const _Float16 *)p.v, a.o = (_Float16 *)p.o;
     a.cu_q = p.cu_q, a.cu_k = p.cu_k;
     a.ldq = p.ldq, a.ldk = p.ldk, a.ldv = p.ldv, a.ldo = p.ldo;
     a.scale = p.scale * 1.44269504088896340736f;
     a.Tq = (int)p.Tq, a.Tk = (int)p.Tk, a.B = (int)p.B, a.Hq = (int)p.Hq, a.group = (int)(p.Hq / p.Hkv), a.causal = p.causal;
-    const int64_t tiles = p.Tq / kRows + p.B;                       // sum of ceil(n / 128) is not more
-    const dim3 grid((unsigned)(tiles * p.Hq));
-    if (p.D == 128)
-        attn_packed_kernel<128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    else
-        attn_packed_kernel<64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    return (int)hipGetLastError();
+    a.splits = sp.splits, a.split_steps = sp.split_steps;
+    a.part = (float *)workspace;
+    a.part_ml = (float2 *)(a.part + (size_t)a.splits * p.Tq * p.Hq * p.D);
+    return p.D == 128 ? launch<128>(a, (hipStream_t)stream) : launch<64>(a, (hipStream_t)stream);
 }

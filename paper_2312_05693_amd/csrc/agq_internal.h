@@ -443,5 +443,31 @@ int agq_launch_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, in
                       int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T, int32_t *kv_len_out, int32_t *cu_new,
                       int32_t *pos, int32_t *slot, int32_t *free_state_out, int32_t *status, void *stream);
 int agq_launch_kv_append(const AgqKvAppend &p, void *stream);
-int agq_launch_attn_packed(const AgqAttnPacked &p, void *stream);
+// Tiles of 128 queries of B sequences with Tq queries in all: the sum of ceil(n / 128) is not more.  (Workgroups that find no tile
+// take turns with the others in the order in which CUs get them: one spare tile for a single one left half of the CUs without
+// work, 128 queries and 4128 keys of 32 heads 29.8 us.)
+static inline int64_t agq_packed_tiles(int64_t Tq, int64_t B) { return (Tq + 127 * (B < Tq ? B : Tq)) / 128; }
+
+// How attention over packed prompts is dealt out when there are few tiles of 128 queries: split_steps sub-tiles of 32 keys to a
+// workgroup, splits workgroups at most to a tile, joined by a second launch.  A CU holds two workgroups (D = 128) or three
+// (D = 64); up to a third of that the chip is filled up, with 16 sub-tiles at least:
+// a workgroup's first and last steps and its launch take 7.5 us, a step by itself 0.5, the join 6.5 (32 heads on 8, D = 128: 128 queries and
+// 4128 keys 73 -> 29 us, 500 and 4500 79 -> 59, 128 and 1128 29 -> 26; D = 64, 1333 queries and 6333 keys, half of that: 64 -> 67).
+struct AgqPackedSplit {
+    int splits, split_steps;
+};
+static inline AgqPackedSplit agq_packed_split(int64_t Tq, int64_t Tk, int64_t B, int64_t Hq, int64_t D) {
+    const int64_t groups = agq_packed_tiles(Tq, B) * Hq, slots = D == 128 ? 512 : 768;
+    const int64_t steps = B > 0 ? (Tk / B + 31) / 32 : 0;                // of a sequence, on average
+    AgqPackedSplit s = {1, 1 << 20};
+    if (groups < 1 || groups * 3 > slots || steps < 32) return s;
+    int64_t splits = slots / groups;
+    if (splits > steps / 16) splits = steps / 16;
+    if (splits < 2) return s;
+    s.split_steps = (int)((steps + splits - 1) / splits);
+    // sequences longer than the average get more workgroups, up to twice as many
+    s.splits = (int)(2 * splits);
+    return s;
+}
+int agq_launch_attn_packed(const AgqAttnPacked &p, const AgqPackedSplit &sp, void *workspace, void *stream);
 int agq_launch_attn_kv(const AgqAttnKv &p, const AgqKvSplit &sp, void *workspace, void *stream);

@@ -68,9 +68,15 @@ int agq_kv_append(const agq_kv_cache *cache, const void *k, int64_t ldk, const v
     return hip_status(agq_launch_kv_append(a, stream));
 }
 
+size_t agq_attn_packed_workspace_bytes(int64_t Tq, int64_t Hq, int64_t Tk, int64_t Hkv, int64_t D, int64_t B) {
+    if (!heads_ok(Hq, Hkv, D) || !count_ok(Tq, kMaxTokens) || !count_ok(Tk, kMaxTokens) || !count_ok(B, (int64_t)1 << 20)) return 0;
+    const AgqPackedSplit s = agq_packed_split(Tq, Tk, B, Hq, D);
+    return s.splits == 1 ? 0 : (size_t)s.splits * (size_t)Tq * (size_t)Hq * (size_t)(D * 4 + 8);
+}
+
 int agq_attn_packed(const void *q, int64_t ldq, int64_t Tq, int64_t Hq, const void *k, int64_t ldk, const void *v, int64_t ldv, int64_t Tk,
                     int64_t Hkv, int64_t D, const int32_t *cu_q, const int32_t *cu_k, int64_t B, int causal, float scale, void *o,
-                    int64_t ldo, void *stream) {
+                    int64_t ldo, void *workspace, size_t workspace_bytes, void *stream) {
     if (!heads_ok(Hq, Hkv, D) || !count_ok(Tq, kMaxTokens) || !count_ok(Tk, kMaxTokens) || !count_ok(B, (int64_t)1 << 20) || !scale_ok(scale))
         return AGQ_EINVAL;
     if ((Tq / 64 + B) * Hq > kMaxIndex) return AGQ_EINVAL;               // workgroups
@@ -79,7 +85,12 @@ int agq_attn_packed(const void *q, int64_t ldq, int64_t Tq, int64_t Hq, const vo
     if (!ints_ok(cu_q) || !ints_ok(cu_k) || !tensor_ok(q, ldq, Hq, D) || !tensor_ok(o, ldo, Hq, D)) return AGQ_EINVAL;
     if (Tk > 0 && (!tensor_ok(k, ldk, Hkv, D) || !tensor_ok(v, ldv, Hkv, D))) return AGQ_EINVAL;
     const AgqAttnPacked a = {q, k, v, o, ldq, ldk, ldv, ldo, Tq, Tk, Hq, Hkv, D, B, cu_q, cu_k, causal != 0, scale};
-    return hip_status(agq_launch_attn_packed(a, stream));
+    const size_t need = agq_attn_packed_workspace_bytes(Tq, Hq, Tk, Hkv, D, B);
+    if (need > 0) {
+        if (!aligned(workspace, 16)) return AGQ_EINVAL;
+        if (workspace_bytes < need) return AGQ_ESIZE;
+    }
+    return hip_status(agq_launch_attn_packed(a, agq_packed_split(Tq, Tk, B, Hq, D), workspace, stream));
 }
 
 size_t agq_attn_kv_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t B, int64_t max_q, int64_t max_kv) {

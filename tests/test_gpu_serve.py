@@ -348,6 +348,26 @@ def test_packed_padding_strides_and_values_that_nobody_sees(agq, D):
     check_packed(agq, q, k, v, cu, cu, parts=(xd[:, :Hq], xd[:, Hq:Hq + Hkv], xd[:, Hq + Hkv:]), finite=False)
 
 
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 2, 1), (64, 4, 4)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,m", [([100], [3000]), ([1, 130, 0, 7], [2500, 4000, 9, 100]), ([1500], [1400])])
+def test_packed_shared_keys(agq, D, Hq, Hkv, causal, n, m):
+    """few queries, many keys: workgroups share the keys of a tile; sequences longer and shorter than the average, rows
+    that see nothing, an infinity and a NaN that nobody sees; a workspace full of NaN"""
+    r = rng_of(19, D, sum(n))
+    q, k, v = random_qkv(r, sum(n), sum(m), Hq, Hkv, D)
+    need = agq.attn_packed_workspace_bytes(sum(n), Hq, sum(m), Hkv, D, len(n))
+    assert need > 0
+    got = check_packed(agq, q, k, v, ramp(n), ramp(m), causal)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    again = agq.attn_packed(dev(q), dev(k), dev(v), i32(ramp(n)), i32(ramp(m)), causal=causal, workspace=ws)
+    assert np.array_equal(host(again).astype(np.float64), got)
+    if causal and n[0] > 1 and m[0] > n[0]:
+        v[m[0] - 1] = np.nan
+        v[m[0] - 2, 0, 3] = np.inf
+        check_packed(agq, q, k, v, ramp(n), ramp(m), causal, finite=False)
+
+
 def test_packed_scale_and_large_scores(agq):
     """one key that takes all; scores in the thousands; thousands of faint keys under a loud one"""
     r = rng_of(17)

@@ -59,7 +59,8 @@ def test_append_refuses(agq):
 
 
 def test_packed_refuses(agq):
-    ok = dict(q=P, ldq=512, Tq=5, Hq=4, k=P, ldk=256, v=P, ldv=256, Tk=7, Hkv=2, D=128, cu_q=P, cu_k=P, B=2, causal=1, scale=0.1, o=P, ldo=512, stream=None)
+    ok = dict(q=P, ldq=512, Tq=5, Hq=4, k=P, ldk=256, v=P, ldv=256, Tk=7, Hkv=2, D=128, cu_q=P, cu_k=P, B=2, causal=1, scale=0.1, o=P, ldo=512, ws=None, wsb=0,
+              stream=None)
     call = lambda **kw: agq.lib().agq_attn_packed(*dict(ok, **kw).values())
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(q=P + 8), dict(k=P + 8), dict(v=P + 2), dict(o=P + 4), dict(ldq=511),
                dict(ldq=504), dict(ldk=128), dict(ldv=260), dict(ldo=500), dict(Tq=-1), dict(Tk=-1), dict(Tq=1 << 31), dict(Hq=3), dict(Hq=0), dict(Hkv=0),
@@ -67,6 +68,12 @@ def test_packed_refuses(agq):
                dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(Tq=1 << 30, Hq=1024, Hkv=1024)):
         assert call(**kw) == EINVAL, kw
     assert call(Tq=0) == 0 and call(B=0) == 0
+    assert call(ldk=(1 << 24) + 8) == EINVAL and call(ldv=(1 << 24) + 8) == EINVAL
+    # few queries and many keys share the keys between workgroups, which takes a workspace
+    need = agq.attn_packed_workspace_bytes(5, 4, 9000, 2, 128, 1)
+    assert need > 0 and need % (5 * 4 * (128 * 4 + 8)) == 0
+    assert call(B=1, Tk=9000) == EINVAL and call(B=1, Tk=9000, ws=P + 4, wsb=need) == EINVAL
+    assert call(B=1, Tk=9000, ws=P, wsb=need - 1) == ESIZE
 
 
 def test_cache_attention_refuses(agq):
@@ -89,6 +96,9 @@ def test_cache_attention_refuses(agq):
 
 
 def test_workspace_sizes(agq):
+    g = agq.attn_packed_workspace_bytes
+    assert g(8192, 32, 8192, 8, 128, 1) == 0 and g(100, 32, 100, 8, 128, 1) == 0 and g(0, 32, 0, 8, 64, 0) == 0
+    assert g(-1, 32, 9000, 8, 128, 1) == 0 and g(5, 3, 9000, 2, 128, 1) == 0 and g(5, 4, 9000, 2, 80, 1) == 0
     f = agq.attn_kv_workspace_bytes
     assert f(64, 32, 8, 128, 64, 1, 256) == 0                     # short: nothing is shared
     assert f(4096, 32, 8, 128, 4096, 1, 131072) == 0              # many requests: nothing to gain
