@@ -587,7 +587,8 @@ int agq_attn_packed(const void *q_f16, int64_t ldq, int64_t Tq, int64_t Hq, cons
  * workspace); larger lengths are computed all the same.  Lengths beyond max_pages * page are cut to it, and tokens of a
  * page number outside the cache are left out.
  * q, o: fp16 [T, Hq, D].  workspace: agq_attn_kv_workspace_bytes (may be 0; NULL then): partial results where the keys
- * of a request are shared by several workgroups; contents are scratch.  Hq / Hkv <= 1024; B <= 65535.
+ * of a request are shared by several workgroups; contents are scratch.  Hq / Hkv <= 1024; B <= 65535;
+ * max_pages * page, max_q and max_kv at most 2^30.
  * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32; a probability (times its page's
  * scale) is rounded to fp16 for the product with v: by 2^-11 of it at most, down to 2^-29 of the row's largest.         */
 size_t agq_attn_kv_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t B, int64_t max_q, int64_t max_kv);

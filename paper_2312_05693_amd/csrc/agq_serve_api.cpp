@@ -94,7 +94,7 @@ int agq_attn_packed(const void *q, int64_t ldq, int64_t Tq, int64_t Hq, const vo
 }
 
 size_t agq_attn_kv_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t B, int64_t max_q, int64_t max_kv) {
-    if (!heads_ok(Hq, Hkv, D) || !count_ok(T, kMaxTokens) || !count_ok(B, 65535) || !count_ok(max_q, kMaxTokens) || !count_ok(max_kv, kMaxIndex))
+    if (!heads_ok(Hq, Hkv, D) || !count_ok(T, kMaxTokens) || !count_ok(B, 65535) || !count_ok(max_q, kMaxTokens) || !count_ok(max_kv, kMaxTokens))
         return 0;
     const AgqKvSplit s = agq_kv_split(B, Hq, Hkv, max_q, max_kv);
     return s.splits == 1 ? 0 : (size_t)s.splits * (size_t)T * (size_t)Hq * (size_t)(D * 4 + 8);
@@ -104,9 +104,9 @@ int agq_attn_kv(const agq_kv_cache *cache, const void *q, int64_t ldq, int64_t T
                 int64_t B, const int32_t *block_table, int64_t max_pages, int64_t max_q, int64_t max_kv, float scale, void *o, int64_t ldo,
                 void *workspace, size_t workspace_bytes, void *stream) {
     if (!cache_ok(cache) || !heads_ok(Hq, cache->Hkv, cache->D) || Hq / cache->Hkv > 1024) return AGQ_EINVAL;
-    if (!count_ok(T, kMaxTokens) || !count_ok(B, 65535) || !count_ok(max_q, kMaxTokens) || !count_ok(max_kv, kMaxIndex) || !scale_ok(scale))
+    if (!count_ok(T, kMaxTokens) || !count_ok(B, 65535) || !count_ok(max_q, kMaxTokens) || !count_ok(max_kv, kMaxTokens) || !scale_ok(scale))
         return AGQ_EINVAL;
-    if (max_pages < 1 || max_pages > kMaxIndex / cache->page) return AGQ_EINVAL;
+    if (max_pages < 1 || max_pages > kMaxTokens / cache->page) return AGQ_EINVAL;   // keys are counted in 31 bits, with a chunk or two to spare
     const AgqKvSplit s = agq_kv_split(B, Hq, cache->Hkv, max_q, max_kv);
     if (B * cache->Hkv * s.row_tiles > kMaxIndex / s.splits) return AGQ_EINVAL;      // workgroups
     if (T == 0 || B == 0) return AGQ_OK;

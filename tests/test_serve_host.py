@@ -84,8 +84,8 @@ def test_cache_attention_refuses(agq):
         assert call(cache=c) == EINVAL
     for kw in (dict(q=None), dict(o=None), dict(q=P + 8), dict(o=P + 2), dict(ldq=504), dict(ldo=520 - 16), dict(ldq=516), dict(T=-1), dict(T=1 << 31),
                dict(Hq=3), dict(Hq=0), dict(Hq=4096, ldq=4096 * 128, ldo=4096 * 128), dict(cu_q=None), dict(kv_len=None), dict(table=None),
-               dict(table=P + 2), dict(B=-1), dict(B=65536), dict(max_pages=0), dict(max_pages=1 << 27), dict(max_q=-1), dict(max_kv=-1),
-               dict(max_kv=1 << 31), dict(scale=0.0), dict(scale=float("nan"))):
+               dict(table=P + 2), dict(B=-1), dict(B=65536), dict(max_pages=0), dict(max_pages=(1 << 26) + 1), dict(max_q=-1), dict(max_kv=-1),
+               dict(max_kv=(1 << 30) + 1), dict(max_q=(1 << 30) + 1), dict(scale=0.0), dict(scale=float("nan"))):
         assert call(**kw) == EINVAL, kw
     assert call(T=0) == 0 and call(B=0) == 0
     # few requests with long caches share a request's keys between workgroups, which takes a workspace
