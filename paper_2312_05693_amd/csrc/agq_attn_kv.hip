@@ -70,6 +70,30 @@ __device__ __forceinline__ Request request_of(const KvArgs &a, int b) {
     return {q0, q1 - q0, (int)min((int64_t)max(a.kv_len[b], 0), cap)};
 }
 
+// The idx-th piece of all requests' keys, requests one after the other; b = -1: there are fewer.  So the workgroups that find
+// none are the last ones: spread over the others they would hold up places on the CUs (64 requests of 16 to 4096 tokens, at most
+// eight pieces of 512 keys each: 29 us).
+struct Unit {
+    int b, split;
+};
+__device__ __forceinline__ Unit unit_of(const KvArgs &a, int idx) {
+    const int lane = threadIdx.x & 63;
+    const int64_t cap = a.max_pages << a.page_log2;
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int b = b0 + lane;
+        const int n = b < a.B ? splits_of((int)min((int64_t)max(a.kv_len[b], 0), cap), a.split_keys, a.splits) : 0;
+        const int up = before + agq_wave_scan(n);
+        const unsigned long long over = __ballot(up > idx);
+        if (over) {
+            const int src = __ffsll((long long)over) - 1;
+            return {b0 + src, idx - __builtin_amdgcn_readlane(up - n, src)};
+        }
+        before = __builtin_amdgcn_readlane(up, 63);
+    }
+    return {-1, 0};
+}
+
 // One workgroup of NW wavefronts (four or eight): NQ tiles of sixteen rows of one key head of one request, over one split of its keys;
 // the wavefronts take the chunks of 64 keys in turn.
 template <int D, int NQ, int NW>
@@ -79,8 +103,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
     __shared__ float2 ml[NW * ROWS];                                      // maxima and sums
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int head = blockIdx.x, b = blockIdx.y, split = a.row_tiles == 1 ? blockIdx.z : blockIdx.z / a.row_tiles;
-    const int tile0 = blockIdx.z - split * a.row_tiles;
+    const int head = blockIdx.x, tile0 = blockIdx.z;
+    int b = blockIdx.y, split = 0;
+    if (a.splits > 1) {
+        const Unit u = unit_of(a, blockIdx.y);
+        if (u.b < 0) return;
+        b = u.b, split = u.split;
+    }
     // The request's numbers and the first chunks' page numbers are requested together.  Pages: of the keys that the lane loads
     // ((i / 4) * 16 + 4 t + i % 4 for tile t), and of those it owns; what the table says behind the last key does not
     // matter: the mask keeps it out.
@@ -91,7 +120,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
     int first[4] = {page_of(c0 * 64 + (i >> 2) * 16), page_of(c0 * 64 + g * 16), page_of((c0 + NW) * 64 + (i >> 2) * 16), page_of((c0 + NW) * 64 + g * 16)};
     const Request rq = request_of(a, b);
     const int ns = splits_of(rq.L, a.split_keys, a.splits), rows = rq.n * a.group;
-    if (split >= ns) return;
 
     const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
     for (int tile = tile0; tile * ROWS < rows; tile += a.row_tiles) {
@@ -363,7 +391,7 @@ __global__ __launch_bounds__(256) void attn_kv_join_kernel(const KvArgs a) {
 
 template <int D, int NQ, int NW>
 int launch(const KvArgs &a, hipStream_t st) {
-    attn_kv_kernel<D, NQ, NW><<<dim3((unsigned)a.Hkv, (unsigned)a.B, (unsigned)(a.row_tiles * a.splits)), NW * 64, 0, st>>>(a);
+    attn_kv_kernel<D, NQ, NW><<<dim3((unsigned)a.Hkv, (unsigned)(a.B * a.splits), (unsigned)a.row_tiles), NW * 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 

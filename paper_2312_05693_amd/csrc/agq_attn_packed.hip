@@ -53,12 +53,7 @@ __device__ __forceinline__ Tile tile_of(const PackedArgs &a, int idx, int rows) 
             n = max(min(max(a.cu_q[b + 1], 0), a.Tq) - q0, 0);
         }
         const int tiles = (n + rows - 1) / rows;
-        int up = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int u = __shfl_up(up, d);
-            up += lane >= d ? u : 0;
-        }
+        const int up = agq_wave_scan(tiles);
         const unsigned long long over = __ballot(before + up > idx);
         if (over) {
             const int src = __ffsll((long long)over) - 1;

@@ -146,3 +146,14 @@ __device__ __forceinline__ void lds_dma16_s(uint32_t voff, const void *sbase, ui
                  : "v"(voff), "s"(sbase), "s"(lds_addr), "n"(L), "n"(G)
                  : "memory", "m0", "scc");
 }
+
+// sums over the lanes of a wavefront up to each one
+__device__ __forceinline__ int agq_wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr 1, 2, 4, 8: inside sixteen lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast 15: the sixteen before
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);      // row_bcast 31: the thirty-two before
+    return v;
+}

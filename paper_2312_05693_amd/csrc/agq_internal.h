@@ -405,11 +405,12 @@ struct AgqAttnKv {
 // with more than one a second launch that joins them.  groups = workgroups without a split.  Measured in a replayed graph (32
 // query heads on 8 key heads, D = 128, B requests x tokens):
 //   one workgroup of eight wavefronts per CU or less, and few keys: no split, as its launch costs more than it saves (8 x 500 7.5 us;
-//     1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against 17.6, 32 x 2000 24.3 against 28.2
+//     1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against 17.6, 32 x 2000 24.3
+//     against 28.2; not for longer ones, whose lengths differ more (32 x 16..4096 27.4 against 15.7, 32 x 4000 42.8 against 45)
 //   a request's keys on eight workgroups or more: eight wavefronts each, 1024 keys at least (1 x 30000 19.0 us against 21.2 with four and
 //     512; 4 x 131072 192.6 against 202)
-//   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 27.5 us against 32.7
-//     with eight, 128 x 16..4096 46.6 against 56.3)
+//   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 26.7 us against 32.7
+//     with eight, 128 x 16..4096 43.0 against 56.3; with half as many pieces 47.3)
 struct AgqKvSplit {
     int tiles, row_tiles, splits, split_keys, waves;
 };
@@ -420,11 +421,11 @@ static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_
     const int64_t row_tiles = (rows + 16 * s.tiles - 1) / (16 * s.tiles);
     s.row_tiles = (int)(row_tiles < 1 ? 1 : row_tiles > 1024 ? 1024 : row_tiles);
     const int64_t groups = B * Hkv * s.row_tiles;
-    if (s.tiles == 1 && groups <= 256 && max_kv <= (groups > 128 ? 4096 : 1024)) {
+    if (s.tiles == 1 && groups <= 256 && max_kv <= (groups > 128 ? 2048 : 1024)) {
         s.waves = 8, s.splits = 1, s.split_keys = 1 << 30;
         return s;
     }
-    auto split = [&](int64_t least, int64_t fill) {          // about `fill` workgroups: 2048 of them at most for one request
+    auto split = [&](int64_t least, int64_t fill) {          // about `fill` workgroups
         int64_t keys = max_kv / 64 * groups / (fill / 64);
         keys = (keys + 255) / 256 * 256;
         s.split_keys = (int)(keys < least ? least : keys > 1 << 30 ? 1 << 30 : keys);
@@ -433,10 +434,11 @@ static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_
     };
     s.waves = 8;
     split(1024, 512);
-    if (s.tiles == 2 || s.splits < 8) {
+    if (s.tiles == 2 || B * s.splits > 65535 || s.splits < 8) {
         s.waves = 4;
-        split(512, 2048);
+        split(512, 4096);
     }
+    if (B * s.splits > 65535) s.splits = 1, s.split_keys = 1 << 30;       // a grid's limit
     return s;
 }
 int agq_launch_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int page, int32_t *block_table, int64_t max_pages,

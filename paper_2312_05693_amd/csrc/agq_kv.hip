@@ -42,15 +42,6 @@ __device__ __forceinline__ MapRow map_row(int past, int add, int page_log2, int6
     return r;
 }
 
-__device__ __forceinline__ int wave_scan(int v) {               // inclusive
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr 1, 2, 4, 8: inside sixteen lanes
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast 15: the sixteen before
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);      // row_bcast 31: the thirty-two before
-    return v;
-}
 // the largest i in [0, n) with at[i] <= x (at[0] <= x)
 __device__ __forceinline__ int find_row(const int *at, int n, int x) {
     int lo = 0, hi = n;
@@ -73,7 +64,7 @@ __global__ __launch_bounds__(kMapThreads) void kv_map_kernel(const MapArgs a) {
     struct Mine {
         int64_t tok, need, back;
     };
-    auto scan64 = [&](int64_t v) { return ((int64_t)wave_scan((int)(v >> 16)) << 16) + wave_scan((int)(v & 0xFFFF)); };
+    auto scan64 = [&](int64_t v) { return ((int64_t)agq_wave_scan((int)(v >> 16)) << 16) + agq_wave_scan((int)(v & 0xFFFF)); };
     auto batch = [&](const MapRow &r, bool bad) {
         const Mine up = {scan64(r.tokens), scan64(r.need), scan64(r.back)};
         const int any_bad = __any(bad);
