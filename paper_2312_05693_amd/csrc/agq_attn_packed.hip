@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         }
     }
     const int past = tl.m - tl.n;                                  // query r sees keys up to past + r
-    const int seen = a.causal ? min(past + row + 1, tl.m) : tl.m;
+    int seen = a.causal ? min(past + row + 1, tl.m) : tl.m;
     const int last_row = min(tl.n - tl.row, kRows) - 1;            // of the workgroup's rows
     const int all_keys = a.causal ? min(past + tl.row + last_row + 1, tl.m) : tl.m;                                 // that some row sees
     const int wave_last = min(last_row, wave * 32 + 31);
@@ -160,7 +160,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     const int wave_all = a.causal ? min(past + tl.row + wave * 32 + 1, tl.m) : tl.m;                                // every row of it
     const int there = (max(all_keys, 0) + 31) >> 5;
     const int steps = (int)blockIdx.y == ns - 1 ? there : min(there, a.split_steps);
-    const int mine = min((max(wave_keys, 0) + 31) >> 5, steps), whole = max(wave_all, 0) >> 5;
+    const int mine = min((max(wave_keys, 0) + 31) >> 5, steps), whole = min(max(wave_all, 0) >> 5, mine);
+    seen = min(seen, steps * 32);                                  // what follows is another workgroup's
 
     // copies: lane l of a wavefront's copy j brings the piece that belongs at place l of 1 KiB.  Sixteen lanes read LDS at a time,
     // 256 bytes: a row's pieces are permuted by the row so that the sixteen rows (keys) or the four rows of 64 bytes (values) of a
@@ -244,12 +245,17 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
 
     auto slot = [](int u) { return (uint32_t)(u & 3) * SUB; };
 
-    // every step that has something at the mask, at the beginning or at the end
+    // the steps that multiply with values under the mask, and what is left at the end
     auto scores = [&](int u, float16_t &s) {
         const uint32_t at = k_lane + slot(u);
         s = float16_t{};
 #pragma unroll
         for (int st = 0; st < KS; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_k(at, st), q[st], s, 0, 0, 0);
+    };
+    auto mask = [&](int u, float16_t &s) {
+        const int left = seen - u * 32 - 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
     };
     auto step_plain = [&](int u) __attribute__((always_inline)) {                                 // scores in s0, probabilities of the sub-tile before in p1
         if (u + 1 < mine) scores(u + 1, s1);
@@ -290,11 +296,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
             }
         }
         if (u < mine) {
-            if (u >= whole) {
-                const int left = seen - u * 32 - 4 * h;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s0[r] = 8 * (r >> 2) + (r & 3) < left ? s0[r] : -INFINITY;
-            }
+            if (u >= whole) mask(u, s0);
             const float top = top_of(s0), over = fmaf(top, c, -off);
             if (__any(over > kSlack + kUpLog2)) {
                 const float to = over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off, f = __builtin_amdgcn_exp2f(off - to);
@@ -309,7 +311,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         s0 = s1;
     };
 
-    // the others: sub-tiles u and u - 1 seen whole, u + 1 there.  The first fragments of a step are read at the end of the one
+    // the others: sub-tile u - 1 seen whole.  (In the first step nothing is multiplied, with values of sub-tile 0, which are
+    // seen whole too; scores of a sub-tile behind the last one are made and not used.)  The first fragments of a step are read at the end of the one
     // before it (in `fr`) unless the wavefronts meet in between.
     constexpr int AHEAD = 3;
     struct Fragments {
@@ -318,12 +321,12 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     auto first_reads = [&](int u, Fragments &fr) {
         unroll<AHEAD>([&](auto n) {
             fr.k[n.value] = read_k(k_lane + slot(u + 1), n.value);
-            fr.v[n.value] = read_v(v_lane + slot(u - 1), n.value % DT, n.value / DT);
+            fr.v[n.value] = read_v(v_lane + slot(max(u - 1, 0)), n.value % DT, n.value / DT);
         });
     };
-    auto step_full = [&](int u, float16_t &s, float16_t &s_next, half8_t (&p)[2], const half8_t (&p_before)[2], Fragments &fr, auto more_tag) {
-        constexpr bool MORE = decltype(more_tag)::value;           // the next step follows at once
-        const uint32_t at_k = k_lane + slot(u + 1), at_v = v_lane + slot(u - 1), next_k = k_lane + slot(u + 2), next_v = v_lane + slot(u);
+    auto step_full = [&](int u, float16_t &s, float16_t &s_next, half8_t (&p)[2], const half8_t (&p_before)[2], Fragments &fr, auto more_tag, auto mask_tag) {
+        constexpr bool MORE = decltype(more_tag)::value, MASK = decltype(mask_tag)::value;     // the next step follows at once; sub-tile u is cut
+        const uint32_t at_k = k_lane + slot(u + 1), at_v = v_lane + slot(max(u - 1, 0)), next_k = k_lane + slot(u + 2), next_v = v_lane + slot(u);
         float f = 1.0f, over = 0.0f, top = 0.0f;
         bool raise = false;
         unroll<2 * KS>([&](auto n) {
@@ -339,7 +342,10 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
                 else if constexpr (MORE) fr.v[R] = read_v(next_v, (R - KS) % DT, (R - KS) / DT);
             }
             // the vector ALU's share: the maximum, the reference, then two scores at a time
-            if constexpr (n.value == 0) top = top_of(s);
+            if constexpr (n.value == 0) {
+                if constexpr (MASK) mask(u, s);
+                top = top_of(s);
+            }
             if constexpr (n.value == 1) {
                 over = fmaf(top, c, -off);
                 raise = __any(over > kSlack + kUpLog2);
@@ -369,7 +375,6 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         copy_v();
         meet<2 * COPIES + COPIES>();
         if (mine > 0) scores(0, s0);
-        const int full = min(whole, mine - 1);                     // steps 1 .. full - 1 are full ones
         // Between two pairs of steps: keys' sub-tiles u + 1, u + 2 and values' u - 1, u have landed, and nobody reads the slots
         // any more that the next ones (keys' up to u + 4, values' up to u + 2) get.
         auto turn = [&]() __attribute__((always_inline)) {
@@ -380,20 +385,22 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
             copy_v();
         };
         int u = 0;
+        auto pair = [&](auto mask_tag) __attribute__((always_inline)) {
+            turn();
+            Fragments fr;
+            first_reads(u, fr);
+            step_full(u, s0, s1, p0, p1, fr, std::true_type{}, std::false_type{});
+            step_full(u + 1, s1, s0, p1, p0, fr, std::false_type{}, mask_tag);
+        };
+        for (; u + 1 < whole; u += 2) pair(std::false_type{});
+        if (u + 1 == whole) {
+            pair(std::true_type{});
+            u += 2;
+        }
+        for (; u <= steps; u += 2) {
+            turn();
 #pragma unroll 1
-        for (int part = 0; part < 2; ++part) {                     // the first pair plain, then the full ones, then the rest
-            for (const int end = part == 0 ? 1 : steps + 1; u < end; u += 2) {
-                turn();
-#pragma unroll 1
-                for (int e = 0; e < 2; ++e) step_plain(u + e);
-            }
-            for (; u + 1 < full; u += 2) {
-                turn();
-                Fragments fr;
-                first_reads(u, fr);
-                step_full(u, s0, s1, p0, p1, fr, std::true_type{});
-                step_full(u + 1, s1, s0, p1, p0, fr, std::false_type{});
-            }
+            for (int e = 0; e < 2; ++e) step_plain(u + e);
         }
         __builtin_amdgcn_s_waitcnt(0x70);                          // the last copies have landed before the LDS is given back
     }

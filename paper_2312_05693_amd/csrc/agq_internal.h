@@ -406,7 +406,7 @@ struct AgqAttnKv {
 // query heads on 8 key heads, D = 128, B requests x tokens):
 //   one workgroup of eight wavefronts per CU or less, and few keys: no split, as its launch costs more than it saves (8 x 500 7.5 us;
 //     1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against 17.6, 32 x 2000 24.3
-//     against 28.2; not for longer ones, whose lengths differ more (32 x 16..4096 27.4 against 15.7, 32 x 4000 42.8 against 45)
+//     against 28.2; not for longer ones, whose lengths differ more (32 x 16..4096 27.4 against 15.7, 32 x 4000 42.8 against 46.9)
 //   a request's keys on eight workgroups or more: eight wavefronts each, 1024 keys at least (1 x 30000 19.0 us against 21.2 with four and
 //     512; 4 x 131072 192.6 against 202)
 //   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 26.7 us against 32.7
