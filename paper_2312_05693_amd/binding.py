@@ -607,6 +607,22 @@ def _kv_cache(k_cache, v_cache, k_exp, v_exp):
     return _pack_cache(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), n_pages, Hkv, D, page), Hkv, D
 
 
+_device_of = torch.Tensor.get_device
+
+
+def _stream_of(*tensors):
+    """the current stream, if all of the tensors are on its device (an address of another one would be a GPU fault)"""
+    dev, *others = {*map(_device_of, tensors)}
+    if others or dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("tensors on the current GPU are wanted")
+    return _stream() if _raw_stream is None else _raw_stream(dev)
+
+
+def _given(workspace, q):
+    if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the same GPU is wanted")
+
+
 class KvStep(NamedTuple):
     """What kv_map says about a step (device int32 tensors): the lengths after it [B], the offsets of the requests' new
     tokens [B+1], position and slot of every token [T], the ring's state [2], and the status [1]."""
@@ -623,6 +639,7 @@ def kv_map(kv_len, n_new, block_table, page, free_ring, free_state, T, out: KvSt
     out: a KvStep to write into (not the one whose kv_len and free_state are passed in: a loop swaps two)."""
     B, max_pages = block_table.shape
     n_pages = free_ring.numel()
+    st = _stream_of(kv_len, n_new, block_table, free_ring, free_state, *(out or ()))
     if out is None:                                # one allocation, cut into the six
         buf = kv_len.new_empty(2 * B + 2 * T + 4)
         out = KvStep._make(buf.split_with_sizes([B, B + 1, T, T, 2, 1]))
@@ -631,7 +648,7 @@ def kv_map(kv_len, n_new, block_table, page, free_ring, free_state, T, out: KvSt
     else:
         to = [_ints(t, n, "out." + name) for t, n, name in zip(out, (B, B + 1, T, T, 2, 1), KvStep._fields)]
     _ok(lib().agq_kv_map(_ints(kv_len, B, "kv_len"), _ints(n_new, B, "n_new"), B, page, _ints(block_table, B * max_pages, "block_table"),
-                         max_pages, _ints(free_ring, n_pages, "free_ring"), n_pages, _ints(free_state, 2, "free_state"), T, *to, _stream()),
+                         max_pages, _ints(free_ring, n_pages, "free_ring"), n_pages, _ints(free_state, 2, "free_state"), T, *to, st),
         "agq_kv_map")
     return out
 
@@ -642,6 +659,7 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
     T = slot.numel()
     shape = T, Hkv, D
+    used = [k, v, slot, k_cache, v_cache, k_exp, v_exp]
     ldk, ldv = _like(k, shape, "k"), _like(v, shape, "v")
     P = Hq = ldq = ldqo = ldko = 0
     pos_p = cos_p = sin_p = q_p = qo_p = ko_p = None
@@ -651,25 +669,29 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
                 or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
             raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
         pos_p, cos_p, sin_p = _ints(pos, T, "pos"), rope_cos.data_ptr(), rope_sin.data_ptr()
+        used += pos, rope_cos, rope_sin
         if k_out is None:
             k_out, ldko = k.new_empty(T, Hkv, D), Hkv * D
         else:
             ldko = _like(k_out, shape, "k_out")
+            used.append(k_out)
         ko_p = k_out.data_ptr()
         if q is not None:
             Hq = q.shape[1]
             ldq = _like(q, (T, Hq, D), "q")
+            used.append(q)
             if q_out is None:
                 q_out, ldqo = q.new_empty(T, Hq, D), Hq * D
             else:
                 ldqo = _like(q_out, (T, Hq, D), "q_out")
+                used.append(q_out)
             q_p, qo_p = q.data_ptr(), q_out.data_ptr()
     elif q is not None or k_out is not None or pos is not None:
         raise ValueError("q, k_out and pos go with rope tables")
     if q is None and q_out is not None:
         raise ValueError("q_out goes with q")
     _ok(lib().agq_kv_append(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, _ints(slot, T, "slot"), q_p, ldq, Hq, pos_p, cos_p, sin_p, P, qo_p,
-                            ldqo, ko_p, ldko, _stream()), "agq_kv_append")
+                            ldqo, ko_p, ldko, _stream_of(*used)), "agq_kv_append")
     return q_out, k_out
 
 
@@ -690,12 +712,15 @@ def attn_packed(q, k, v, cu_q, cu_k, causal=True, scale=None, o=None, workspace=
         o, ldo = q.new_empty(Tq, Hq, D), Hq * D
     else:
         ldo = _like(o, (Tq, Hq, D), "o")
+    st = _stream_of(q, k, v, cu_q, cu_k, o)
     if workspace is None:
         need = lib().agq_attn_packed_workspace_bytes(Tq, Hq, Tk, Hkv, D, n - 1)
         workspace = cu_q.new_empty(need >> 2) if need else None
+    else:
+        _given(workspace, q)
     _ok(lib().agq_attn_packed(q.data_ptr(), ldq, Tq, Hq, k.data_ptr(), ldk, v.data_ptr(), ldv, Tk, Hkv, D, _ints(cu_q, n, "cu_q"),
                               _ints(cu_k, n, "cu_k"), n - 1, 1 if causal else 0, D ** -0.5 if scale is None else scale, o.data_ptr(), ldo,
-                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream()),
+                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, st),
         "agq_attn_packed")
     return o
 
@@ -716,11 +741,14 @@ def attn_kv(q, cu_q, kv_len, block_table, k_cache, v_cache, k_exp, v_exp, max_q,
         o, ldo = q.new_empty(T, Hq, D), Hq * D
     else:
         ldo = _like(o, (T, Hq, D), "o")
+    st = _stream_of(q, cu_q, kv_len, block_table, k_cache, v_cache, k_exp, v_exp, o)
     if workspace is None:
         need = lib().agq_attn_kv_workspace_bytes(T, Hq, Hkv, D, B, max_q, max_kv)
         workspace = k_cache.new_empty(need) if need else None
+    else:
+        _given(workspace, q)
     _ok(lib().agq_attn_kv(cache, q.data_ptr(), ldq, T, Hq, _ints(cu_q, B + 1, "cu_q"), _ints(kv_len, B, "kv_len"), B,
                           _ints(block_table, B * max_pages, "block_table"), max_pages, max_q, max_kv, D ** -0.5 if scale is None else scale,
                           o.data_ptr(), ldo, None if workspace is None else workspace.data_ptr(),
-                          0 if workspace is None else workspace.nbytes, _stream()), "agq_attn_kv")
+                          0 if workspace is None else workspace.nbytes, st), "agq_attn_kv")
     return o

@@ -415,7 +415,7 @@ int agq_launch_attn_kv(const AgqAttnKv &p, const AgqKvSplit &sp, void *workspace
     else
         err = sp.tiles == 2 ? launch<64, 2, 4>(a, st) : sp.waves == 8 ? launch<64, 1, 8>(a, st) : launch<64, 1, 4>(a, st);
     if (err || a.splits == 1) return err;
-    const int64_t rows = p.max_q * p.Hq;
+    const int64_t rows = (p.max_q > 0 ? p.max_q : 1) * p.Hq;
     const dim3 grid((unsigned)(rows < 4 * 1024 ? (rows + 3) / 4 : 1024), (unsigned)p.B);
     if (p.D == 128)
         attn_kv_join_kernel<128><<<grid, 256, 0, st>>>(a);

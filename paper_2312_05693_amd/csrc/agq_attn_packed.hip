@@ -221,8 +221,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
     };
 
     float c = a.scale, off = kNone, l = 0.0f;
-    if constexpr (D == 64) asm("" : "+v"(c));                      // a scalar operand takes the ALU half as long again, which bounds this one (1 %)
-                                            // products with a scalar operand take the ALU half as long again
+    if constexpr (D == 64) asm("" : "+v"(c));                      // a scalar operand takes the ALU half as long again (1 % of D = 64)
     float16_t o[DT], s0 = {}, s1 = {};
     half8_t p0[2] = {}, p1[2] = {};
 #pragma unroll
@@ -314,9 +313,9 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         s0 = s1;
     };
 
-    // the others: sub-tile u - 1 seen whole.  (In the first step nothing is multiplied, with values of sub-tile 0, which are
-    // seen whole too; scores of a sub-tile behind the last one are made and not used.)  The first fragments of a step are read at the end of the one
-    // before it (in `fr`) unless the wavefronts meet in between.
+    // the others: sub-tile u - 1 seen whole.  (In the first step the weights are 0 and the values those of sub-tile 0; its rise
+    // of the reference clears the sums.  Scores of a sub-tile behind the last one are made and not used.)  The first fragments
+    // of a step are read at the end of the one before it (in `fr`) unless the wavefronts meet in between.
     constexpr int AHEAD = 3;
     struct Fragments {
         half8_t k[KS + AHEAD], v[KS + AHEAD];                      // KS == 2 DT: as many products with values
@@ -364,9 +363,11 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-        if (raise) {
+        if (raise) {                                               // what the first step made of infinities is 0 as well (f = 0)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= f;
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] = f == 0.0f ? 0.0f : o[d][e] * f;
         }
         if constexpr (MORE) unroll<AHEAD>([&](auto n) { fr.k[n.value] = fr.k[KS + n.value], fr.v[n.value] = fr.v[KS + n.value]; });
     };
@@ -481,7 +482,9 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(const PackedArgs 
         acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) {
-            const float f = s + e < ns ? __builtin_amdgcn_exp2f(ml[e].x - to) : 0.0f;
+            const bool again = s + e >= ns;                        // the last one's, which may be infinite: not times 0
+            const float f = again ? 0.0f : __builtin_amdgcn_exp2f(ml[e].x - to);
+            if (again) x[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f), ml[e].y = 0.0f;
             sum = fmaf(ml[e].y, f, sum);
             acc.x = fmaf(x[e].x, f, acc.x), acc.y = fmaf(x[e].y, f, acc.y), acc.z = fmaf(x[e].z, f, acc.z), acc.w = fmaf(x[e].w, f, acc.w);
         }

@@ -368,6 +368,39 @@ def test_packed_shared_keys(agq, D, Hq, Hkv, causal, n, m):
         check_packed(agq, q, k, v, ramp(n), ramp(m), causal, finite=False)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,m", [(40, 40), (200, 200), (300, 333), (20, 3000)])
+def test_packed_infinities_that_are_seen(agq, D, causal, n, m):
+    """an infinity among the values gives infinities of its sign in its column, a NaN or two opposite ones NaN"""
+    r = rng_of(20, D, n)
+    q, k, v = random_qkv(r, n, m, 2, 1, D)
+    v[0, 0, 3], v[7, 0, 5], v[33, 0, 9], v[35, 0, 9], v[m - 1, 0, 11], v[1, 0, 20] = np.inf, -np.inf, np.inf, -np.inf, np.inf, np.nan
+    check_packed(agq, q, k, v, ramp([n]), ramp([m]), causal, finite=False)
+    o = host(agq.attn_packed(dev(q), dev(k), dev(v), i32(ramp([n])), i32(ramp([m])), causal=causal)).astype(np.float64)
+    for i in range(n):
+        keys = m - n + i + 1 if causal else m
+        assert (o[i, :, 3] == np.inf).all() and (keys <= 7 or (o[i, :, 5] == -np.inf).all())
+        assert keys <= 33 or (np.isnan(o[i, :, 9]).all() if keys > 35 else (o[i, :, 9] == np.inf).all())
+        assert keys < m or (o[i, :, 11] == np.inf).all()
+
+
+@pytest.mark.parametrize("D,tokens,Hq,Hkv", [(128, 1100, 40, 40), (64, 1400, 24, 8), (128, 2300, 33, 11)])
+def test_packed_one_prompt_of_many_workgroups(agq, D, tokens, Hq, Hkv):
+    """more workgroups than CUs, which are taken in another order then: every row of every head against the same head alone"""
+    r = rng_of(25, D, tokens)
+    q, k, v = (dev(x) for x in random_qkv(r, tokens, tokens, Hq, Hkv, D))
+    cu = i32([0, tokens])
+    o = torch.full((tokens, Hq, D), 7.0, dtype=torch.float16, device="cuda")
+    agq.attn_packed(q, k, v, cu, cu, o=o)
+    for h in range(Hq):
+        kv = h // (Hq // Hkv)
+        alone = agq.attn_packed(q[:, h:h + 1], k[:, kv:kv + 1], v[:, kv:kv + 1], cu, cu,
+                                workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))
+        assert ((o[:, h:h + 1].double() - alone.double()).abs() <= 2.0 ** -9 * alone.double().abs() + 2.0 ** -8).all(), h
+    check_packed(agq, *(host(x[:, :1]) for x in (q, k, v)), ramp([tokens]), ramp([tokens]))
+
+
 def test_packed_scale_and_large_scores(agq):
     """one key that takes all; scores in the thousands; thousands of faint keys under a loud one"""
     r = rng_of(17)
@@ -449,6 +482,14 @@ def test_cache_several_tokens(agq, n, lens, max_q):
     r = rng_of(21, sum(n))
     table, n_pages = make_pages(r, lens, 16)
     check_cache(agq, random_q(r, sum(n), 6, 64), ramp(n), lens, table, random_cache(r, n_pages, 2, 16, 64), max_q=max_q)
+
+
+def test_cache_shared_keys_no_new_tokens_expected(agq):
+    """max_q = 0 with tokens all the same"""
+    r, lens = rng_of(24), [3000, 500]
+    table, n_pages = make_pages(r, lens, 32)
+    assert agq.attn_kv_workspace_bytes(2, 4, 2, 64, 2, 0, 60000) > 0
+    check_cache(agq, random_q(r, 2, 4, 64), ramp([1, 1]), lens, table, random_cache(r, n_pages, 2, 32, 64), max_q=0, max_kv=60000)
 
 
 @pytest.mark.parametrize("lens,max_kv", [([9000], None), ([5000, 3, 0, 1700], None), ([2600, 4100], 1500), ([600], 60000)])

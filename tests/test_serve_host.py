@@ -153,6 +153,22 @@ def test_binding_refuses_other_tensors(agq):
         agq.kv_map(i(3), i(3), i(3, 2), 16, i(6), i(2), 4, out=step)              # of another number of tokens
 
 
+def test_binding_refuses_tensors_that_are_not_on_the_gpu(agq):
+    """calls that are right but for their device"""
+    h, i, c = tensors()
+    kv = (c(6, 2, 16, 64), c(6, 2, 64, 16), c(6, 2), c(6, 2))
+    cos = torch.zeros(8, 32)
+    for call in (lambda: agq.kv_map(i(3), i(3), i(3, 2), 16, i(6), i(2), 3),
+                 lambda: agq.kv_map(i(3), i(3), i(3, 2), 16, i(6), i(2), 3, out=agq.KvStep(i(3), i(4), i(3), i(3), i(2), i(1))),
+                 lambda: agq.kv_append(h(3, 2, 64), h(3, 2, 64), i(3), *kv),
+                 lambda: agq.kv_append(h(3, 2, 64), h(3, 2, 64), i(3), *kv, q=h(3, 4, 64), pos=i(3), rope_cos=cos, rope_sin=cos),
+                 lambda: agq.attn_packed(h(3, 4, 64), h(3, 2, 64), h(3, 2, 64), i(2), i(2)),
+                 lambda: agq.attn_kv(h(3, 4, 64), i(4), i(3), i(3, 2), *kv, 1, 32),
+                 lambda: agq.attn_kv(h(3, 4, 64).to("meta"), i(4), i(3), i(3, 2), *kv, 1, 32)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
+
+
 def test_oracle_attention_against_torch():
     """the yardstick of the GPU tests against torch's own float64 operators"""
     from oracle import agq_serve_oracle as so
