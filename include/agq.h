@@ -1,5 +1,6 @@
 /* agq - the W4A8 / W4A4 quantized linear layer of Agile-Quant (arxiv 2312.05693)
- * and its log2-quantized softmax x V path, as HIP kernels for gfx950 (MI355X).
+ * and its log2-quantized softmax x V path, with the paged 8-bit key/value cache
+ * and the attentions that serving needs, as HIP kernels for gfx950 (MI355X).
  *
  * C ABI.  Conventions that hold for every call unless a comment says otherwise:
  *   - every tensor pointer is a DEVICE pointer owned by the caller; the library

@@ -1,11 +1,18 @@
 // Attention over whole prompts, packed one behind the other, causal or not, with grouped heads.
 //
 // One pass over the keys with the running maximum and sum of the softmax.  A workgroup of four wavefronts takes 128 queries
-// of one head, a wavefront 32 of them; the keys and values pass through LDS, 64 at a time.  Scores transposed: S^T = K Q^T
+// of one head, a wavefront 32 of them; keys and values pass through LDS in sub-tiles of 32.  Scores transposed: S^T = K Q^T
 // on 32 x 32 x 16 matrix instructions leaves a lane with one query's scores of sixteen keys out of 32, and O^T = V^T P^T
 // takes the probabilities from those very registers, if the keys of its operand V^T are dealt out in the same order; that
 // operand comes out of LDS by transposing reads.  Sums, maxima and accumulators are fp32; probabilities go into the second
-// product as fp16 times 2^10 (off by 2^-11 of it at most, down to 2^-24 of the largest).
+// product as fp16 times 2^10 (off by 2^-11 of it at most, down to 2^-24 of the largest), because the matrix instruction takes
+// both operands in 16 bits.
+//
+// Bound and figures.  Long prompts: the issue of instructions.  A step of 32 keys has 2 D / 16 matrix instructions of 32
+// cycles and about as many cycles of vector arithmetic in between; 16000 tokens in seven prompts of up to 8191, 32 heads on
+// 8, D = 128, 790 us, 943 TFLOP/s (a library product of two matrices of that size class reaches 1264), matrix cores busy 38 %
+// of the time; D = 64, with half the products for the same exponentials, 454 us, 820.  One prompt of 2048 in 40 heads, 59 us:
+// the chain of its longest tiles, 64 steps.  A handful of short prompts 7.6 us, of which an empty launch is 1.6.
 #include "agq_device.h"
 #include "agq_internal.h"
 
