@@ -14,9 +14,9 @@
 //
 // Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 166 us,
 // 5.0 TB/s (a plain read reaches 6.05).  Many requests of all lengths up to 4096, 64 of them, 100 MB, 26.7 us with the join:
-// a chunk's bytes take 2.7 us to come and are requested one chunk ahead; two ahead do not fit the registers.  One request of
-// 1000 tokens, 10.4 us: two chunks one after the other, the launch and the join of the wavefronts; sixteen wavefronts, a
-// chunk each, do not fit the registers (23 us).
+// a chunk's bytes take 2.7 us to come.  One request of 1000 tokens, 10.4 us: what 32 CUs can have on its way, the launch and
+// the join of the wavefronts.  Bytes requested two chunks ahead change nothing where the registers hold them (D = 64) and
+// spill otherwise (13.9 us); so do sixteen wavefronts to a workgroup (23 us) and three workgroups to a CU (64 requests, 30.8).
 #include "agq_device.h"
 #include "agq_internal.h"
 
@@ -188,7 +188,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
         auto load_v = [&](int c) {
             const int8_t *src = a.vc + ((((int64_t)(inside(pv1) ? pv1 : 0) * a.Hkv + head) * D + i) << a.page_log2) + ((c * 64 + g * 16) & page1);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) vraw[d] = *reinterpret_cast<const uint4 *>(src + (d * 16 << a.page_log2));
+            for (int d = 0; d < DT; ++d) {
+                vraw[d] = *reinterpret_cast<const uint4 *>(src);
+                src += 16 << a.page_log2;
+                // two tiles of rows: one address instead of eight, for the registers (eleven in memory otherwise; 64 requests of
+                // 8 new tokens, lengths 16 to 4096, 41.1 -> 39.9 us; one tile of rows, which has them, is 5 % slower for it)
+                if constexpr (NQ == 2) asm volatile("" : "+v"(src));
+            }
         };
         auto chunk = [&](int c, auto more_tag) {
             constexpr bool more = decltype(more_tag)::value;
