@@ -628,6 +628,25 @@ def test_step_without_pages_does_nothing(agq):
     assert all(torch.equal(a, b) for a, b in zip(before, s.cache + [s.table, s.ring]))
 
 
+def test_workspaces_refused(agq):
+    """too small, strided, on the host"""
+    q, k, cu = torch.zeros(5, 2, 64, dtype=torch.float16, device="cuda"), torch.zeros(4000, 2, 64, dtype=torch.float16, device="cuda"), i32([0, 4000])
+    need = agq.attn_packed_workspace_bytes(5, 2, 4000, 2, 64, 1)
+    cache = [torch.zeros(s, dtype=torch.int8, device="cuda") for s in ((4, 2, 64, 64), (4, 2, 64, 64), (4, 2), (4, 2))]
+    need_kv = agq.attn_kv_workspace_bytes(5, 2, 2, 64, 1, 5, 60000)
+    assert need > 0 and need_kv > 0
+    packed = lambda ws: agq.attn_packed(q, k, k, i32([0, 5]), cu, workspace=ws)
+    kv = lambda ws: agq.attn_kv(q, i32([0, 5]), i32([200]), i32([[0, 1, 2, 3]]), *cache, 5, 60000, workspace=ws)
+    for call, n in ((packed, need), (kv, need_kv)):
+        with pytest.raises(agq.AgqError):
+            call(torch.empty(n - 16, dtype=torch.uint8, device="cuda"))
+        with pytest.raises(ValueError):
+            call(torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2])
+        with pytest.raises(ValueError):
+            call(torch.empty(n, dtype=torch.uint8))
+        assert (call(torch.empty(n, dtype=torch.uint8, device="cuda")) == 0).all()
+
+
 def test_generation_captured_and_replayed(agq):
     """two steps (the lengths and the ring's state go there and back) in one graph on another stream, replayed with the
     program's own work in between, against the same steps called one by one"""
