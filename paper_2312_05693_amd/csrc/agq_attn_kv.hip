@@ -41,7 +41,8 @@ struct KvArgs {
     float2 *part_ml;      // [split][token][query head]: maximum, sum
     int64_t ldq, ldo, max_pages;
     float scale;          // log2(e) times the softmax's factor
-    int T, B, Hq, Hkv, group, page_log2, n_pages, splits, split_keys, row_tiles;
+    float per_piece;      // 1 / pieces
+    int T, B, Hq, Hkv, group, page_log2, n_pages, splits, split_keys, row_tiles, pieces;
 };
 
 // Eight codes of K as fp16: code + 128 is the low byte of a half, a subnormal, 2^-24 times itself; three instructions for
@@ -77,19 +78,37 @@ __device__ __forceinline__ Request request_of(const KvArgs &a, int b) {
     return {q0, q1 - q0, (int)min((int64_t)max(a.kv_len[b], 0), cap)};
 }
 
+// Keys of a piece.  pieces != 0: the least number, not below split_keys, with which the requests (64 at most) make no more than
+// that many pieces, one for every CU; lengths are known here only.  (4 requests of 60000 to 131072 tokens: with the keys that
+// 131072 each would need, a quarter of the CUs has none.)
+__device__ __forceinline__ int piece_keys(const KvArgs &a) {
+    if (a.pieces == 0) return a.split_keys;
+    const int lane = threadIdx.x & 63;
+    const int64_t cap = a.max_pages << a.page_log2;
+    const int L = lane < a.B ? (int)min((int64_t)max(a.kv_len[lane], 0), cap) : 0;
+    const int64_t total = ((int64_t)__builtin_amdgcn_readlane(agq_wave_scan(L >> 8), 63) << 8) + __builtin_amdgcn_readlane(agq_wave_scan(L & 255), 63);
+    int keys = max(a.split_keys, (int)((float)total * a.per_piece));
+    for (;;) {
+        keys = (keys + 255) & ~255;
+        const int n = lane < a.B ? splits_of(L, keys, a.splits) : 0;
+        if (__builtin_amdgcn_readlane(agq_wave_scan(n), 63) <= a.pieces) return keys;
+        keys += keys >> 4;                                                // B <= pieces / 4: ends with a piece for each at the latest
+    }
+}
+
 // The idx-th piece of all requests' keys, requests one after the other; b = -1: there are fewer.  So the workgroups that find
 // none are the last ones: spread over the others they would hold up places on the CUs (64 requests of 16 to 4096 tokens, at most
 // eight pieces of 512 keys each: 29 us).
 struct Unit {
     int b, split;
 };
-__device__ __forceinline__ Unit unit_of(const KvArgs &a, int idx) {
+__device__ __forceinline__ Unit unit_of(const KvArgs &a, int idx, int split_keys) {
     const int lane = threadIdx.x & 63;
     const int64_t cap = a.max_pages << a.page_log2;
     int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const int b = b0 + lane;
-        const int n = b < a.B ? splits_of((int)min((int64_t)max(a.kv_len[b], 0), cap), a.split_keys, a.splits) : 0;
+        const int n = b < a.B ? splits_of((int)min((int64_t)max(a.kv_len[b], 0), cap), split_keys, a.splits) : 0;
         const int up = before + agq_wave_scan(n);
         const unsigned long long over = __ballot(up > idx);
         if (over) {
@@ -112,8 +131,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int head = blockIdx.x, tile0 = blockIdx.z;
     int b = blockIdx.y, split = 0;
+    const int split_keys = piece_keys(a);
     if (a.splits > 1) {
-        const Unit u = unit_of(a, blockIdx.y);
+        const Unit u = unit_of(a, blockIdx.y, split_keys);
         if (u.b < 0) return;
         b = u.b, split = u.split;
     }
@@ -121,12 +141,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
     // ((i / 4) * 16 + 4 t + i % 4 for tile t), and of those it owns; what the table says behind the last key does not
     // matter: the mask keeps it out.
     const int32_t *table = a.table + (int64_t)b * a.max_pages;
-    const int page1 = (1 << a.page_log2) - 1, k0 = split * a.split_keys, c0 = (k0 >> 6) + wave;
+    const int page1 = (1 << a.page_log2) - 1, k0 = split * split_keys, c0 = (k0 >> 6) + wave;
     auto page_of = [&](int key) { return table[min(key >> a.page_log2, (int)a.max_pages - 1)]; };
     auto inside = [&](int p) { return (unsigned)p < (unsigned)a.n_pages; };
     int first[4] = {page_of(c0 * 64 + (i >> 2) * 16), page_of(c0 * 64 + g * 16), page_of((c0 + NW) * 64 + (i >> 2) * 16), page_of((c0 + NW) * 64 + g * 16)};
     const Request rq = request_of(a, b);
-    const int ns = splits_of(rq.L, a.split_keys, a.splits), rows = rq.n * a.group;
+    const int ns = splits_of(rq.L, split_keys, a.splits), rows = rq.n * a.group;
 
     const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
     for (int tile = tile0; tile * ROWS < rows; tile += a.row_tiles) {
@@ -160,7 +180,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
         }
         const int t_first = tile * ROWS / a.group, t_last = min(tile * ROWS + ROWS, rows) - 1;
         const int all_see = rq.L - rq.n + t_first + 1;                    // keys that every row of the tile sees
-        const int k1 = min(split == ns - 1 ? rq.L : k0 + a.split_keys, rq.L - rq.n + t_last / a.group + 1);
+        const int k1 = min(split == ns - 1 ? rq.L : k0 + split_keys, rq.L - rq.n + t_last / a.group + 1);
 
         float M[NQ], l[NQ];                                               // maximum, sum of w 2^-e_v
         float4_t o[NQ][DT];
@@ -354,7 +374,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
 template <int D>
 __global__ __launch_bounds__(256) void attn_kv_join_kernel(const KvArgs a) {
     const Request rq = request_of(a, blockIdx.y);
-    const int ns = splits_of(rq.L, a.split_keys, a.splits), lane = threadIdx.x & 63;
+    const int ns = splits_of(rq.L, piece_keys(a), a.splits), lane = threadIdx.x & 63;
     if (ns == 1) return;
     constexpr int W = D / 64, AHEAD = 8;
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rq.n * a.Hq; r += gridDim.x * 4) {
@@ -404,7 +424,7 @@ __global__ __launch_bounds__(256) void attn_kv_join_kernel(const KvArgs a) {
 
 template <int D, int NQ, int NW>
 int launch(const KvArgs &a, hipStream_t st) {
-    attn_kv_kernel<D, NQ, NW><<<dim3((unsigned)a.Hkv, (unsigned)(a.B * a.splits), (unsigned)a.row_tiles), NW * 64, 0, st>>>(a);
+    attn_kv_kernel<D, NQ, NW><<<dim3((unsigned)a.Hkv, (unsigned)(a.pieces ? a.pieces : a.B * a.splits), (unsigned)a.row_tiles), NW * 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -418,7 +438,7 @@ int agq_launch_attn_kv(const AgqAttnKv &p, const AgqKvSplit &sp, void *workspace
     a.scale = p.scale * 1.44269504088896340736f;
     a.T = (int)p.T, a.B = (int)p.B, a.Hq = (int)p.Hq, a.Hkv = (int)p.Hkv, a.group = (int)(p.Hq / p.Hkv);
     a.page_log2 = __builtin_ctz((unsigned)p.page), a.n_pages = (int)p.n_pages;
-    a.splits = sp.splits, a.split_keys = sp.split_keys, a.row_tiles = sp.row_tiles;
+    a.splits = sp.splits, a.split_keys = sp.split_keys, a.row_tiles = sp.row_tiles, a.pieces = sp.pieces, a.per_piece = sp.pieces ? 1.0f / (float)sp.pieces : 0.0f;
     a.part = (float *)workspace;
     a.part_ml = (float2 *)(a.part + (size_t)a.splits * p.T * p.Hq * p.D);
     hipStream_t st = (hipStream_t)stream;

@@ -401,22 +401,26 @@ struct AgqAttnKv {
     float scale;
 };
 // How attention over the cache is dealt out: 16 * tiles rows (new tokens x query heads of a key head) and `waves` wavefronts
-// per workgroup, row_tiles workgroups over the rows, splits over the keys with split_keys keys each (a multiple of 64), and
-// with more than one a second launch that joins them.  groups = workgroups without a split.  Measured in a replayed graph (32
-// query heads on 8 key heads, D = 128, B requests x tokens):
-//   one workgroup of eight wavefronts per CU or less, and few keys: no split, as its launch costs more than it saves (8 x 500 7.5 us;
-//     1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against 17.6, 32 x 2000 24.3
-//     against 28.2; not for longer ones, whose lengths differ more (32 x 16..4096 27.4 against 15.7, 32 x 4000 42.8 against 46.9)
-//   a request's keys on eight workgroups or more: eight wavefronts each, 1024 keys at least (1 x 30000 19.0 us against 21.2 with four and
-//     512; 4 x 131072 192.6 against 202)
-//   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 26.7 us against 32.7
-//     with eight, 128 x 16..4096 43.0 against 56.3; with half as many pieces 47.3)
+// per workgroup, row_tiles workgroups over the rows, up to `splits` splits of a request's keys with split_keys keys each (a
+// multiple of 64), and with more than one a second launch that joins them; pieces != 0: that many splits in all for a key
+// head, of a size that the device chooses from the lengths, split_keys at least.  groups = workgroups without a split.
+// Measured in a replayed graph (32 query heads on 8 key heads, D = 128, B requests x tokens):
+//   one workgroup of eight wavefronts per CU or less, and few keys: no split, as its launch costs more than it saves (8 x 500
+//     7.5 us; 1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against
+//     17.6, 32 x 2000 24.3 against 28.2; not for longer ones, whose lengths differ more (32 x 16..4096 27.4 against 15.7,
+//     32 x 4000 42.8 against 46.9)
+//   a request's keys on eight workgroups or more: eight wavefronts each, one workgroup per CU in all, 1024 keys at least
+//     (4 x 60000..131072, 4 new tokens, 155 us; with 8192 keys each, as 131072 would need, 179; two workgroups per CU 162;
+//     2 x 30000..65536 40, 46 and 45; 4 x 131072 193, 196 and 196; 1 x 30000 19.4, 18.8 and 20.2, and 21.2 with four
+//     wavefronts and 512 keys; 40 x 8000 of 8 heads on one 21.2 against 26.8)
+//   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 26.7 us
+//     against 32.7 with eight, 128 x 16..4096 43.0 against 56.3; with half as many pieces 47.3)
 struct AgqKvSplit {
-    int tiles, row_tiles, splits, split_keys, waves;
+    int tiles, row_tiles, splits, split_keys, waves, pieces;
 };
 static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv) {
     const int64_t rows = max_q * (Hq / Hkv);
-    AgqKvSplit s;
+    AgqKvSplit s = {};
     s.tiles = rows <= 16 ? 1 : 2;
     const int64_t row_tiles = (rows + 16 * s.tiles - 1) / (16 * s.tiles);
     s.row_tiles = (int)(row_tiles < 1 ? 1 : row_tiles > 1024 ? 1024 : row_tiles);
@@ -437,6 +441,11 @@ static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_
     if (s.tiles == 2 || B * s.splits > 65535 || s.splits < 8) {
         s.waves = 4;
         split(512, 4096);
+    } else {                                                  // groups <= 64, so pieces >= 4 B
+        s.pieces = (int)(256 / (groups / B));
+        const int64_t most = B > 4 ? 4 * s.pieces / B : s.pieces, keys = ((max_kv + most - 1) / most + 255) / 256 * 256;
+        s.split_keys = (int)(keys < 1024 ? 1024 : keys);
+        s.splits = (int)((max_kv + s.split_keys - 1) / s.split_keys);
     }
     if (B * s.splits > 65535) s.splits = 1, s.split_keys = 1 << 30;       // a grid's limit
     return s;

@@ -484,6 +484,17 @@ def test_cache_several_tokens(agq, n, lens, max_q):
     check_cache(agq, random_q(r, sum(n), 6, 64), ramp(n), lens, table, random_cache(r, n_pages, 2, 16, 64), max_q=max_q)
 
 
+@pytest.mark.parametrize("lens,max_kv", [([20000, 3, 0, 9000], 20000), ([16383, 16384, 16385], 20000), ([30000, 70], 8200), ([9000], 200000),
+                                         ([0, 0, 8000, 1, 0, 5000, 257, 256], 8192)])
+@pytest.mark.parametrize("D,Hq,Hkv,page", [(128, 4, 1, 64), (64, 6, 2, 16)])
+def test_cache_pieces_by_the_lengths(agq, lens, max_kv, D, Hq, Hkv, page):
+    """few requests with long caches: the device chooses the pieces; empty requests, one long one, longer than max_kv"""
+    r, B = rng_of(26, sum(lens), D), len(lens)
+    table, n_pages = make_pages(r, lens, page)
+    assert agq.attn_kv_workspace_bytes(B, Hq, Hkv, D, B, 1, max_kv) > 0
+    check_cache(agq, random_q(r, B, Hq, D), ramp([1] * B), lens, table, random_cache(r, n_pages, Hkv, page, D), max_kv=max_kv)
+
+
 def test_cache_shared_keys_no_new_tokens_expected(agq):
     """max_q = 0 with tokens all the same"""
     r, lens = rng_of(24), [3000, 500]
