@@ -92,7 +92,7 @@ __device__ __forceinline__ int piece_keys(const KvArgs &a) {
         keys = (keys + 255) & ~255;
         const int n = lane < a.B ? splits_of(L, keys, a.splits) : 0;
         if (__builtin_amdgcn_readlane(agq_wave_scan(n), 63) <= a.pieces) return keys;
-        keys += keys >> 4;                                                // B <= pieces / 4: ends with a piece for each at the latest
+        keys += keys >> 4;                                                // B <= pieces / 2: ends with a piece for each at the latest
     }
 }
 
@@ -444,9 +444,9 @@ int agq_launch_attn_kv(const AgqAttnKv &p, const AgqKvSplit &sp, void *workspace
     hipStream_t st = (hipStream_t)stream;
     int err;
     if (p.D == 128)
-        err = sp.tiles == 2 ? launch<128, 2, 4>(a, st) : sp.waves == 8 ? launch<128, 1, 8>(a, st) : launch<128, 1, 4>(a, st);
+        err = sp.tiles == 2 ? sp.waves == 8 ? launch<128, 2, 8>(a, st) : launch<128, 2, 4>(a, st) : sp.waves == 8 ? launch<128, 1, 8>(a, st) : launch<128, 1, 4>(a, st);
     else
-        err = sp.tiles == 2 ? launch<64, 2, 4>(a, st) : sp.waves == 8 ? launch<64, 1, 8>(a, st) : launch<64, 1, 4>(a, st);
+        err = sp.tiles == 2 ? sp.waves == 8 ? launch<64, 2, 8>(a, st) : launch<64, 2, 4>(a, st) : sp.waves == 8 ? launch<64, 1, 8>(a, st) : launch<64, 1, 4>(a, st);
     if (err || a.splits == 1) return err;
     const int64_t rows = (p.max_q > 0 ? p.max_q : 1) * p.Hq;
     const dim3 grid((unsigned)(rows < 4 * 1024 ? (rows + 3) / 4 : 1024), (unsigned)p.B);

@@ -409,11 +409,14 @@ struct AgqAttnKv {
 //     7.5 us; 1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against
 //     17.6, 32 x 2000 24.3 against 28.2; not for longer ones, whose lengths differ more (32 x 16..4096 27.4 against 15.7,
 //     32 x 4000 42.8 against 46.9)
-//   a request's keys on eight workgroups or more: eight wavefronts each, one workgroup per CU in all, 1024 keys at least
-//     (4 x 60000..131072, 4 new tokens, 155 us; with 8192 keys each, as 131072 would need, 179; two workgroups per CU 162;
-//     2 x 30000..65536 40, 46 and 45; 4 x 131072 193, 196 and 196; 1 x 30000 19.4, 18.8 and 20.2, and 21.2 with four
-//     wavefronts and 512 keys; 40 x 8000 of 8 heads on one 21.2 against 26.8)
-//   between: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 26.7 us
+//   640 keys or more to a CU, two splits or more to a request and four if two workgroups were on each: eight wavefronts to a
+//     workgroup, one workgroup per CU in all, 1024 keys at least (4 x 60000..131072, 4 new tokens, 155 us; with 8192 keys each,
+//     as 131072 would need, 179; two workgroups per CU 162; 2 x 30000..65536 40, 46 and 45; 4 x 131072 193, 196 and 196;
+//     against four wavefronts and about 4096 workgroups of 512 keys at least: 1 x 30000 19.4 and 21.2, 2 x 16000..32000 of 40
+//     heads on 40 119.6 and 124.7, 16 x 2000..4096 24.2 and 26.2, 8 x 2000..4096 15.9 and 15.4, 8 new tokens of 4 x
+//     30000..60000 73 and 105, of 16 x 2000..4096 29 and 35, of 1 x 24000 22 and 24; with fewer keys 1 x 8000 14.2 and 10.8,
+//     1 x 16000 15.7 and 13.3, 8 new tokens of 1 x 16000 21 and 17)
+//   else: four wavefronts, so that two workgroups on a CU fill each other's gaps, 512 keys at least (64 x 16..4096 26.7 us
 //     against 32.7 with eight, 128 x 16..4096 43.0 against 56.3; with half as many pieces 47.3)
 struct AgqKvSplit {
     int tiles, row_tiles, splits, split_keys, waves, pieces;
@@ -438,12 +441,13 @@ static inline AgqKvSplit agq_kv_split(int64_t B, int64_t Hq, int64_t Hkv, int64_
     };
     s.waves = 8;
     split(1024, 512);
-    if (s.tiles == 2 || B * s.splits > 65535 || s.splits < 8) {
+    const int64_t pieces = 256 / (Hkv * s.row_tiles);
+    if (max_kv * groups < 256 * 640 || B > 64 || 2 * B > pieces || s.splits < 4) {
         s.waves = 4;
         split(512, 4096);
-    } else {                                                  // groups <= 64, so pieces >= 4 B
-        s.pieces = (int)(256 / (groups / B));
-        const int64_t most = B > 4 ? 4 * s.pieces / B : s.pieces, keys = ((max_kv + most - 1) / most + 255) / 256 * 256;
+    } else {
+        const int64_t most = B > 4 ? 4 * pieces / B : pieces, keys = ((max_kv + most - 1) / most + 255) / 256 * 256;
+        s.pieces = (int)pieces;
         s.split_keys = (int)(keys < 1024 ? 1024 : keys);
         s.splits = (int)((max_kv + s.split_keys - 1) / s.split_keys);
     }

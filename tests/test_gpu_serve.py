@@ -495,6 +495,20 @@ def test_cache_pieces_by_the_lengths(agq, lens, max_kv, D, Hq, Hkv, page):
     check_cache(agq, random_q(r, B, Hq, D), ramp([1] * B), lens, table, random_cache(r, n_pages, Hkv, page, D), max_kv=max_kv)
 
 
+@pytest.mark.parametrize("lens,max_kv", [([20000, 9, 6, 9000], 60000), ([16383, 16384, 16385], 60000), ([90000, 70], 82000), ([9000], 200000),
+                                         ([0, 0, 8000, 1, 0, 5000, 257, 256], 24000), ([1] * 40 + [3000] * 24, 4096)])
+@pytest.mark.parametrize("n,D,Hq,Hkv,page", [(1, 128, 4, 1, 64), (1, 64, 6, 2, 16), (6, 128, 4, 1, 32), (9, 64, 6, 2, 128)])
+def test_cache_one_piece_per_cu(agq, lens, max_kv, n, D, Hq, Hkv, page):
+    """few requests with long caches, one or two tiles of rows: the device chooses the pieces; requests that are empty, that hold fewer
+    tokens than are new, or more than max_kv"""
+    r, B = rng_of(27, sum(lens), D, n), len(lens)
+    table, n_pages = make_pages(r, lens, page)
+    need = agq.attn_kv_workspace_bytes(n * B, Hq, Hkv, D, B, n, max_kv)
+    assert need > 0
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")                                                     # NaN
+    check_cache(agq, random_q(r, n * B, Hq, D), ramp([n] * B), lens, table, random_cache(r, n_pages, Hkv, page, D), max_kv=max_kv, workspace=ws)
+
+
 def test_cache_shared_keys_no_new_tokens_expected(agq):
     """max_q = 0 with tokens all the same"""
     r, lens = rng_of(24), [3000, 500]

@@ -103,6 +103,7 @@ def test_workspace_sizes(agq):
     assert f(64, 32, 8, 128, 64, 1, 256) == 0                     # short: nothing is shared
     assert f(4096, 32, 8, 128, 4096, 1, 131072) == 0              # many requests: nothing to gain
     assert f(1, 32, 8, 128, 1, 1, 131072) > 0
+    assert f(0, 32, 8, 128, 0, 1, 131072) == 0 and f(0, 32, 8, 128, 0, 0, 0) == 0
     for bad in ((-1, 32, 8, 128, 1, 1, 9), (1, 32, 5, 128, 1, 1, 9), (1, 32, 8, 96, 1, 1, 9), (1, 32, 8, 128, 70000, 1, 9), (1, 32, 8, 128, 1, -1, 9),
                 (1, 32, 8, 128, 1, 1, -9)):
         assert f(*bad) == 0
