@@ -12,8 +12,8 @@
 // instruction takes both operands in 16 bits: down to 2^-29 of the largest weight it has all eleven bits (off by 2^-11 of it
 // at most, and as often up as down); sums, maxima and accumulators are fp32.
 //
-// Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 166 us,
-// 5.0 TB/s (a plain read reaches 6.05).  Many requests of all lengths up to 4096, 64 of them, 100 MB, 26.7 us with the join:
+// Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 143 us,
+// 5.8 TB/s (a plain read reaches 6.05), and 5 for the join.  Many requests of all lengths up to 4096, 64 of them, 100 MB, 26.7 us with the join:
 // a chunk's bytes take 2.7 us to come.  One request of 1000 tokens, 10.4 us: what 32 CUs can have on its way, the launch and
 // the join of the wavefronts.  Bytes requested two chunks ahead change nothing where the registers hold them (D = 64) and
 // spill otherwise (13.9 us); so do sixteen wavefronts to a workgroup (23 us) and three workgroups to a CU (64 requests, 30.8).

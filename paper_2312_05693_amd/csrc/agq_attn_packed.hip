@@ -10,7 +10,7 @@
 //
 // Bound and figures.  Long prompts: the issue of instructions.  A step of 32 keys has 2 D / 16 matrix instructions of 32
 // cycles and about as many cycles of vector arithmetic in between; 16000 tokens in seven prompts of up to 8191, 32 heads on
-// 8, D = 128, 790 us, 943 TFLOP/s (a library product of two matrices of that size class reaches 1264), matrix cores busy 38 %
+// 8, D = 128, 785 us, 950 TFLOP/s (a library product of two matrices of that size class reaches 1264), matrix cores busy 38 %
 // of the time; D = 64, with half the products for the same exponentials, 454 us, 820.  One prompt of 2048 in 40 heads, 59 us:
 // the chain of its longest tiles, 64 steps.  A handful of short prompts 7.6 us, of which an empty launch is 1.6.
 #include "agq_device.h"
