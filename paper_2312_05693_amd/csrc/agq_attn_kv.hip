@@ -13,10 +13,11 @@
 // at most, and as often up as down); sums, maxima and accumulators are fp32.
 //
 // Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 143 us,
-// 5.8 TB/s (a plain read reaches 6.05), and 5 for the join.  Many requests of all lengths up to 4096, 64 of them, 100 MB, 26.7 us with the join:
-// a chunk's bytes take 2.7 us to come.  One request of 1000 tokens, 10.4 us: what 32 CUs can have on its way, the launch and
-// the join of the wavefronts.  Bytes requested two chunks ahead change nothing where the registers hold them (D = 64) and
-// spill otherwise (13.9 us); so do sixteen wavefronts to a workgroup (23 us) and three workgroups to a CU (64 requests, 30.8).
+// 5.8 TB/s (a plain read reaches 6.05), and 5 for the join.  Many requests of all lengths up to 4096, 64 of them, 100 MB,
+// 26.7 us with the join: a chunk's bytes take 2.7 us to come.  One request of 1000 tokens, 10.4 us: what 32 CUs can have on
+// its way, the launch and the join of the wavefronts.  Bytes requested two chunks ahead change nothing where the registers
+// hold them (D = 64) and spill otherwise (13.9 us); so do sixteen wavefronts to a workgroup (23 us) and three workgroups to a
+// CU (64 requests, 30.8).
 #include "agq_device.h"
 #include "agq_internal.h"
 
@@ -66,7 +67,7 @@ __device__ __forceinline__ half8_t widen_v(uint32_t w0, uint32_t w1) {
 
 // how many workgroups share the keys of a request of L tokens
 __device__ __forceinline__ int splits_of(int L, int split_keys, int splits) {
-    return min(max((L + split_keys - 1) / split_keys, 1), splits);
+    return min(max((int)(((uint32_t)L + (uint32_t)split_keys - 1) / (uint32_t)split_keys), 1), splits);
 }
 
 struct Request {
