@@ -591,8 +591,9 @@ int agq_attn_packed(const void *q_f16, int64_t ldq, int64_t Tq, int64_t Hq, cons
  * q, o: fp16 [T, Hq, D].  workspace: agq_attn_kv_workspace_bytes (may be 0; NULL then): partial results where the keys
  * of a request are shared by several workgroups; contents are scratch.  Hq / Hkv <= 1024; B <= 65535;
  * max_pages * page, max_q and max_kv at most 2^30.
- * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32; a probability (times its page's
- * scale) is rounded to fp16 for the product with v: by 2^-11 of it at most, down to 2^-29 of the row's largest.         */
+ * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32.  For the product with v, and for it
+ * alone, a probability times its page's scale of v is rounded to fp16: by 2^-11 of it at most, down to 2^-29 of the row's
+ * largest such product, and by 2^-40 of that one below.                                                              */
 size_t agq_attn_kv_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t B, int64_t max_q, int64_t max_kv);
 int agq_attn_kv(const agq_kv_cache *cache, const void *q_f16, int64_t ldq, int64_t T, int64_t Hq, const int32_t *cu_q,
                 const int32_t *kv_len, int64_t B, const int32_t *block_table, int64_t max_pages, int64_t max_q,

@@ -108,9 +108,10 @@ def cache_rows(codes, exps, table, L, h, transposed):
     return (np.concatenate(rows)[:L] if rows else np.zeros((0, D))), np.array(there[:L], dtype=bool)
 
 
-def attention(q, k, v, past, causal=True, scale=None, there=None):
+def attention(q, k, v, past, causal=True, scale=None, there=None, offset=None):
     """q [n, D], k and v [m, D], float64: (o [n, D], bound [n, D]).  Query i sees keys j <= past + i (past = m - n) if causal, and
-    only those that are there.  bound: how far a result with the roundings that include/agq.h allows can be from o:
+    only those that are there.  offset [n]: added to X below, for keys that are multiplied in a form with larger products.
+    bound: how far a result with the roundings that include/agq.h allows can be from o:
       scores: fp32 sums of D exact products, then a multiply-add and a difference; relative to the sum of the products'
               magnitudes X (in units of the exponent of 2) D + 4 roundings of 2^-24, twice (its own and the maximum's), which
               the exponential turns into a relative error of the weight of ln 2 times that; the exponential itself 2^-22
@@ -134,7 +135,7 @@ def attention(q, k, v, past, causal=True, scale=None, there=None):
             w = np.exp(s - s.max())
             total = w.sum()
             o[i] = (w @ vv) / total
-            X = (np.abs(kk) @ np.abs(q[i])).max() * scale * np.log2(np.e)
+            X = ((np.abs(kk) @ np.abs(q[i])).max() + (0.0 if offset is None else offset[i])) * scale * np.log2(np.e)
             A = (w @ np.abs(vv)) / total
             rel = 2 * np.log(2) * (D + 4) * 2.0 ** -24 * X + 2.0 ** -22
             bound[i] = (2.0 ** -11 + 2 * rel + 2 * (len(kk) + 64) * 2.0 ** -24) * A + len(kk) * 2.0 ** -35 * np.abs(vv).max(0) / total \

@@ -8,9 +8,11 @@
 // in a page) are one load, and so is its piece of a key.  Nothing goes through LDS but the join of the wavefronts.
 // A page's scale of K is a factor of the scores.  Its scale of V is added to the exponent: the weight of key j is
 // w = 2^(s_j + e_v - M), M the running maximum of s_j + e_v, so the products of pages with different scales add up in one
-// accumulator, and the softmax's sum is that of w 2^-e_v.  w goes into the product as fp16 times 2^15, because the matrix
-// instruction takes both operands in 16 bits: down to 2^-29 of the largest weight it has all eleven bits (off by 2^-11 of it
-// at most, and as often up as down); sums, maxima and accumulators are fp32.
+// accumulator.  w goes into the product as fp16 times 2^15, because the matrix instruction takes both operands in 16 bits: down
+// to 2^-29 of the largest weight it has all eleven bits (off by 2^-11 of it at most, and as often up as down); sums, maxima
+// and accumulators are fp32.  The softmax's sum is that of w 2^-e_v before w's rounding: on a page of small values w may be
+// nothing in fp16, as it is in the product, while w 2^-e_v is most of the sum (exponents lie 40 powers of two apart at most
+// where agq_kv_append made them, so w is a normal fp32 number for keys down to 2^-100 of the loudest).
 //
 // Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 143 us,
 // 5.8 TB/s (a plain read reaches 6.05), and 5 for the join.  Many requests of all lengths up to 4096, 64 of them, 100 MB,
@@ -276,11 +278,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][k & 3], sk24, off)),
-                                       (_Float16)__builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][(k & 3) + 1], sk24, off))};
-                    sum = __builtin_amdgcn_fdot2(w, ones, sum, false);
-                    p[n][k >> 3][k & 7] = w.x;
-                    p[n][k >> 3][(k & 7) + 1] = w.y;
+                    const float w0 = __builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][k & 3], sk24, off));
+                    const float w1 = __builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][(k & 3) + 1], sk24, off));
+                    sum += w0 + w1;
+                    p[n][k >> 3][k & 7] = (_Float16)w0;
+                    p[n][k >> 3][(k & 7) + 1] = (_Float16)w1;
                 }
                 l[n] = fmaf(sum, inv, l[n]);
             }
@@ -342,7 +344,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) mine[d * 4] = o[n][d];
             __syncthreads();
-            for (int it = threadIdx.x; it < 16 * (D / 4); it += NW * 64) {
+            int it = threadIdx.x;
+            asm volatile("" : "+v"(it));                                  // addresses of the stores: made here, no registers before
+            for (; it < 16 * (D / 4); it += NW * 64) {
                 const int rr = it / (D / 4), d = it % (D / 4) * 4, r = tile * ROWS + n * 16 + rr;
                 if (r >= rows) continue;
                 float top = kNone, sum = 0.0f;

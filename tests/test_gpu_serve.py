@@ -723,3 +723,77 @@ def test_two_streams_at_once(agq):
     torch.cuda.synchronize()
     for _, _, _, want, o in sides:
         assert torch.equal(o, want)
+
+
+# ------------------------------------------------------------------ the softmax's sum and the values' scales
+
+def check_far(agq, q, cu_q, lens, table, cache, max_kv, max_q=1):
+    """as check_cache, the scores' bound with what K's form in the matrix instructions adds: sums 128 steps of its page times |q|_1 in size"""
+    D, page, Hkv = q.shape[2], cache[0].shape[2], cache[0].shape[1]
+    group = q.shape[1] // Hkv
+    got = host(agq.attn_kv(dev(q), i32(cu_q), i32(lens), i32(table), *(dev(c) for c in cache), max_q, max_kv)).astype(np.float64)
+    for b, L in enumerate(lens):
+        step = 2.0 ** cache[2][table[b, :-(-L // page)]].astype(np.float64).max(0)
+        for h in range(Hkv):
+            k, there = so.cache_rows(cache[0], cache[2], table[b], L, h, False)
+            v, _ = so.cache_rows(cache[1], cache[3], table[b], L, h, True)
+            for hh in range(h * group, (h + 1) * group):
+                x = q[cu_q[b]:cu_q[b + 1], hh].astype(np.float64)
+                want, bound = so.attention(x, k, v, L - len(x), True, None, there, offset=128 * step[h] * np.abs(x).sum(-1))
+                off = np.abs(got[cu_q[b]:cu_q[b + 1], hh] - want)
+                assert np.isfinite(want).all() and (off <= bound).all(), (b, hh, off.max(), np.abs(want).max(), (off - bound).max())
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,page,n", [(64, 2, 1, 16, 1), (128, 4, 2, 32, 1), (128, 20, 1, 16, 1), (64, 3, 1, 64, 7)])
+@pytest.mark.parametrize("lens,loud,max_kv", [([32], [1], 32), ([64], [2], 64), ([1024, 70], [0, 1], 1024), ([2048], [9], 2048), ([16384], [0], 1),
+                                              ([16384], [70], 16384), ([30000], [100], 200000)])
+@pytest.mark.parametrize("lower", [-2.0, 0.5, 1.0, 3.0, 10.5])
+def test_cache_sum_counts_keys_whose_values_are_small(agq, D, Hq, Hkv, page, n, lens, loud, max_kv, lower):
+    """pages of zeros, as agq_kv_append writes them (the exponent -30), beside one page of values near fp16's largest (9): the keys
+    of the zeros, `lower` powers of two below the others, add nothing to the product with V and most of the softmax's sum.
+    In one workgroup of four or eight wavefronts, and shared by several."""
+    r, B = rng_of(40, D, Hq, sum(lens), abs(int(10 * lower))), len(lens)
+    table, n_pages = make_pages(r, lens, page)
+    k = r.integers(-9, 10, (n_pages, Hkv, page, D)).astype(np.int8)
+    v = np.zeros((n_pages, Hkv, D, page), np.int8)
+    ke, ve = np.full((n_pages, Hkv), -6, np.int8), np.full((n_pages, Hkv), so.E_ZERO, np.int8)
+    k[..., 0] = 0
+    q = (r.standard_normal((n * B, Hq, D)) * 0.25).astype(np.float16)
+    q[..., 0] = 64.0
+    for b, j in enumerate(loud):
+        p = table[b, min(j * 16, lens[b] - 1) // page]
+        k[p, :, :, 0] = np.rint(lower / (64 * D ** -0.5 * np.log2(np.e)) * 64)
+        v[p] = r.integers(64, 128, v[p].shape) * r.choice([-1, 1], (Hkv, D, 1))
+        ve[p] = 9
+    check_far(agq, q, ramp([n] * B), lens, table, (k, v, ke, ve), max_kv, n)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_cache_scales_far_apart_in_a_chunk(agq, seed):
+    """value scales from end to end of what agq_kv_append makes, the finest and the coarsest of them in every chunk of 64 keys"""
+    r, page, lens = rng_of(41, seed), 16, [200, 64, 700]
+    D = [64, 128][seed % 2]
+    table, n_pages = make_pages(r, lens, page)
+    k, v, ke, ve = random_cache(r, n_pages, 2, page, D)
+    ve[:] = r.integers(-30, 9, ve.shape)
+    for row in table:
+        for j in range(0, (row >= 0).sum(), 4):
+            ve[row[j + int(r.integers(0, min(4, (row >= 0).sum() - j)))]] = -30
+            ve[row[j + int(r.integers(0, min(4, (row >= 0).sum() - j)))]] = 8
+    ke[:] = r.integers(-9, -5, ke.shape)
+    check_far(agq, random_q(r, 3, 6, D), ramp([1, 1, 1]), lens, table, (k, v, ke, ve), 700)
+
+
+def test_cache_sum_from_appended_tokens(agq):
+    """the same as a server meets it: tokens whose values are zero, one whose values are large, all through agq_kv_append"""
+    r, page, T, Hkv, D = rng_of(42), 16, 300, 2, 128
+    x = (r.standard_normal((T, 2 * Hkv, D)) * 0.25).astype(np.float16)
+    x[:, Hkv:] = 0
+    x[130:140, Hkv:] = (r.uniform(20000, 60000, (10, Hkv, D)) * r.choice([-1, 1], (1, Hkv, D))).astype(np.float16)
+    cache = [torch.zeros(s, dtype=torch.int8, device="cuda") for s in ((20, Hkv, page, D), (20, Hkv, D, page), (20, Hkv), (20, Hkv))]
+    slot = np.arange(T, dtype=np.int32)
+    xd = dev(x)
+    agq.kv_append(xd[:, :Hkv], xd[:, Hkv:], i32(slot), *cache)
+    cache = [host(c).copy() for c in cache]
+    assert cache[3].min() == so.E_ZERO and cache[3].max() == 9
+    check_far(agq, random_q(r, 1, 4, D), ramp([1]), [T], np.arange(20, dtype=np.int32)[None], cache, T)
