@@ -320,8 +320,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         s0 = s1;
     };
 
-    // the others: sub-tile u - 1 seen whole.  (In the first step the weights are 0 and the values those of sub-tile 0; its rise
-    // of the reference clears the sums.  Scores of a sub-tile behind the last one are made and not used.)  The first fragments
+    // the others: sub-tile u - 1 seen whole.  (In the first step the weights are 0 and the values those of sub-tile 0; the
+    // sums are cleared behind it.  Scores of a sub-tile behind the last one are made and not used.)  The first fragments
     // of a step are read at the end of the one before it (in `fr`) unless the wavefronts meet in between.
     constexpr int AHEAD = 3;
     struct Fragments {
@@ -370,11 +370,12 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-        if (raise) {                                               // what the first step made of infinities is 0 as well (f = 0)
+        if (MORE && u == 0) {                                      // nothing is summed yet; what the step made of infinities goes
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d) o[d] = float16_t{};
+        } else if (raise) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[d][e] = f == 0.0f ? 0.0f : o[d][e] * f;
+            for (int d = 0; d < DT; ++d) o[d] *= f;                // (an infinity that was seen stays one or becomes NaN, f = 0 or not)
         }
         if constexpr (MORE) unroll<AHEAD>([&](auto n) { fr.k[n.value] = fr.k[KS + n.value], fr.v[n.value] = fr.v[KS + n.value]; });
     };

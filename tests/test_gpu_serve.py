@@ -797,3 +797,20 @@ def test_cache_sum_from_appended_tokens(agq):
     cache = [host(c).copy() for c in cache]
     assert cache[3].min() == so.E_ZERO and cache[3].max() == 9
     check_far(agq, random_q(r, 1, 4, D), ramp([1]), [T], np.arange(20, dtype=np.int32)[None], cache, T)
+
+
+# ------------------------------------------------------------------ infinities beside scores that are far apart
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,m,at", [(32, 96, 40), (40, 200, 33), (40, 200, 130), (200, 200, 60), (200, 230, 199), (130, 300, 299), (20, 3000, 2000)])
+def test_packed_infinity_under_a_louder_key(agq, D, causal, n, m, at):
+    """an infinity and a NaN among the first values, then a key whose score is 180 powers of two above theirs: their weights
+    are small, not nothing"""
+    r = rng_of(43, D, n, m, at)
+    q, k, v = np.full((n, 2, D), 8.0, np.float16), np.zeros((m, 1, D), np.float16), r.standard_normal((m, 1, D)).astype(np.float16)
+    k[at] = 2.0
+    v[0, 0, 3], v[1, 0, 9], v[2, 0, 20], v[at - 1, 0, 31] = np.inf, np.nan, -np.inf, np.inf
+    got = check_packed(agq, q, k, v, ramp([n]), ramp([m]), causal, finite=False)
+    sees = np.arange(n) + (m - n if causal else m) >= at
+    assert sees.any() and not np.isfinite(got[sees][:, :, [3, 9, 20, 31]]).any()
