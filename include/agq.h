@@ -568,8 +568,9 @@ int agq_kv_append(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, con
  *   o[i,h] = sum_j softmax_j( scale * q[i,h] . k[j,h'] ) v[j,h'],   h' = h / (Hq / Hkv)
  * over the keys j of the query's own sequence; causal != 0: query i of n sees keys j <= i + (m - n) of m, so the last
  * query sees the last key (n < m: the queries are the later part of the prompt; n > m: the first queries see nothing).
- * A row that sees no key is 0.  Keys and values that a row does not see do not reach it, infinities and NaN included; an
- * infinity or NaN among the values that it sees makes their column of it infinite or NaN.
+ * A row that sees no key is 0, one that sees keys with scores of -infinity only is NaN.  Keys and values that a row does
+ * not see do not reach it, infinities and NaN included; an infinity or NaN among the values that it sees makes their
+ * column of it infinite or NaN.
  * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D], ldk and ldv at most 2^24; cu_q, cu_k [B+1].  scale > 0, usually
  * 1 / sqrt(D).  workspace: agq_attn_packed_workspace_bytes (0, and NULL, unless there are few queries and many keys):
  * partial results where workgroups share the keys of a tile of queries; contents are scratch.

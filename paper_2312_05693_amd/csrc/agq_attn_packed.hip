@@ -91,6 +91,12 @@ __device__ __forceinline__ int splits_of(const PackedArgs &a, const Tile &t) {
     return a.splits == 1 ? 1 : min(max((steps_of(a, t) + a.split_steps - 1) / a.split_steps, 1), a.splits);
 }
 
+// what a row's sum is divided by: a row without a key is 0; one that sees keys, but none with a score above -infinity, has no
+// softmax and is NaN
+__device__ __forceinline__ float inverse_of(float sum, bool sees) {
+    return sum == 0.0f ? sees ? __builtin_nanf("") : 0.0f : 1.0f / sum;
+}
+
 // four keys of one column of a [key][d] tile in LDS: lanes 4 r + c of a group of sixteen name row r's columns 4 c .. 4 c + 3,
 // lane j receives column j of the four rows
 __device__ __forceinline__ short4_t read_tr(uint32_t at) {
@@ -447,7 +453,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         }
         return;
     }
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    const float f = inverse_of(l, seen > 0);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -497,7 +503,7 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(const PackedArgs 
             acc.x = fmaf(x[e].x, f, acc.x), acc.y = fmaf(x[e].y, f, acc.y), acc.z = fmaf(x[e].z, f, acc.z), acc.w = fmaf(x[e].w, f, acc.w);
         }
     }
-    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float f = inverse_of(sum, tl.m > 0 && (!a.causal || tl.m - tl.n + tl.row + r >= 0));
     const _Float16 y[4] = {(_Float16)(acc.x * f), (_Float16)(acc.y * f), (_Float16)(acc.z * f), (_Float16)(acc.w * f)};
     *reinterpret_cast<uint2 *>(a.o + t * a.ldo + head * D + d) = __builtin_bit_cast(uint2, y);
 }

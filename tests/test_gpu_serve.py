@@ -814,3 +814,17 @@ def test_packed_infinity_under_a_louder_key(agq, D, causal, n, m, at):
     got = check_packed(agq, q, k, v, ramp([n]), ramp([m]), causal, finite=False)
     sees = np.arange(n) + (m - n if causal else m) >= at
     assert sees.any() and not np.isfinite(got[sees][:, :, [3, 9, 20, 31]]).any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,m,quiet", [(1, 1, 1), (5, 40, 40), (40, 40, 33), (140, 300, 300), (70, 200, 64), (6, 3000, 3000), (6, 3000, 1500), (50, 7, 7)])
+def test_packed_scores_of_minus_infinity(agq, D, n, m, quiet):
+    """keys whose scores are -infinity weigh nothing; a row that sees no others has no softmax and is NaN, a row that sees no key at
+    all is 0"""
+    r = rng_of(44, D, n, m)
+    q, k, v = random_qkv(r, n, m, 2, 1, D)
+    q[..., 0] = 1.0
+    k[:quiet, :, 0] = -np.inf
+    got = check_packed(agq, q, k, v, ramp([n]), ramp([m]), finite=False)
+    keys = np.arange(n) + m - n + 1
+    assert np.isnan(got[(keys > 0) & (keys <= quiet)]).all() and (got[keys <= 0] == 0).all() and np.isfinite(got[keys > quiet]).all()
