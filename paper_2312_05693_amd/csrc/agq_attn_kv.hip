@@ -13,6 +13,8 @@
 // and accumulators are fp32.  The softmax's sum is that of w 2^-e_v before w's rounding: on a page of small values w may be
 // nothing in fp16, as it is in the product, while w 2^-e_v is most of the sum (exponents lie 40 powers of two apart at most
 // where agq_kv_append made them, so w is a normal fp32 number for keys down to 2^-100 of the loudest).
+// w's exponent is the score's difference to the lane's largest in the chunk, taken before the scale, and that one's to M: neither is
+// above 0 whatever the rounding, so scores of any size (an fp16 query of 60000 makes them up to 2^36) leave weights in fp16's range.
 //
 // Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 143 us,
 // 5.8 TB/s (a plain read reaches 6.05), and 5 for the join.  Many requests of all lengths up to 4096, 64 of them, 100 MB,
@@ -58,6 +60,7 @@ __device__ __forceinline__ half8_t widen_k(uint32_t w0, uint32_t w1) {
     return __builtin_bit_cast(half8_t, h);
 }
 constexpr float kCode = 16777216.0f;  // 2^24
+constexpr float kLowest = -0x1p10f;   // below every score in that form: 128 * 255 * 2^16 / 2^24 at most
 // Eight codes of V as fp16, exactly: 1024 + (code + 128) - 1152.  (K's form would leave an error of 128 times the rounding
 // of the weights' sum in an output whose values are all small.)
 __device__ __forceinline__ half8_t widen_v(uint32_t w0, uint32_t w1) {
@@ -263,9 +266,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][t][r]);
-                const float sk24 = sk * kCode, base = fmaf(-sk, q128[n], sv);
-                top = fmaf(top, sk24, base);
-                top = fmaxf(top, __shfl_xor(top, 16));
+                const float sk24 = sk * kCode, most = fmaxf(top, kLowest), mine = fmaf(top, sk24, fmaf(-sk, q128[n], sv));
+                top = fmaxf(mine, __shfl_xor(mine, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 if (__any(top > M[n])) {
                     const float to = fmaxf(M[n], top), f = __builtin_amdgcn_exp2f(M[n] - to);
@@ -274,12 +276,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_kernel(const KvArgs a) {
 #pragma unroll
                     for (int d = 0; d < DT; ++d) o[n][d] *= f;
                 }
-                const float off = base - (M[n] - kUpLog2);
+                const float off = mine - M[n] + kUpLog2;                  // of the lane's largest, kUpLog2 at most whatever its size
                 float sum = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    const float w0 = __builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][k & 3], sk24, off));
-                    const float w1 = __builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][(k & 3) + 1], sk24, off));
+                    const float w0 = __builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][k & 3] - most, sk24, off));
+                    const float w1 = __builtin_amdgcn_exp2f(fmaf(s[n][k >> 2][(k & 3) + 1] - most, sk24, off));
                     sum += w0 + w1;
                     p[n][k >> 3][k & 7] = (_Float16)w0;
                     p[n][k >> 3][(k & 7) + 1] = (_Float16)w1;

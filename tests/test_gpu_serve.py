@@ -828,3 +828,27 @@ def test_packed_scores_of_minus_infinity(agq, D, n, m, quiet):
     got = check_packed(agq, q, k, v, ramp([n]), ramp([m]), finite=False)
     keys = np.arange(n) + m - n + 1
     assert np.isnan(got[(keys > 0) & (keys <= quiet)]).all() and (got[keys <= 0] == 0).all() and np.isfinite(got[keys > quiet]).all()
+
+
+# ------------------------------------------------------------------ scores of many millions
+
+@pytest.mark.parametrize("D,group,page", [(64, 1, 16), (128, 4, 64), (128, 20, 128)])
+@pytest.mark.parametrize("L,max_kv", [(40, 40), (700, 700), (3000, 3000), (20000, 200000)])
+@pytest.mark.parametrize("top,sign", [(700.0, 0), (8000.0, 0), (60000.0, 0), (8000.0, -1), (60000.0, 1)])
+def test_cache_scores_of_many_millions(agq, D, group, page, L, max_kv, top, sign):
+    """queries of up to 60000 against codes of every size on pages of one scale: the loudest keys take all, however large the scores are;
+    all scores negative, and all positive"""
+    r = rng_of(50, D, L, int(top), sign + 1)
+    table, n_pages = make_pages(r, [L], page)
+    pattern = np.ones(D) if sign else r.choice([-1, 1], D)
+    size = np.clip(r.integers(-127, 128, (n_pages, 1, page, 1)), -127 if sign <= 0 else 5, 127 if sign >= 0 else -5)
+    k, v = (size * pattern).astype(np.int8), r.integers(-127, 128, (n_pages, 1, D, page)).astype(np.int8)
+    ke, ve = np.full((n_pages, 1), 9, np.int8), np.full((n_pages, 1), -7, np.int8)
+    q = (r.uniform(0.5, 1.0, (2, group, 1)) * top * pattern).astype(np.float16)
+    got = host(agq.attn_kv(dev(q), i32([0, 2]), i32([L]), i32(table), *(dev(c) for c in (k, v, ke, ve)), 2, max_kv)).astype(np.float64)
+    codes = size[table[0, :-(-L // page)], 0, :, 0].reshape(-1)
+    values, _ = so.cache_rows(v, ve, table[0], L, 0, True)
+    for i in range(2):
+        seen = codes[:L - 1 + i]
+        want = values[:L - 1 + i][seen == seen.max()].mean(0)
+        assert np.abs(got[i] - want).max() <= 2.0 ** -10, (i, np.abs(got[i] - want).max())
