@@ -240,7 +240,6 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = float16_t{};
     const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
-
     auto max3 = [](float x, float y, float z) { return fmaxf(fmaxf(x, y), z); };
     auto top_of = [&](const float16_t &s) {
         const float t0 = max3(s[0], s[1], s[2]), t1 = max3(s[3], s[4], s[5]), t2 = max3(s[6], s[7], s[8]), t3 = max3(s[9], s[10], s[11]);
@@ -248,8 +247,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         const auto both = __builtin_amdgcn_permlane32_swap(x, x, false, false);      // the other sixteen keys of the query
         return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
     };
-    auto weigh = [&](const float16_t &s, half8_t (&p)[2], int g) {   // scores 2 g and 2 g + 1
-        const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * g], c, -off)), (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * g + 1], c, -off))};
+    auto weigh = [&](float x0, float x1, half8_t (&p)[2], int g) {   // of scores 2 g and 2 g + 1, their exponents
+        const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(x0), (_Float16)__builtin_amdgcn_exp2f(x1)};
         uint32_t bits = __builtin_bit_cast(uint32_t, w);
         asm volatile("" : "+v"(bits));                             // here, beside the matrix instructions, not where p is used
         uint4_t all = __builtin_bit_cast(uint4_t, p[g >> 2]);
@@ -272,7 +271,10 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
     };
-    auto step_plain = [&](int u) __attribute__((always_inline)) {                                 // scores in s0, probabilities of the sub-tile before in p1
+    // Rows with scores of 2^26 and more: the multiply-add of a score and its reference would be off by powers of two, so the
+    // reference is a score here, the row's maximum, and is taken off before the scale.
+    auto step_plain = [&](int u, auto loud_tag) __attribute__((always_inline)) {                  // scores in s0, probabilities of the sub-tile before in p1
+        constexpr bool LOUD = decltype(loud_tag)::value;
         if (u + 1 < mine) scores(u + 1, s1);
         if (u > 0 && u - 1 < mine) {
             const uint32_t at = v_lane + slot(u - 1);
@@ -312,16 +314,18 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         }
         if (u < mine) {
             if (u >= whole) mask(u, s0);
-            const float top = top_of(s0), over = fmaf(top, c, -off);
-            if (__any(over > kSlack + kUpLog2)) {
-                const float to = over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off, f = __builtin_amdgcn_exp2f(off - to);
+            const float top = top_of(s0), over = LOUD ? top - off : fmaf(top, c, -off);
+            if (__any(over > (LOUD ? 0.0f : kSlack + kUpLog2))) {
+                const float to = LOUD ? fmaxf(top, off) : over > kSlack + kUpLog2 ? fmaf(top, c, -kUpLog2) : off;
+                const float f = __builtin_amdgcn_exp2f(LOUD ? (off - to) * c : off - to);
                 off = to;
                 l *= f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= f;
             }
+            auto exponent = [&](float x) { return LOUD ? fmaf(x - off, c, kUpLog2) : fmaf(x, c, -off); };
 #pragma unroll
-            for (int g = 0; g < 8; ++g) weigh(s0, p1, g);
+            for (int g = 0; g < 8; ++g) weigh(exponent(s0[2 * g]), exponent(s0[2 * g + 1]), p1, g);
         }
         s0 = s1;
     };
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
             constexpr int FROM = KS == 8 ? 2 : 1, DONE = (n.value - FROM) * 8 / (2 * KS - 1 - FROM), NEXT = (n.value + 1 - FROM) * 8 / (2 * KS - 1 - FROM);
             if constexpr (n.value >= FROM) {
 #pragma unroll
-                for (int g = DONE; g < (NEXT < 8 ? NEXT : 8); ++g) weigh(s, p, g);
+                for (int g = DONE; g < (NEXT < 8 ? NEXT : 8); ++g) weigh(fmaf(s[2 * g], c, -off), fmaf(s[2 * g + 1], c, -off), p, g);
             }
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -393,6 +397,17 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
         copy_v();
         meet<2 * COPIES + COPIES>();
         if (mine > 0) scores(0, s0);
+        // Whether a row's scores might reach 2^26, by |q| |k| with the largest finite key: half of q is a lane's, so queries of 45 and
+        // more in every dimension.
+        float square[4] = {};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                const half2_t two = {q[st][2 * e], q[st][2 * e + 1]};
+                square[e] = __builtin_amdgcn_fdot2(two, two, square[e], false);
+            }
+        const bool loud = __any(((square[0] + square[1]) + (square[2] + square[3])) * (c * c) > 0x1p19f / D);
         // Between two pairs of steps: keys' sub-tiles u + 1, u + 2 and values' u - 1, u have landed, and nobody reads the slots
         // any more that the next ones (keys' up to u + 4, values' up to u + 2) get.
         auto turn = [&]() __attribute__((always_inline)) {
@@ -410,15 +425,23 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(const PackedArgs a)
             step_full(u, s0, s1, p0, p1, fr, std::true_type{}, std::false_type{});
             step_full(u + 1, s1, s0, p1, p0, fr, std::false_type{}, mask_tag);
         };
-        for (; u + 1 < whole; u += 2) pair(std::false_type{});
-        if (u + 1 == whole) {
-            pair(std::true_type{});
-            u += 2;
-        }
-        for (; u <= steps; u += 2) {
-            turn();
+        auto rest = [&](auto loud_tag) __attribute__((always_inline)) {
+            for (; u <= steps; u += 2) {
+                turn();
 #pragma unroll 1
-            for (int e = 0; e < 2; ++e) step_plain(u + e);
+                for (int e = 0; e < 2; ++e) step_plain(u + e, loud_tag);
+            }
+        };
+        if (__builtin_expect(loud, 0)) {
+            rest(std::true_type{});
+            off = fmaf(off, c, -kUpLog2);
+        } else {
+            for (; u + 1 < whole; u += 2) pair(std::false_type{});
+            if (u + 1 == whole) {
+                pair(std::true_type{});
+                u += 2;
+            }
+            rest(std::false_type{});
         }
         __builtin_amdgcn_s_waitcnt(0x70);                          // the last copies have landed before the LDS is given back
     }

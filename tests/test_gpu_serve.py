@@ -852,3 +852,37 @@ def test_cache_scores_of_many_millions(agq, D, group, page, L, max_kv, top, sign
         seen = codes[:L - 1 + i]
         want = values[:L - 1 + i][seen == seen.max()].mean(0)
         assert np.abs(got[i] - want).max() <= 2.0 ** -10, (i, np.abs(got[i] - want).max())
+
+
+def loud_rows(r, n, m, D, top, key):
+    """q [n, D] and k [m, D] of one sign pattern, so that scores are products of two sizes; keys' sizes are 8 / 1024 of `key` apart at least: far
+    more, in scores, than the 2^-16 of them that fp32 sums may be off by, so every row's softmax is one key, or those of one size"""
+    sign = r.choice([-1.0, 1.0], D)
+    size = r.integers(-128, 128, m) * (key / 128)
+    return (r.uniform(0.5, 1.0, (n, 1)) * top * sign).astype(np.float16), (size[:, None] * sign).astype(np.float16), size
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,m", [(5, 40), (130, 130), (300, 500), (20, 3000)])
+@pytest.mark.parametrize("top,key", [(700.0, 700.0), (3000.0, 3000.0), (8000.0, 8000.0), (60000.0, 60000.0), (20.0, 60000.0), (40.0, 60000.0), (60000.0, 20.0)])
+def test_packed_scores_of_many_millions(agq, D, causal, n, m, top, key):
+    """queries and keys of up to 60000: a row's loudest keys take all, however large the scores are"""
+    r = rng_of(51, D, n, m, int(top), int(key))
+    q, k, size = loud_rows(r, 2 * n, m, D, top, key)
+    q, k, v = q.reshape(n, 2, D), k.reshape(m, 1, D), r.uniform(-1, 1, (m, 1, D)).astype(np.float16)
+    got = host(agq.attn_packed(dev(q), dev(k), dev(v), i32([0, n]), i32([0, m]), causal=causal)).astype(np.float64)
+    for i in range(n):
+        seen = size[:m - n + i + 1] if causal else size
+        want = v[:len(seen), 0].astype(np.float64)[seen == seen.max()].mean(0)
+        assert np.abs(got[i] - want).max() <= 2.0 ** -10, (i, np.abs(got[i] - want).max())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,m", [(130, 130), (300, 300), (20, 3000)])
+def test_packed_loud_rows_beside_others(agq, D, n, m):
+    """a few queries a thousand times the others, in the same tiles: every row within its own bound"""
+    r = rng_of(52, D, n)
+    q, k, v = random_qkv(r, n, m, 2, 1, D)
+    q[3::17] *= np.float16(1000.0)
+    check_packed(agq, q, k, v, ramp([n]), ramp([m]))
