@@ -517,8 +517,9 @@ int agq_cascade_keep(int64_t S, double beta, int m, int64_t *keep_out);
  * gives back pages).                                                                                                 */
 
 /* The cache of one layer.  Entry (token, d) of page p and head h is the code k[p, h, token, d] with the scale
- * 2^k_exp[p, h]; values lie transposed inside a page, v[p, h, d, token], scale 2^v_exp[p, h].  All pages of a cache lie
- * in one allocation; n_pages * page < 2^31.  HOST struct, read before a call returns.                                */
+ * 2^k_exp[p, h]; values lie transposed inside a page, v[p, h, d, token], scale 2^v_exp[p, h].  agq_kv_append makes
+ * exponents of -30 .. 10; agq_attn_kv reads any, those beyond -64 .. 64 as the nearer of the two.  All pages of a cache
+ * lie in one allocation; n_pages * page < 2^31.  HOST struct, read before a call returns.                            */
 typedef struct agq_kv_cache {
     int8_t *k;              /* int8 [n_pages, Hkv, page, D]                          */
     int8_t *v;              /* int8 [n_pages, Hkv, D, page]                          */
@@ -571,9 +572,9 @@ int agq_kv_append(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, con
  * A row that sees no key is 0, one that sees keys with scores of -infinity only is NaN.  Keys and values that a row does
  * not see do not reach it, infinities and NaN included; an infinity or NaN among the values that it sees makes their
  * column of it infinite or NaN.
- * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D], ldk and ldv at most 2^24; cu_q, cu_k [B+1].  scale > 0, usually
- * 1 / sqrt(D).  workspace: agq_attn_packed_workspace_bytes (0, and NULL, unless there are few queries and many keys):
- * partial results where workgroups share the keys of a tile of queries; contents are scratch.
+ * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D], ldk and ldv at most 2^24; cu_q, cu_k [B+1].  2^-60 <=
+ * scale <= 2^24, usually 1 / sqrt(D).  workspace: agq_attn_packed_workspace_bytes (0, and NULL, unless there are few
+ * queries and many keys): partial results where workgroups share the keys of a tile of queries; contents are scratch.
  * Scores, maxima, sums and the accumulated output are fp32; a probability is rounded to fp16 (by 2^-11 of it at
  * most) for the product with v; the output is rounded once.                                                            */
 size_t agq_attn_packed_workspace_bytes(int64_t Tq, int64_t Hq, int64_t Tk, int64_t Hkv, int64_t D, int64_t B);
@@ -590,8 +591,8 @@ int agq_attn_packed(const void *q_f16, int64_t ldq, int64_t Tq, int64_t Hq, cons
  * workspace); larger lengths are computed all the same.  Lengths beyond max_pages * page are cut to it, and tokens of a
  * page number outside the cache are left out.
  * q, o: fp16 [T, Hq, D].  workspace: agq_attn_kv_workspace_bytes (may be 0; NULL then): partial results where the keys
- * of a request are shared by several workgroups; contents are scratch.  Hq / Hkv <= 1024; B <= 65535;
- * max_pages * page, max_q and max_kv at most 2^30.
+ * of a request are shared by several workgroups; contents are scratch.  scale as in agq_attn_packed; Hq / Hkv <= 1024;
+ * B <= 65535; max_pages * page, max_q and max_kv at most 2^30.
  * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32.  For the product with v, and for it
  * alone, a probability times its page's scale of v is rounded to fp16: by 2^-11 of it at most, down to 2^-29 of the row's
  * largest such product, and by 2^-40 of that one below.                                                              */

@@ -34,7 +34,7 @@ typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 
-constexpr float kNone = -1e30f;       // the maximum of no keys
+constexpr float kNone = -1e37f;       // the maximum of no keys; scores are above -2^119 with a scale of 2^24 and exponents of 64
 constexpr float kUpLog2 = 15.0f;      // weights are 2^15 times what they are, in sums and product alike
 
 struct KvArgs {

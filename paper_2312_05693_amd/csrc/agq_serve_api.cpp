@@ -2,8 +2,6 @@
 #include "../../include/agq.h"
 #include "agq_internal.h"
 
-#include <math.h>
-
 namespace {
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
@@ -27,7 +25,8 @@ inline bool cache_ok(const agq_kv_cache *c) {
     return c && page_ok(c->page) && (c->D == 64 || c->D == 128) && c->Hkv >= 1 && c->Hkv <= kMaxHeads && c->n_pages >= 1 &&
            c->n_pages <= kMaxIndex / c->page && aligned(c->k, 16) && aligned(c->v, 16) && c->k_exp && c->v_exp;
 }
-inline bool scale_ok(float s) { return isfinite(s) && s > 0.0f; }
+// with it the largest and smallest scores that fp16 queries and keys, or codes of exponents -64 to 64, can make are normal fp32 numbers
+inline bool scale_ok(float s) { return s >= 0x1p-60f && s <= 0x1p24f; }
 inline bool apart(const void *a, size_t an, const void *b, size_t bn) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x + an <= y || y + bn <= x;

@@ -886,3 +886,45 @@ def test_packed_loud_rows_beside_others(agq, D, n, m):
     q, k, v = random_qkv(r, n, m, 2, 1, D)
     q[3::17] *= np.float16(1000.0)
     check_packed(agq, q, k, v, ramp([n]), ramp([m]))
+
+
+# ------------------------------------------------------------------ the ends of the scales' range
+
+@pytest.mark.parametrize("group", [1, 20])
+def test_cache_exponents_and_scale_at_their_ends(agq, group):
+    """exponents beyond -64 .. 64 are read as the nearer of the two; scores of 2^118, all of them negative, and masked keys beside scores
+    of 2^-120"""
+    r, page, D, L = rng_of(53, group), 16, 128, 200
+    table, n_pages = make_pages(r, [L], page)
+    k, v, ke, ve = random_cache(r, n_pages, 1, page, D)
+    q, rest = dev(random_q(r, 3, group, D)), (i32([0, 3]), i32([L]), i32(table))
+    call = lambda ke, ve, **kw: host(agq.attn_kv(kw.pop("q", q), *rest, *(dev(c) for c in (kw.pop("k", k), v, ke, ve)), 3, L, **kw))
+    for far, near in ((-128, -64), (-65, -64), (65, 64), (127, 64)):
+        some = r.random(ke.shape) < 0.5
+        for one in (0, 1):
+            a, b = ((np.where(some, e, ke).astype(np.int8), ve) if one else (ke, np.where(some, e, ve).astype(np.int8)) for e in (far, near))
+            assert np.array_equal(call(*a).view(np.uint16), call(*b).view(np.uint16)), (far, one)
+    # codes -5 .. -127 of one sign pattern, the same for all of q
+    size = r.integers(-127, -4, (n_pages, 1, page, 1))
+    loud = dict(q=dev(np.full((3, group, D), 60000.0, np.float16)), k=np.broadcast_to(size, k.shape).astype(np.int8), scale=2.0 ** 24)
+    got = call(np.full_like(ke, 64), np.full_like(ve, -7), **loud).astype(np.float64)
+    codes, values = size[table[0], 0, :, 0].reshape(-1), so.cache_rows(v, np.full_like(ve, -7), table[0], L, 0, True)[0]
+    for i in range(3):
+        seen = codes[:L - 2 + i]
+        assert np.abs(got[i] - values[:L - 2 + i][seen == seen.max()].mean(0)).max() <= 2.0 ** -10
+    got = call(np.full_like(ke, -64), np.full_like(ve, -7), scale=2.0 ** -60).astype(np.float64)      # no score differs from another
+    for i in range(3):
+        # fp16 weights of one size: the sum's roundings, and the output's
+        assert np.abs(got[i] - values[:L - 2 + i].mean(0)).max() <= 2.0 ** -11
+
+
+def test_packed_scale_at_its_ends(agq):
+    r = rng_of(54)
+    q, k, v = random_qkv(r, 50, 90, 2, 1, 64)
+    check_packed(agq, q, k, v, ramp([50]), ramp([90]), scale=2.0 ** -60)
+    got = host(agq.attn_packed(dev(q), dev(k), dev(v), i32([0, 50]), i32([0, 90]), scale=2.0 ** 24)).astype(np.float64)
+    s = np.einsum("ihd,jd->ihj", q.astype(np.float64), k[:, 0].astype(np.float64))
+    for i in range(50):
+        order = np.sort(s[i, :, :41 + i], -1)
+        assert (order[:, -1] - order[:, -2] > 2.0 ** -12).all()      # scores of 2^5: fp32 sums are off by less, 2^12 powers of two apart
+        assert np.array_equal(got[i], v[:41 + i, 0].astype(np.float64)[s[i, :, :41 + i].argmax(-1)])

@@ -182,3 +182,10 @@ def test_oracle_attention_against_torch():
     assert abs(got - want.numpy()).max() < 1e-13 and (bound > 0).all() and bound.max() < 2e-2
     assert so.exponent(127.0) == 0 and so.exponent(127.5) == 1 and so.exponent(0) == -30 and so.exponent(float("inf")) == 10
     assert so.exponent(2.0 ** -24) == -30 and so.exponent(65504.0) == 10
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -61, 1e-38, 2.0 ** 24 * (1 + 2.0 ** -23), 1e30, 3e38])
+def test_scales_out_of_range_are_refused(agq, scale):
+    """scales with which scores would leave fp32's normal numbers"""
+    assert agq.lib().agq_attn_packed(P, 512, 5, 4, P, 256, P, 256, 7, 2, 128, P, P, 2, 1, scale, P, 512, None, 0, None) == EINVAL
+    assert agq.lib().agq_attn_kv(cache_of(), P, 512, 3, 4, P, P, 3, P, 4, 1, 64, scale, P, 512, None, 0, None) == EINVAL
