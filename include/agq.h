@@ -572,9 +572,10 @@ int agq_kv_append(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, con
  * A row that sees no key is 0, one that sees keys with scores of -infinity only is NaN.  Keys and values that a row does
  * not see do not reach it, infinities and NaN included; an infinity or NaN among the values that it sees makes their
  * column of it infinite or NaN.
- * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D], ldk and ldv at most 2^24; cu_q, cu_k [B+1].  2^-60 <=
- * scale <= 2^24, usually 1 / sqrt(D).  workspace: agq_attn_packed_workspace_bytes (0, and NULL, unless there are few
- * queries and many keys): partial results where workgroups share the keys of a tile of queries; contents are scratch.
+ * q, o: fp16 [Tq, Hq, D]; k, v: fp16 [Tk, Hkv, D], ldk and ldv at most 2^24; cu_q, cu_k [B+1].
+ * 2^-60 <= scale <= 2^24, usually 1 / sqrt(D); B <= 2^20; Hq * (Tq / 128 + B) < 2^24 (a launch's workgroups).
+ * workspace: agq_attn_packed_workspace_bytes (0, and NULL, unless there are few queries and many keys): partial results
+ * where workgroups share the keys of a tile of queries; contents are scratch.
  * Scores, maxima, sums and the accumulated output are fp32; a probability is rounded to fp16 (by 2^-11 of it at
  * most) for the product with v; the output is rounded once.                                                            */
 size_t agq_attn_packed_workspace_bytes(int64_t Tq, int64_t Hq, int64_t Tk, int64_t Hkv, int64_t D, int64_t B);

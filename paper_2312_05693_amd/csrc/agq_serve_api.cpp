@@ -8,6 +8,7 @@ constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxIndex = 0x7FFFFFFF;
 constexpr int64_t kMaxHeads = 65536;
 constexpr int64_t kMaxRow = (int64_t)1 << 24;
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;      // workgroups of 256: a launch has less than 2^32 threads in a dimension
 
 inline int hip_status(int err) { return err == 0 ? AGQ_OK : AGQ_EHIP; }
 inline bool aligned(const void *p, uintptr_t n) { return p && (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -78,7 +79,7 @@ int agq_attn_packed(const void *q, int64_t ldq, int64_t Tq, int64_t Hq, const vo
                     int64_t ldo, void *workspace, size_t workspace_bytes, void *stream) {
     if (!heads_ok(Hq, Hkv, D) || !count_ok(Tq, kMaxTokens) || !count_ok(Tk, kMaxTokens) || !count_ok(B, (int64_t)1 << 20) || !scale_ok(scale))
         return AGQ_EINVAL;
-    if ((Tq / 64 + B) * Hq > kMaxIndex) return AGQ_EINVAL;               // workgroups
+    if (agq_packed_tiles(Tq, B) * Hq >= kMaxGroups) return AGQ_EINVAL;
     if (ldk > kMaxRow || ldv > kMaxRow) return AGQ_EINVAL;                // 32 rows are reached by 32-bit offsets
     if (Tq == 0 || B == 0) return AGQ_OK;
     if (!ints_ok(cu_q) || !ints_ok(cu_k) || !tensor_ok(q, ldq, Hq, D) || !tensor_ok(o, ldo, Hq, D)) return AGQ_EINVAL;

@@ -189,3 +189,9 @@ def test_scales_out_of_range_are_refused(agq, scale):
     """scales with which scores would leave fp32's normal numbers"""
     assert agq.lib().agq_attn_packed(P, 512, 5, 4, P, 256, P, 256, 7, 2, 128, P, P, 2, 1, scale, P, 512, None, 0, None) == EINVAL
     assert agq.lib().agq_attn_kv(cache_of(), P, 512, 3, 4, P, P, 3, P, 4, 1, 64, scale, P, 512, None, 0, None) == EINVAL
+
+
+def test_packed_refuses_more_workgroups_than_a_launch_has(agq):
+    """a launch has less than 2^32 threads in a dimension: 2^24 workgroups of 256 are too many"""
+    for Tq, B, H in ((1 << 20, 1 << 20, 32), (1 << 26, 1, 32), (1 << 19, 1 << 19, 32), (1 << 30, 1, 8), ((1 << 19) - 256, 1 << 19, 33)):
+        assert agq.lib().agq_attn_packed(P, H * 64, Tq, H, P, 64, P, 64, 0, 1, 64, P, P, B, 1, 0.1, P, H * 64, None, 0, None) == EINVAL, (Tq, B, H)
