@@ -664,6 +664,8 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     P = Hq = ldq = ldqo = ldko = 0
     pos_p = cos_p = sin_p = q_p = qo_p = ko_p = None
     if rope_cos is not None:
+        if rope_sin is None or pos is None:
+            raise ValueError("rope_cos, rope_sin and pos go together")
         P = rope_cos.shape[0]
         if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is _f32) \
                 or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
@@ -686,8 +688,8 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
                 ldqo = _like(q_out, (T, Hq, D), "q_out")
                 used.append(q_out)
             q_p, qo_p = q.data_ptr(), q_out.data_ptr()
-    elif q is not None or k_out is not None or pos is not None:
-        raise ValueError("q, k_out and pos go with rope tables")
+    elif q is not None or k_out is not None or pos is not None or rope_sin is not None:
+        raise ValueError("q, k_out, pos and rope_sin go with rope_cos")
     if q is None and q_out is not None:
         raise ValueError("q_out goes with q")
     _ok(lib().agq_kv_append(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, _ints(slot, T, "slot"), q_p, ldq, Hq, pos_p, cos_p, sin_p, P, qo_p,

@@ -195,3 +195,13 @@ def test_packed_refuses_more_workgroups_than_a_launch_has(agq):
     """a launch has less than 2^32 threads in a dimension: 2^24 workgroups of 256 are too many"""
     for Tq, B, H in ((1 << 20, 1 << 20, 32), (1 << 26, 1, 32), (1 << 19, 1 << 19, 32), (1 << 30, 1, 8), ((1 << 19) - 256, 1 << 19, 33)):
         assert agq.lib().agq_attn_packed(P, H * 64, Tq, H, P, 64, P, 64, 0, 1, 64, P, P, B, 1, 0.1, P, H * 64, None, 0, None) == EINVAL, (Tq, B, H)
+
+
+def test_binding_refuses_half_a_rotation(agq):
+    """rope_cos, rope_sin and pos without one of the others"""
+    h, i, c = tensors()
+    args, cos = (h(3, 2, 64), h(3, 2, 64), i(3), c(6, 2, 16, 64), c(6, 2, 64, 16), c(6, 2), c(6, 2)), torch.zeros(8, 32)
+    for kw in (dict(rope_cos=cos), dict(rope_sin=cos), dict(pos=i(3)), dict(rope_cos=cos, rope_sin=cos), dict(rope_cos=cos, pos=i(3)),
+               dict(rope_sin=cos, pos=i(3)), dict(rope_sin=cos, q=h(3, 4, 64))):
+        with pytest.raises(ValueError, match="go with|go together"):
+            agq.kv_append(*args, **kw)
