@@ -53,13 +53,14 @@ int agq_kv_append(const agq_kv_cache *cache, const void *k, int64_t ldk, const v
                   void *q_out, int64_t ldqo, void *k_out, int64_t ldko, void *stream) {
     if (!cache_ok(cache) || !count_ok(T, kMaxTokens)) return AGQ_EINVAL;
     const int64_t D = cache->D, Hkv = cache->Hkv;
+    if (Hq < 0 || Hq > kMaxHeads) return AGQ_EINVAL;
+    if (T == 0) return AGQ_OK;                                            // tensors of no tokens have no addresses
     const bool rope = rope_cos || rope_sin || pos;
-    if ((q != nullptr) != (q_out != nullptr) || Hq < 0 || Hq > kMaxHeads || (q != nullptr) != (Hq > 0)) return AGQ_EINVAL;
+    if ((q != nullptr) != (q_out != nullptr) || (q != nullptr) != (Hq > 0)) return AGQ_EINVAL;
     if (!rope && (q || k_out)) return AGQ_EINVAL;
     if (rope && (P < 1 || P > kMaxIndex || !aligned(rope_cos, 16) || !aligned(rope_sin, 16))) return AGQ_EINVAL;
     // workgroups and work items are counted in 31 bits
     if (T * (D / 16) > kMaxIndex / (Hq > 2 * Hkv ? Hq : 2 * Hkv) - 4096) return AGQ_EINVAL;
-    if (T == 0) return AGQ_OK;
     if (!ints_ok(slot) || (rope && !ints_ok(pos)) || !tensor_ok(k, ldk, Hkv, D) || !tensor_ok(v, ldv, Hkv, D)) return AGQ_EINVAL;
     if (q && (!tensor_ok(q, ldq, Hq, D) || !tensor_ok(q_out, ldqo, Hq, D))) return AGQ_EINVAL;
     if (k_out && !tensor_ok(k_out, ldko, Hkv, D)) return AGQ_EINVAL;

@@ -928,3 +928,21 @@ def test_packed_scale_at_its_ends(agq):
         order = np.sort(s[i, :, :41 + i], -1)
         assert (order[:, -1] - order[:, -2] > 2.0 ** -12).all()      # scores of 2^5: fp32 sums are off by less, 2^12 powers of two apart
         assert np.array_equal(got[i], v[:41 + i, 0].astype(np.float64)[s[i, :, :41 + i].argmax(-1)])
+
+
+# ------------------------------------------------------------------ calls that a program may make
+
+def test_no_tokens_no_requests(agq):
+    h = lambda *s: torch.zeros(*s, dtype=torch.float16, device="cuda")
+    cache = [torch.ones(s, dtype=torch.int8, device="cuda") for s in ((4, 2, 16, 64), (4, 2, 64, 16), (4, 2), (4, 2))]
+    cos = torch.zeros(8, 32, device="cuda")
+    q, k = agq.kv_append(h(0, 2, 64), h(0, 2, 64), i32([]), *cache, q=h(0, 4, 64), pos=i32([]), rope_cos=cos, rope_sin=cos)
+    assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64) and all((c == 1).all() for c in cache)
+    assert agq.attn_kv(h(0, 4, 64), i32([0, 0]), i32([7]), i32([[0]]), *cache, 0, 7).shape == (0, 4, 64)
+    assert agq.attn_packed(h(0, 4, 64), h(5, 2, 64), h(5, 2, 64), i32([0, 0]), i32([0, 5])).shape == (0, 4, 64)
+    o = h(3, 4, 64) + 7.0
+    agq.attn_kv(h(3, 4, 64), i32([0]), i32([]), i32(np.zeros((0, 1))), *cache, 1, 7, o=o)
+    agq.attn_packed(h(3, 4, 64), h(5, 2, 64), h(5, 2, 64), i32([0]), i32([0]), o=o)
+    assert (o == 7.0).all()
+    assert (agq.attn_packed(h(3, 4, 64), h(0, 2, 64), h(0, 2, 64), i32([0, 3]), i32([0, 0]), o=o) == 0).all()
+    assert (agq.attn_kv(h(3, 4, 64), i32([0, 3]), i32([0]), i32([[0]]), *cache, 3, 0, o=o + 7.0) == 0).all()

@@ -205,3 +205,11 @@ def test_binding_refuses_half_a_rotation(agq):
                dict(rope_sin=cos, pos=i(3)), dict(rope_sin=cos, q=h(3, 4, 64))):
         with pytest.raises(ValueError, match="go with|go together"):
             agq.kv_append(*args, **kw)
+
+
+def test_append_of_no_tokens_is_a_no_op(agq):
+    """whatever is asked for: tensors of no tokens have no addresses"""
+    call = lambda **kw: agq.lib().agq_kv_append(*dict(dict(cache=cache_of(), k=None, ldk=256, v=None, ldv=256, T=0, slot=None, q=None, ldq=512, Hq=4, pos=None,
+                                                          cos=P, sin=P, rows=64, q_out=None, ldqo=512, k_out=None, ldko=256, stream=None), **kw).values())
+    assert call() == 0 and call(Hq=0) == 0 and call(q=P, k_out=P) == 0
+    assert call(Hq=-1) == EINVAL and call(cache=None) == EINVAL and call(T=5) == EINVAL
