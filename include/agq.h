@@ -513,8 +513,8 @@ int agq_cascade_keep(int64_t S, double beta, int m, int64_t *keep_out);
  * ascending order; sequence b is tokens cu[b] .. cu[b+1] - 1 of the packed tensor, and rows that belong to no sequence
  * (padding behind the last one) are neither read nor written.  Offsets, lengths, page numbers and slots live on the
  * device and are never trusted with an address: whatever lies outside the tensors is left out.  Every call enqueues
- * kernels only, may be captured, and needs nothing cleared.  A call with no tokens is a no-op (agq_kv_map: it still
- * gives back pages).                                                                                                 */
+ * kernels only, may be captured, and needs nothing cleared.  Outputs overlap neither inputs nor each other unless a call
+ * says so.  A call with no tokens is a no-op (agq_kv_map: it still gives back pages).                                */
 
 /* The cache of one layer.  Entry (token, d) of page p and head h is the code k[p, h, token, d] with the scale
  * 2^k_exp[p, h]; values lie transposed inside a page, v[p, h, d, token], scale 2^v_exp[p, h].  agq_kv_append makes
@@ -540,7 +540,9 @@ typedef struct agq_kv_cache {
  * are missing; or -1 (a negative length, n_new < -1, a request longer than max_pages * page, more than T tokens, an
  * impossible free_state).  With a status other than 0 the step is left out: lengths, table, ring and state stay as they
  * are, cu_new is all 0 and every slot -1, so that calls which follow do nothing.
- * kv_len_out and free_state_out must not overlap kv_len and free_state (AGQ_EINVAL): a loop swaps two of each.
+ * kv_len_out and free_state_out must not overlap kv_len and free_state (AGQ_EINVAL): a loop swaps two of each.  Between
+ * steps a program may lower a length (a draft's tokens that were not taken) as far as the request keeps its pages;
+ * pages behind that would be lost, as nothing gives them back.
  * B <= 2^20; max_pages * page < 2^31; pos and slot may be NULL when T == 0.                                          */
 int agq_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int64_t page, int32_t *block_table,
                int64_t max_pages, int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T,
@@ -551,9 +553,10 @@ int agq_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int64_t p
  * (i, i + D/2), float64 arithmetic, rounded once to fp16; positions are clamped into the tables).
  * slot [T]: as agq_kv_map writes it.  A token whose slot is negative or not in the cache is left out: nothing of it is
  * read or written.  Codes: Eq.2 on the signed 8-bit grid with the step 2^e, e that of the page and head:
- *   e = the smallest e with max|x| <= 127 * 2^e over the tokens that this call writes there (infinities count as 2^16,
- *       all zeros as 2^-30's e), but not below the page's present e if earlier tokens lie in front of them (slot % page
- *       of the first one > 0); the codes of those are then divided by 2^(e - present e), halves to the even code.
+ *   e = the smallest e with max|x| <= 127 * 2^e over the tokens that this call writes there (infinities count as 2^16, a
+ *       NaN as nothing, all zeros as 2^-30's e), but not below the page's present e if earlier tokens lie in front of
+ *       them (slot % page of the first one > 0); the codes of those are then divided by 2^(e - present e), halves to the
+ *       even code.
  * Tokens of the call in one page have to be consecutive, in the order of their slots, and no slot twice, as agq_kv_map
  * makes them; otherwise the contents of that page (of no other memory) are unspecified.  Bytes of the page behind them
  * stay as they are.
@@ -594,9 +597,11 @@ int agq_attn_packed(const void *q_f16, int64_t ldq, int64_t Tq, int64_t Hq, cons
  * q, o: fp16 [T, Hq, D].  workspace: agq_attn_kv_workspace_bytes (may be 0; NULL then): partial results where the keys
  * of a request are shared by several workgroups; contents are scratch.  scale as in agq_attn_packed; Hq / Hkv <= 1024;
  * B <= 65535; max_pages * page, max_q and max_kv at most 2^30.
- * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32.  For the product with v, and for it
- * alone, a probability times its page's scale of v is rounded to fp16: by 2^-11 of it at most, down to 2^-29 of the row's
- * largest such product, and by 2^-40 of that one below.                                                              */
+ * Codes are exact in fp16; scores, maxima, sums and the accumulated output are fp32.  (A key enters its score's sum 128
+ * steps larger, which are taken out again: the sum's roundings are those of 128 * 2^k_exp * |q|_1 in size, as if every
+ * code of the page were that large.)  For the product with v, and for it alone, a probability times its page's scale of
+ * v is rounded to fp16: by 2^-11 of it at most, down to 2^-29 of the row's largest such product, and by 2^-40 of that
+ * one below.                                                                                                         */
 size_t agq_attn_kv_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t B, int64_t max_q, int64_t max_kv);
 int agq_attn_kv(const agq_kv_cache *cache, const void *q_f16, int64_t ldq, int64_t T, int64_t Hq, const int32_t *cu_q,
                 const int32_t *kv_len, int64_t B, const int32_t *block_table, int64_t max_pages, int64_t max_q,

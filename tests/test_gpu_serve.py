@@ -946,3 +946,165 @@ def test_no_tokens_no_requests(agq):
     assert (o == 7.0).all()
     assert (agq.attn_packed(h(3, 4, 64), h(0, 2, 64), h(0, 2, 64), i32([0, 3]), i32([0, 0]), o=o) == 0).all()
     assert (agq.attn_kv(h(3, 4, 64), i32([0, 3]), i32([0]), i32([[0]]), *cache, 3, 0, o=o + 7.0) == 0).all()
+
+@pytest.mark.parametrize("past,new", [([3], [1]), ([3, 0], [40, 7])])
+def test_append_nan_touches_nothing_else(agq, past, new):
+    """a NaN has no part in a page's scale; every other entry's code is as if it were 0"""
+    r, Hkv, D, page, n_pages = rng_of(55, len(new)), 2, 64, 16, 9
+    slot, _ = random_slots(r, past, new, page, n_pages, 1)
+    T = len(slot)
+    x = r.standard_normal((T, 2 * Hkv, D)).astype(np.float16)
+    odd = r.random(x.shape) < 0.02
+    odd[0, :, 7] = True
+    cache = random_cache(r, n_pages, Hkv, page, D, lo=-9, hi=-9)
+    d = [dev(c) for c in cache]
+    xd = dev(np.where(odd, np.float16(np.nan), x))
+    agq.kv_append(xd[:, :Hkv], xd[:, Hkv:], i32(slot), *d)
+    zero = np.where(odd, np.float16(0), x)
+    for half, at, turned in ((slice(0, Hkv), 0, False), (slice(Hkv, 2 * Hkv), 1, True)):
+        codes, exps = so.kv_append(zero[:, half], slot, cache[at], cache[2 + at], turned)
+        same = np.ones(codes.shape, bool)
+        for t, h, i in zip(*np.nonzero(odd[:, half])):
+            if slot[t] >= 0:
+                same[(slot[t] // page, h, i, slot[t] % page) if turned else (slot[t] // page, h, slot[t] % page, i)] = False
+        assert np.array_equal(host(d[2 + at]), exps) and np.array_equal(host(d[at])[same], codes[same])
+
+
+def test_tokens_a_gigabyte_apart(agq):
+    """distances between tokens of 2^30 elements (2^24 for packed keys and values): addresses behind 2^32 bytes"""
+    r, D, Hq, Hkv, T, far = rng_of(56), 64, 4, 2, 5, 1 << 30
+    buf = torch.zeros(4 * far + 16 * D, dtype=torch.float16, device="cuda")
+    apart = lambda heads, at, ld=far: buf.as_strided((T, heads, D), (ld, D, 1), at * D)
+    q, k, v = random_qkv(r, T, T, Hq, Hkv, D)
+    q_far, k_far, v_far, o_far = apart(Hq, 0), apart(Hkv, Hq), apart(Hkv, Hq + Hkv), apart(Hq, Hq + 2 * Hkv)
+    for t, x in ((q_far, q), (k_far, k), (v_far, v)):
+        t.copy_(dev(x))
+    cos, sin = (dev(t) for t in synth.rope_tables(64, D))
+    slot, pos, cu, lens, table = i32(np.arange(16, 16 + T)), i32(np.arange(T)), i32([0, T]), i32([T]), i32([[1]])
+    near, there = ([torch.zeros(s, dtype=torch.int8, device="cuda") for s in ((2, Hkv, 16, D), (2, Hkv, D, 16), (2, Hkv), (2, Hkv))] for _ in range(2))
+    rest = dict(pos=pos, rope_cos=cos, rope_sin=sin)
+    want_q, want_k = agq.kv_append(dev(k), dev(v), slot, *near, q=dev(q), **rest)
+    agq.kv_append(k_far, v_far, slot, *there, q=q_far, q_out=o_far, k_out=k_far, **rest)
+    assert torch.equal(o_far, want_q) and torch.equal(k_far, want_k) and all(torch.equal(a, b) for a, b in zip(near, there))
+    assert torch.equal(agq.attn_kv(q_far, cu, lens, table, *there, T, T, o=o_far), agq.attn_kv(dev(q), cu, lens, table, *near, T, T))
+    k_wide, v_wide = (buf.as_strided((T, Hkv, D), (1 << 24, D, 1), 4096 + at * D) for at in (0, Hkv))
+    k_wide.copy_(dev(k)), v_wide.copy_(dev(v))
+    assert torch.equal(agq.attn_packed(q_far, k_wide, v_wide, cu, cu, o=o_far), agq.attn_packed(dev(q), dev(k), dev(v), cu, cu))
+
+
+def test_pages_that_requests_share(agq):
+    """a prompt's pages in several tables, and one page twice in a table: they are read like any others"""
+    r, page = rng_of(57), 16
+    lens = [200, 170, 100]
+    table, n_pages = make_pages(r, lens, page)
+    table[1, :9], table[2, :6] = table[0, :9], table[0, :6]
+    table[0, 11] = table[0, 2]
+    check_cache(agq, random_q(r, 6, 4, 128), ramp([2, 2, 2]), lens, table, random_cache(r, n_pages, 2, page, 128))
+
+
+def test_joins_captured_and_replayed(agq):
+    """both attentions with shared keys in one graph, on one workspace one after the other; lengths, offsets and keys change between the
+    replays, and the program works in between"""
+    r, Hq, Hkv, D, page = rng_of(58), 4, 1, 128, 64
+    n, m, lens = 40, 3000, [20000, 9000]
+    table, n_pages = make_pages(r, lens, page)
+    cache = [dev(c) for c in random_cache(r, n_pages, Hkv, page, D)]
+    q, k, v = (dev(t) for t in random_qkv(r, n, m, Hq, Hkv, D))
+    cu_q, cu_k, cu_1, d_len, d_table = i32([0, 25, n]), i32([0, 1000, m]), i32([0, 1, 2]), i32(lens), i32(table)
+    most = 200000                                          # more than the lengths, as a program that captures a step says
+    ws = torch.empty(max(agq.attn_packed_workspace_bytes(n, Hq, m, Hkv, D, 2), agq.attn_kv_workspace_bytes(2, Hq, Hkv, D, 2, 1, most)),
+                     dtype=torch.uint8, device="cuda")
+    assert agq.attn_packed_workspace_bytes(n, Hq, m, Hkv, D, 2) > 0 and agq.attn_kv_workspace_bytes(2, Hq, Hkv, D, 2, 1, most) > 0
+    o, a = torch.empty(n, Hq, D, dtype=torch.float16, device="cuda"), torch.empty(2, Hq, D, dtype=torch.float16, device="cuda")
+
+    def both(o, a, ws):
+        agq.attn_packed(q, k, v, cu_q, cu_k, o=o, workspace=ws)
+        agq.attn_kv(o[:2], cu_1, d_len, d_table, *cache, 1, most, o=a, workspace=ws)
+    both(o, a, ws)
+    torch.cuda.synchronize()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        both(o, a, ws)
+    for cut, key, x, y in ((25, 1000, 20000, 9000), (0, 0, 0, 9000), (39, 2999, 64, 1), (3, 40, 19999, 8999), (25, 1000, 20000, 9000)):
+        cu_q.copy_(i32([0, cut, n])), cu_k.copy_(i32([0, key, m])), d_len.copy_(i32([x, y]))
+        k.mul_(1.0625)
+        o2, a2 = torch.empty_like(o), torch.empty_like(a)
+        both(o2, a2, torch.full_like(ws, 255))
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, o2) and torch.equal(a, a2), (cut, x)
+        q.clone().mul_(2.0).sum().item()
+
+
+# ------------------------------------------------------------------ parts of wider tensors, in and out
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 6, 2), (128, 4, 4)])
+@pytest.mark.parametrize("n,lens,max_kv", [(1, [70, 300], 300), (5, [70, 300], 300), (12, [90, 40], 90), (1, [3000, 40], 3000), (6, [3000, 700], 3000),
+                                           (3, [20000], 200000)])
+def test_cache_in_and_out_of_wider_tensors(agq, D, Hq, Hkv, n, lens, max_kv):
+    """several new tokens, q a part of a projection's output and o a part of a wider tensor, whose other bytes stay; one launch, a join, and
+    pieces that the device chooses"""
+    r, B = rng_of(45, D, n, sum(lens)), len(lens)
+    table, n_pages = make_pages(r, lens, 64)
+    cache = [dev(c) for c in random_cache(r, n_pages, Hkv, 64, D)]
+    T = n * B + 3
+    x, wide = dev(random_q(r, T, Hq + 2 * Hkv, D)), torch.full((T, Hq + 3, D), 7.0, dtype=torch.float16, device="cuda")
+    rest = (i32(ramp([n] * B) + 1), i32(lens), i32(table), *cache, n, max_kv)
+    want = agq.attn_kv(x[:, :Hq].contiguous(), *rest, o=torch.full((T, Hq, D), 7.0, dtype=torch.float16, device="cuda"))
+    check_cache(agq, host(x[:, :Hq].contiguous()), ramp([n] * B) + 1, lens, table, [host(c) for c in cache], max_q=n, max_kv=max_kv)
+    assert agq.attn_kv(x[:, :Hq], *rest, o=wide[:, 2:2 + Hq]).data_ptr() == wide[:, 2:].data_ptr()
+    assert torch.equal(wide[:, 2:2 + Hq], want) and (wide[:, :2] == 7.0).all() and (wide[:, 2 + Hq:] == 7.0).all()
+    assert (wide[0] == 7.0).all() and (wide[-2:] == 7.0).all()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 6, 2), (128, 4, 4)])
+@pytest.mark.parametrize("n,m", [([70, 300], [70, 300]), ([1, 130], [2500, 4000]), ([100], [3000])])
+def test_packed_out_into_a_wider_tensor(agq, D, Hq, Hkv, n, m):
+    """o a part of a wider tensor, whose other bytes stay; with and without a join"""
+    r = rng_of(46, D, sum(n))
+    q, k, v = (dev(t) for t in random_qkv(r, sum(n) + 2, sum(m), Hq, Hkv, D))
+    wide = torch.full((sum(n) + 2, Hq + 3, D), 7.0, dtype=torch.float16, device="cuda")
+    cu = (i32(ramp(n) + 1), i32(ramp(m)))
+    want = agq.attn_packed(q, k, v, *cu, o=torch.full((sum(n) + 2, Hq, D), 7.0, dtype=torch.float16, device="cuda"))
+    agq.attn_packed(q, k, v, *cu, o=wide[:, 1:1 + Hq])
+    assert torch.equal(wide[:, 1:1 + Hq], want) and (wide[:, :1] == 7.0).all() and (wide[:, 1 + Hq:] == 7.0).all()
+    assert (wide[0] == 7.0).all() and (wide[-1] == 7.0).all()
+    check_packed(agq, *(host(t) for t in (q, k, v)), ramp(n) + 1, ramp(m))
+
+
+# ------------------------------------------------------------------ many sequences, and pieces that the device chooses
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 2, 1), (128, 2, 2)])
+def test_packed_a_thousand_sequences(agq, D, Hq, Hkv):
+    """sixteen times as many as a wavefront looks at together, empty ones and ones of several tiles among them"""
+    r = rng_of(47, D)
+    n = r.integers(0, 12, 1000)
+    n[[3, 500, 999]] = [200, 0, 140]
+    m = n + r.integers(0, 9, 1000)
+    check_packed(agq, *random_qkv(r, int(n.sum()), int(m.sum()), Hq, Hkv, D), ramp(n), ramp(m))
+
+
+@pytest.mark.parametrize("max_kv", [64, 4096])
+def test_cache_a_thousand_requests(agq, max_kv):
+    """in one launch, and with room for several pieces each, of which few requests have more than one"""
+    r, page = rng_of(48), 32
+    lens = r.integers(0, 60, 1000)
+    lens[[0, 640, 999]] = [700, 1500, 900]
+    table, n_pages = make_pages(r, lens, page)
+    check_cache(agq, random_q(r, 1000, 2, 64), ramp([1] * 1000), lens, table, random_cache(r, n_pages, 1, page, 64), max_kv=max_kv)
+
+
+@pytest.mark.parametrize("lens,max_kv", [([20000, 3, 0, 9000], 100000), ([16383, 16384, 16385], 60000), ([30000, 70], 90000), ([0, 0, 8000, 1, 0, 5000, 257, 256], 30000)])
+@pytest.mark.parametrize("D,Hq,Hkv,page", [(128, 4, 1, 64), (64, 6, 2, 16)])
+def test_cache_pieces_that_the_device_chooses(agq, lens, max_kv, D, Hq, Hkv, page):
+    """max_kv large enough that a CU has 640 keys or more of it, so that the pieces' size comes from the lengths: the workspace has room for the
+    pieces that max_kv over the pieces per request makes, not for 512 keys each"""
+    r, B = rng_of(49, sum(lens), D), len(lens)
+    assert max_kv * B * Hkv >= 256 * 640 and 2 * B <= 256 // Hkv
+    most = 4 * (256 // Hkv) // B if B > 4 else 256 // Hkv
+    keys = max(1024, -(-(-(-max_kv // most)) // 256) * 256)
+    table, n_pages = make_pages(r, lens, page)
+    assert agq.attn_kv_workspace_bytes(B, Hq, Hkv, D, B, 1, max_kv) == -(-max_kv // keys) * B * Hq * (D * 4 + 8)
+    check_cache(agq, random_q(r, B, Hq, D), ramp([1] * B), lens, table, random_cache(r, n_pages, Hkv, page, D), max_kv=max_kv)
