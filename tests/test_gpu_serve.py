@@ -1108,3 +1108,25 @@ def test_cache_pieces_that_the_device_chooses(agq, lens, max_kv, D, Hq, Hkv, pag
     table, n_pages = make_pages(r, lens, page)
     assert agq.attn_kv_workspace_bytes(B, Hq, Hkv, D, B, 1, max_kv) == -(-max_kv // keys) * B * Hq * (D * 4 + 8)
     check_cache(agq, random_q(r, B, Hq, D), ramp([1] * B), lens, table, random_cache(r, n_pages, Hkv, page, D), max_kv=max_kv)
+
+
+def test_lengths_lowered_between_steps(agq):
+    """a draft's tokens that were not taken: the program lowers the lengths inside the requests' pages, the next step writes over them"""
+    r, Hq, Hkv, D, page, B = rng_of(59), 4, 2, 64, 16, 2
+    s = Server(agq, B, page, 8, Hq, Hkv, D)
+    draw = lambda T: r.standard_normal((T, Hq + 2 * Hkv, D)).astype(np.float16)
+    s.step(dev(draw(30)), i32([20, 10]), 64)
+    before = [host(t).copy() for t in (s.table, s.ring, s.free)]
+    s.step(dev(draw(9)), i32([4, 5]), 64)
+    s.kv_len = i32([21, 12])                               # three and three of them go
+    x = draw(3)
+    o, _, st = s.step(dev(x), i32([1, 2]), 64)
+    assert host(st.status)[0] == 0 and list(host(st.kv_len)) == [22, 14] and list(host(st.pos)) == [21, 12, 13]
+    assert all(np.array_equal(a, host(t)) for a, t in zip(before, (s.table, s.ring, s.free)))
+    cache, q, cu = [host(t) for t in s.cache], so.rotate(x[:, :Hq], host(st.pos), *(host(t) for t in s.rope)), host(st.cu_new)
+    for b, L in enumerate((22, 14)):
+        for h in range(Hq):
+            k, _ = so.cache_rows(cache[0], cache[2], before[0][b], L, h * Hkv // Hq, False)
+            v, _ = so.cache_rows(cache[1], cache[3], before[0][b], L, h * Hkv // Hq, True)
+            want, bound = so.attention(q[cu[b]:cu[b + 1], h].astype(np.float64), k, v, L - (cu[b + 1] - cu[b]))
+            assert (np.abs(host(o)[cu[b]:cu[b + 1], h] - want) <= bound).all()
