@@ -17,8 +17,9 @@
 // above 0 whatever the rounding, so scores of any size (an fp16 query of 60000 makes them up to 2^36) leave weights in fp16's range.
 //
 // Bound and figures.  Long caches: memory; 4 requests of 60000 to 131072 tokens, 8 key heads of 128, 827 MB in 143 us,
-// 5.8 TB/s (a plain read reaches 6.05), and 5 for the join.  Many requests of all lengths up to 4096, 64 of them, 100 MB,
-// 26.7 us with the join: a chunk's bytes take 2.7 us to come.  One request of 1000 tokens, 10.4 us: what 32 CUs can have on
+// 5.8 TB/s (a plain read reaches 6.05), and 5 for the join, in a trace; 149 one call after the other, 155 in a replayed graph.
+// Many requests of all lengths up to 4096, 64 of them, 100 MB, 26.6 us with the join: a chunk's bytes take 2.7 us to come.
+// One request of 1000 tokens, 10.3 us: what 32 CUs can have on
 // its way, the launch and the join of the wavefronts.  Bytes requested two chunks ahead change nothing where the registers
 // hold them (D = 64) and spill otherwise (13.9 us); so do sixteen wavefronts to a workgroup (23 us) and three workgroups to a
 // CU (64 requests, 30.8).
