@@ -10,7 +10,7 @@
 //
 // Bound and figures.  Long prompts: a step of 32 keys has 2 D / 16 matrix instructions of 32 cycles and about as many cycles of
 // vector arithmetic, and the two units mostly take turns: 16000 tokens in seven prompts of up to 8191, 32 heads on 8, D = 128,
-// 770 to 835 us from box to box, 890 to 970 TFLOP/s (a library product of two matrices of that size class reaches 1264),
+// 770 to 835 us from card to card, 890 to 970 TFLOP/s (a library product of two matrices of that size class reaches 1264),
 // matrix cores busy 54 % of the cycles and the vector ALU 48 %; D = 64, with half the products for the same exponentials, 451
 // to 480 us, 780 to 830.  One prompt of 2048 in 40 heads, 59 to 62 us: its longest tiles, 64 steps, take 42 with a CU to
 // themselves and 54 in pairs.  A handful of short prompts 7.6 us, of which an empty launch is 1.6.
@@ -539,7 +539,7 @@ int launch(PackedArgs a, hipStream_t st) {
     // One causal prompt: its longest tiles go first, and workgroup n + 256 gets its place on the CU of workgroup n.  So the
     // second 256 are taken in the opposite order (eight at a time, for the XCDs): the longest share a CU with the shortest.
     // Tokens x heads of 128: 4096 x 32 164 -> 157 us, 2048 x 32 54 -> 52, 2500 x 28 65.5 -> 63.7, 6000 x 12 of 64 90 -> 86,
-    // 8192 x 32 and longer level; 2048 x 40, where the shortest tiles of all follow, 59.5 -> 60.5 (both sides on one box).
+    // 8192 x 32 and longer level; 2048 x 40, where the shortest tiles of all follow, 59.5 -> 60.5 (both sides on one card).
     a.turned = 0;
     if (a.B == 1 && a.causal && a.splits == 1) a.turned = groups < 512 ? (int)groups & ~7 : 512;
     attn_packed_kernel<D><<<dim3(groups, (unsigned)a.splits), 256, 0, st>>>(a);

@@ -404,7 +404,7 @@ struct AgqAttnKv {
 // per workgroup, row_tiles workgroups over the rows, up to `splits` splits of a request's keys with split_keys keys each (a
 // multiple of 64), and with more than one a second launch that joins them; pieces != 0: that many splits in all for a key
 // head, of a size that the device chooses from the lengths, split_keys at least.  groups = workgroups without a split.
-// Measured in a replayed graph, with the join, all sides of a comparison on one box (32 query heads on 8 key heads, D = 128, B
+// Measured in a replayed graph, with the join, all sides of a comparison on one card (32 query heads on 8 key heads, D = 128, B
 // requests x tokens):
 //   one workgroup of eight wavefronts per CU or less, and few keys: no split, as its launch costs more than it saves (8 x 500
 //     7.5 us; 1 x 1000 10.3 against 8.5 with 256 keys a split, but the host takes 4 us for a launch); 32 x 1000 15.0 against
