@@ -608,6 +608,104 @@ int agq_attn_kv(const agq_kv_cache *cache, const void *q_f16, int64_t ldq, int64
                 int64_t max_kv, float scale, void *o_f16, int64_t ldo, void *workspace, size_t workspace_bytes,
                 void *stream);
 
+/* agq_kv_append for models that normalise their queries and keys per head: before the rotation
+ *   y[i] = x[i] * g[i] / sqrt(mean(x^2) + eps)        over the D values of each head of q and of k, not of v,
+ * and y is rotated and rounded once: float64 arithmetic from the fp16 input to the fp16 result.
+ * g_q, g_k: fp16, 16-byte aligned, [D] for all heads (ldgq, ldgk = 0) or [heads, D] with ldg elements between heads (a
+ * multiple of 8, at least D).  g_q is NULL where q is.  eps >= 0.  q, q_out and k_out may be given without tables (pos,
+ * rope_cos, rope_sin NULL: no rotation).  Everything else as in agq_kv_append.                                          */
+int agq_kv_append_norm(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, const void *v_f16, int64_t ldv, int64_t T,
+                       const int32_t *slot, const void *q_f16, int64_t ldq, int64_t Hq, const void *g_q_f16, int64_t ldgq,
+                       const void *g_k_f16, int64_t ldgk, double eps, const int32_t *pos, const float *rope_cos,
+                       const float *rope_sin, int64_t P, void *q_out_f16, int64_t ldqo, void *k_out_f16, int64_t ldko, void *stream);
+
+/* The same normalisation and rotation without a cache, fp16 to fp16, for texts that are only scored (agq_attn_packed reads
+ * the results).  q: fp16 [T, Hq, D], k: [T, Hkv, D]; either may be absent (NULL, with its output, and 0 heads).  A gain that
+ * is NULL: that tensor is not normalised.  No tables (all three NULL): no rotation; one of the two has to be there.  q_out
+ * and k_out may be q and k themselves.  T * (Hq + Hkv) * D < 2^35.                                                        */
+int agq_qk_norm_rope(const void *q_f16, int64_t ldq, int64_t Hq, const void *k_f16, int64_t ldk, int64_t Hkv, int64_t T, int64_t D,
+                     const void *g_q_f16, int64_t ldgq, const void *g_k_f16, int64_t ldgk, double eps, const int32_t *pos,
+                     const float *rope_cos, const float *rope_sin, int64_t P, void *q_out_f16, int64_t ldqo, void *k_out_f16,
+                     int64_t ldko, void *stream);
+
+/* ---- Pages that several requests hold, requests that go on as copies of others, and requests that lose tokens.
+ *
+ * shared [n_pages] counts the requests that hold a page beyond the first one: 0 for a free page and for one with a single
+ * holder (a count below 0 is taken as 0).  To begin with all are 0; agq_kv_map neither needs nor changes them, as the pages
+ * that it takes are free.  But it gives pages back without looking: with shared pages around, requests are ended by
+ * agq_kv_fork.  A request writes only into the page that its length ends in, so full pages can be shared; agq_kv_fork and
+ * agq_kv_compact leave every partly filled page that a request would write into to that request alone.  A length that a
+ * program lowers by itself must therefore stay within the last page if that one is not shared; agq_kv_compact takes any.
+ * Both calls work from the old lengths, table, counts and ring state to new ones, which must not overlap them (AGQ_EINVAL;
+ * a loop swaps two of each), on the device, in three launches; the ring alone is updated in place, behind the free pages.
+ * Pages are taken at the ring's head in the order of requests and entries, as in agq_kv_map; pages that lost their last
+ * holder are given back in ascending order, and are not taken again by the same call.  Entries of block_table_out behind a
+ * request's pages are left as they are.  *status: 0; or the number of free pages that are missing; or -1 (an impossible
+ * free_state, a length that is negative or beyond max_pages * page, and what each call adds).  With a status other than 0
+ * nothing happens: the outputs are copies of the inputs, and the calls that follow do nothing.
+ * 0 <= B <= AGQ_KV_MAX_FORK.  Everything is captured and replayed like the other calls.                                 */
+#define AGQ_KV_MAX_FORK 4096
+
+/* After the call request b is what request parent[b] was before it: itself (parent[b] == b), a copy of another one, or
+ * nothing (-1: length 0).  A request that is nobody's parent has ended.  Full pages are held by every copy; a partly filled
+ * last page goes to the first copy (the lowest b; to none if the page is shared), and the others get a free page each that
+ * it has to be copied into: copy_src[b] to copy_dst[b], -1 where nothing is to be copied.  agq_kv_copy_pages does that, in
+ * every layer, before anything else is written into the cache.  status -1 also for a parent outside -1 .. B - 1.          */
+int agq_kv_fork(const int32_t *kv_len, const int32_t *parent, int64_t B, int64_t page, const int32_t *block_table,
+                int64_t max_pages, const int32_t *shared, int32_t *free_ring, int64_t n_pages, const int32_t *free_state,
+                int32_t *kv_len_out, int32_t *block_table_out, int32_t *shared_out, int32_t *copy_src, int32_t *copy_dst,
+                int32_t *free_state_out, int32_t *status, void *stream);
+
+/* Pages src[i] to dst[i], codes and exponents, whole, in each of the caches (HOST array, n_caches <= 65536, read before the
+ * call returns; all of one n_pages, Hkv, D and page).  An i whose src or dst is not in the cache is left out.  No page may
+ * be written twice or be both read and written (unspecified contents of those pages).  0 <= n <= 2^20.                    */
+int agq_kv_copy_pages(const agq_kv_cache *caches, int n_caches, const int32_t *src, const int32_t *dst, int64_t n, void *stream);
+
+/* Request b keeps its first stay[b] tokens (all of them if it has no more) and of the others those that are listed:
+ * keep[cu_keep[b]] .. keep[cu_keep[b+1] - 1], in ascending order, each at least stay[b] and below kv_len[b].  They move
+ * together: token i of the request is token i as before for i < stay[b], else keep[cu_keep[b] + i - stay[b]].  With no
+ * listed tokens the request is cut to its first stay[b]; with those all kept as well it stays as it is.
+ * Pages in front of stay[b] / page stay; where tokens are listed the pages from there on are new ones, else all remaining
+ * pages stay, but a partly filled last page that is shared and is now to be written into becomes a new one.  The old pages
+ * are let go.  moves [agq_kv_moves_ints(N, B, page)], 16-byte aligned: the new pages, for agq_kv_move; its contents are the library's.
+ * Keys keep the rotation of their old positions, while agq_kv_map counts a request's next position from its new length: a
+ * program that wants the old count adds the difference to pos.
+ * status -1 also for a stay below 0, cu_keep that descends or leaves 0 .. N, and listed tokens that are not as said.
+ * 0 <= N < 2^30.                                                                                                         */
+size_t agq_kv_moves_ints(int64_t N, int64_t B, int64_t page);
+int agq_kv_compact(const int32_t *kv_len, const int32_t *stay, const int32_t *cu_keep, const int32_t *keep, int64_t N, int64_t B,
+                   int64_t page, const int32_t *block_table, int64_t max_pages, const int32_t *shared, int32_t *free_ring,
+                   int64_t n_pages, const int32_t *free_state, int32_t *kv_len_out, int32_t *block_table_out,
+                   int32_t *shared_out, int32_t *moves, int32_t *free_state_out, int32_t *status, void *stream);
+
+/* The tokens of agq_kv_compact's new pages, in each of the caches (as in agq_kv_copy_pages), from the pages that held them:
+ * block_table, stay, cu_keep and keep are those that agq_kv_compact was given.  It comes before anything else is written
+ * into the cache, as the old pages are free by then.  A new page's exponent is the largest of its tokens' old ones; codes of
+ * the others are divided by what it grew by, halves to the even code.  Entries of a new page behind its tokens are 0.      */
+int agq_kv_move(const agq_kv_cache *caches, int n_caches, const int32_t *moves, const int32_t *block_table, int64_t max_pages,
+                const int32_t *stay, const int32_t *cu_keep, const int32_t *keep, int64_t N, int64_t B, void *stream);
+
+/* ---- What a model answers: log probabilities of given tokens, entropy, and the likeliest tokens of each row of logits.
+ *   p[t,:] = softmax(scale * x[t,:]),   logprob[t] = log p[t, tokens[t]],   entropy[t] = - sum_v p log p,
+ *   top_idx[t, 0..n_top-1] = the tokens with the largest x[t,v], equal ones by their index, top_logprob their log p.
+ * logits: [T, V], fp16 or float32 (kind), ld >= V elements between rows, aligned to its type; agq_gemm_w4a8's output is such
+ * a tensor.  tokens int32 [T]; a token outside 0 .. V - 1 (no token is given) has logprob NaN.  scale: 1 / temperature.
+ * logprob, entropy float32 [T]; top_idx int32, top_logprob float32 [T, n_top] contiguous.  tokens and logprob, entropy, and
+ * both of top_* (n_top == 0 then) may be NULL.
+ * Logits of -infinity are tokens that are ruled out: p = 0, log p = -infinity, 0 in the entropy; as alternatives they come
+ * last.  A row without a distribution (a NaN or +infinity among its logits, or -infinity only) has NaN for logprob, entropy
+ * and top_logprob, and -1 for top_idx.
+ * 1 <= V <= 2^24, 0 <= T <= 2^22, 0 <= n_top <= min(V, AGQ_MAX_TOP), 2^-24 <= scale <= 2^24, ld <= 2^30; float32 logits times
+ * scale have to be finite.  workspace: agq_logprobs_workspace_bytes, 16-byte aligned; contents are scratch.
+ * Exponents, sums and results are float32, the sums of a row in a fixed order: a result's error is about 2^-22 of the largest
+ * difference of scaled logits that counts in it.                                                                          */
+enum agq_logit_kind { AGQ_LOGITS_F16 = 0, AGQ_LOGITS_F32 = 1 };
+#define AGQ_MAX_TOP 64
+size_t agq_logprobs_workspace_bytes(int64_t T, int64_t V, int kind, int64_t n_top);
+int agq_logprobs(const void *logits, int kind, int64_t T, int64_t V, int64_t ld, float scale, const int32_t *tokens,
+                 int64_t n_top, float *logprob, float *entropy, int32_t *top_idx, float *top_logprob, void *workspace,
+                 size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -141,3 +141,182 @@ def attention(q, k, v, past, causal=True, scale=None, there=None, offset=None):
             bound[i] = (2.0 ** -11 + 2 * rel + 2 * (len(kk) + 64) * 2.0 ** -24) * A + len(kk) * 2.0 ** -35 * np.abs(vv).max(0) / total \
                 + 2.0 ** -11 * np.abs(o[i]) + 2.0 ** -25
     return o, bound
+
+
+# ------------------------------------------------------------------ normalised heads
+
+def norm_rotate(x, g, eps, pos=None, cos=None, sin=None):
+    """fp16 [T, H, D] divided by each head's root mean square, times g ([D] or [H, D]; None: as it is), and rotated as in
+    rotate() if there are tables: float64, rounded once"""
+    y = x.astype(np.float64)
+    if g is not None:
+        with np.errstate(invalid="ignore", divide="ignore"):
+            y = y / np.sqrt((y * y).mean(-1, keepdims=True) + eps) * g.astype(np.float64)
+    if cos is not None:
+        p = np.clip(pos, 0, cos.shape[0] - 1)
+        c, s = cos[p][:, None, :].astype(np.float64), sin[p][:, None, :].astype(np.float64)
+        lo, hi = np.split(y, 2, -1)
+        y = np.concatenate([lo * c - hi * s, hi * c + lo * s], -1)
+    with np.errstate(over="ignore"):
+        return y.astype(np.float16)
+
+
+# ------------------------------------------------------------------ shared pages, forks, compactions
+
+def _give_back(shared, ring, head, count, took):
+    back = [p for p in range(len(shared)) if shared[p] < 0]
+    for i, p in enumerate(back):
+        ring[(head + count + i) % len(ring)] = p
+        shared[p] = 0
+    return [(head + took) % len(ring), count - took + len(back)]
+
+
+def kv_fork(kv_len, parent, page, table, shared, ring, state, table_out):
+    """(kv_len, table, shared, copy_src, copy_dst, ring, state, status) after the requests went on as copies of others"""
+    kv_len, parent, table, ring = [int(x) for x in kv_len], [int(x) for x in parent], np.array(table), np.array(ring)
+    shared, out = np.maximum(np.array(shared), 0), np.array(table_out)
+    B, (head, count), n_pages = len(kv_len), (int(x) for x in state), len(ring)
+    up = lambda n: -(-n // page)
+    cap = table.shape[1] * page
+    wrong = not (0 <= head < n_pages and 0 <= count <= n_pages) or any(p < -1 or p >= B for p in parent) or any(n < 0 or n > cap for n in kv_len)
+
+    def refused(status):
+        for b in range(B):
+            n = min(up(max(kv_len[b], 0)), table.shape[1])
+            out[b, :n] = table[b, :n]
+        return kv_len, out, shared, [-1] * B, [-1] * B, ring, [head, count], status
+    if wrong:
+        return refused(-1)
+    there = lambda p: 0 <= p < n_pages
+    joint = lambda b: there(table[b, up(kv_len[b]) - 1]) and shared[table[b, up(kv_len[b]) - 1]] > 0
+    copies, first = [], set()
+    for b, p in enumerate(parent):
+        if p >= 0 and kv_len[p] % page and (p in first or joint(p)):
+            copies.append(b)
+        first.add(p)
+    if len(copies) > count:
+        return refused(len(copies) - count)
+    src, dst, holders = [-1] * B, [-1] * B, np.zeros(n_pages, dtype=np.int64)
+    for b in range(B):
+        for p in table[b, :up(kv_len[b])]:
+            if there(p):
+                holders[p] -= 1
+    for b, p in enumerate(parent):
+        if p < 0:
+            continue
+        n = up(kv_len[p])
+        out[b, :n] = table[p, :n]
+        if b in copies:
+            src[b], dst[b] = int(table[p, n - 1]), int(ring[(head + copies.index(b)) % n_pages])
+            out[b, n - 1] = dst[b]
+        for q in table[p, :n - 1 if b in copies else n]:
+            if there(q):
+                holders[q] += 1
+    shared = shared + holders
+    state = _give_back(shared, ring, head, count, len(copies))
+    return [kv_len[p] if p >= 0 else 0 for p in parent], out, shared, src, dst, ring, state, 0
+
+
+def kv_compact(kv_len, stay, cu, keep, page, table, shared, ring, state, table_out):
+    """(kv_len, table, shared, ring, state, status, moves) after the requests lost tokens; moves: (new page, the tokens that it
+    gets as (page, slot) pairs)"""
+    kv_len, stay, cu, keep = ([int(x) for x in a] for a in (kv_len, stay, cu, keep))
+    table, ring, shared, out = np.array(table), np.array(ring), np.maximum(np.array(shared), 0), np.array(table_out)
+    B, (head, count), n_pages, cap = len(kv_len), (int(x) for x in state), len(ring), table.shape[1] * page
+    up = lambda n: -(-n // page)
+
+    def refused(status):
+        for b in range(B):
+            n = min(up(max(kv_len[b], 0)), table.shape[1])
+            out[b, :n] = table[b, :n]
+        return kv_len, out, shared, ring, [head, count], status, []
+    wrong = not (0 <= head < n_pages and 0 <= count <= n_pages) or any(n < 0 or n > cap for n in kv_len) or any(s < 0 for s in stay)
+    wrong = wrong or any(not 0 <= a <= b <= len(keep) for a, b in zip(cu, cu[1:]))
+    if not wrong:
+        for b in range(B):
+            mine = keep[cu[b]:cu[b + 1]]
+            wrong = wrong or any(x < stay[b] or x >= kv_len[b] for x in mine) or any(x >= y for x, y in zip(mine, mine[1:]))
+    if wrong:
+        return refused(-1)
+    plan, need = [], 0
+    for b in range(B):
+        tokens = list(range(min(stay[b], kv_len[b]))) + keep[cu[b]:cu[b + 1]]
+        n, some = len(tokens), cu[b + 1] > cu[b]
+        same = stay[b] // page if some else up(n)
+        if not some and n < kv_len[b] and n % page:
+            last = table[b, up(n) - 1]
+            same -= bool(0 <= last < n_pages and shared[last] > 0)
+        plan.append((tokens, same))
+        need += up(n) - same
+    if need > count:
+        return refused(need - count)
+    took, moves, held = 0, [], np.zeros(n_pages, dtype=np.int64)
+    for b, (tokens, same) in enumerate(plan):
+        out[b, :same] = table[b, :same]
+        for j in range(same, up(len(tokens))):
+            new = int(ring[(head + took) % n_pages])
+            out[b, j] = new
+            took += 1
+            moves.append((new, [(int(table[b, i // page]), i % page) for i in tokens[j * page:(j + 1) * page]]))
+        for p in table[b, same:up(kv_len[b])]:
+            if 0 <= p < n_pages:
+                held[p] -= 1
+    shared = shared + held
+    state = _give_back(shared, ring, head, count, took)
+    return [len(t) for t, _ in plan], out, shared, ring, state, 0, moves
+
+
+def kv_move(codes, exps, moves, transposed):
+    """the codes and exponents of one layer (keys, or values: transposed) after kv_compact's moves; new arrays"""
+    old = codes.transpose(0, 1, 3, 2) if transposed else codes
+    codes, new_exps = codes.copy(), exps.copy()
+    view = codes.transpose(0, 1, 3, 2) if transposed else codes
+    for to, tokens in moves:
+        for h in range(old.shape[1]):
+            e = max(int(exps[p, h]) for p, _ in tokens)
+            view[to, h] = 0
+            for i, (p, slot) in enumerate(tokens):
+                view[to, h, i] = np.rint(old[p, h, slot].astype(np.float64) * 2.0 ** (int(exps[p, h]) - e))
+            new_exps[to, h] = e
+    return codes, new_exps
+
+
+# ------------------------------------------------------------------ log probabilities
+
+def logprobs(x, tokens, n_top, scale=1.0):
+    """Rows of logits x [T, V] (fp16 or float32): dict of logprob, entropy, top_idx, top_logprob in float64, and of bounds on
+    what float32 arithmetic may be off, in units of d = 2^-24, to first order:
+      z = (x - m) c, c = scale log2(e): a difference, a product, c's two roundings: 4 d |z|
+      2^z: ln 2 times that, and the exponential's own 2 d, relative
+      S, E: sums of V terms in up to V / 256 + 64 steps in a row
+      log2 S: 2 d of itself, and S's relative error over ln 2; differences, products and factors: d or two of the result"""
+    T, V = x.shape
+    d, ln2, steps = 2.0 ** -24, np.log(2.0), V / 256 + 64
+    r = dict(logprob=np.full(T, np.nan), entropy=np.full(T, np.nan), top_idx=np.full((T, n_top), -1, dtype=np.int64),
+             top_logprob=np.full((T, n_top), np.nan), logprob_bound=np.zeros(T), entropy_bound=np.zeros(T), top_bound=np.zeros((T, n_top)))
+    for t in range(T):
+        y = x[t].astype(np.float64)
+        if np.isnan(y).any() or y.max() == np.inf or y.max() == -np.inf:
+            continue
+        with np.errstate(invalid="ignore"):
+            z = (y - y.max()) * float(scale)
+            w = np.exp(z)
+            lse = np.log1p(w.sum() - 1.0) if w.sum() < 1.5 else np.log(w.sum())
+            p = w / w.sum()
+            lp = z - lse
+            size = np.where(p > 0, p * np.abs(z), 0.0).sum()
+            square = np.where(p > 0, p * z * z, 0.0).sum()
+        S = 4 * size + 2 + steps                                                        # relative error of S over d
+        log_err = S + 2 * abs(lse)
+        at = lambda v: d * (4 * np.abs(v) + log_err + 4 * np.abs(v - lse)) + 2.0 ** -149
+        r["entropy"][t] = -(p[p > 0] * lp[p > 0]).sum()
+        r["entropy_bound"][t] = d * (log_err + 4 * square + (steps + 8 + S) * size + 4 * (abs(lse) + size))
+        tok = -1 if tokens is None else int(tokens[t])
+        if 0 <= tok < V:
+            r["logprob"][t] = lp[tok]
+            r["logprob_bound"][t] = 0 if np.isinf(z[tok]) else at(z[tok])
+        order = np.argsort(-(y + 0.0), kind="stable")[:n_top]
+        r["top_idx"][t], r["top_logprob"][t] = order, lp[order]
+        fin = np.isfinite(z[order])
+        r["top_bound"][t, fin] = at(z[order][fin])
+    return r

@@ -69,6 +69,17 @@ SIGNATURES = {
                                _i64, _vp, _sz, _vp]),
     "agq_attn_kv_workspace_bytes": (_sz, [_i64] * 7),
     "agq_attn_kv": (_int, [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_float, _vp, _i64, _vp, _sz, _vp]),
+    "agq_kv_append_norm": (_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _i64, ctypes.c_double, _vp, _vp, _vp, _i64,
+                                  _vp, _i64, _vp, _i64, _vp]),
+    "agq_qk_norm_rope": (_int, [_vp, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _i64, _vp, _i64, ctypes.c_double, _vp, _vp, _vp, _i64, _vp, _i64,
+                                _vp, _i64, _vp]),
+    "agq_kv_fork": (_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "agq_kv_copy_pages": (_int, [_vp, _int, _vp, _vp, _i64, _vp]),
+    "agq_kv_moves_ints": (_sz, [_i64] * 3),
+    "agq_kv_compact": (_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "agq_kv_move": (_int, [_vp, _int, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _vp]),
+    "agq_logprobs_workspace_bytes": (_sz, [_i64, _i64, _int, _i64]),
+    "agq_logprobs": (_int, [_vp, _int, _i64, _i64, _i64, ctypes.c_float, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "agq_stack_forward": (_int, [_vp, _int, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
 }
 
@@ -597,6 +608,30 @@ def _ints(t, n, name):
     return t.data_ptr()
 
 
+def _rope(rope_cos, rope_sin, pos, T, D, used):
+    """(rows, pos, cos, sin) of the rotary tables, or none of them"""
+    if rope_cos is None and rope_sin is None and pos is None:
+        return 0, None, None, None
+    if rope_cos is None or rope_sin is None or pos is None:
+        raise ValueError("rope_cos, rope_sin and pos go together")
+    P = rope_cos.shape[0]
+    if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is _f32) \
+            or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
+        raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
+    used += pos, rope_cos, rope_sin
+    return P, _ints(pos, T, "pos"), rope_cos.data_ptr(), rope_sin.data_ptr()
+
+
+def _gain(g, H, D, name, used):
+    """(address, elements between heads) of gains [D] or [H, D]"""
+    if g is None:
+        return None, 0
+    if g.dtype is not _f16 or tuple(g.shape) not in ((D,), (H, D)) or g.stride(-1) != 1:
+        raise ValueError("%s: fp16 [%d] or [%d, %d] is wanted" % (name, D, H, D))
+    used.append(g)
+    return g.data_ptr(), (g.stride(0) if g.dim() == 2 and H > 1 else 0)
+
+
 def _kv_cache(k_cache, v_cache, k_exp, v_exp):
     """struct agq_kv_cache as bytes, key heads, D"""
     n_pages, Hkv, page, D = k_cache.shape
@@ -653,7 +688,7 @@ def kv_map(kv_len, n_new, block_table, page, free_ring, free_state, T, out: KvSt
     return out
 
 
-def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope_cos=None, rope_sin=None, q_out=None, k_out=None):
+def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope_cos=None, rope_sin=None, q_out=None, k_out=None, _norm=None):
     """agq_kv_append: a step's keys and values into the cache.  With rope tables (float32 [P, D/2]) and pos the keys, and
     the queries if given, are rotated first: returns (rotated q or None, rotated k), else (None, None)."""
     cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
@@ -672,6 +707,9 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
             raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
         pos_p, cos_p, sin_p = _ints(pos, T, "pos"), rope_cos.data_ptr(), rope_sin.data_ptr()
         used += pos, rope_cos, rope_sin
+    elif pos is not None or rope_sin is not None or (_norm is None and (q is not None or k_out is not None)):
+        raise ValueError("q, k_out, pos and rope_sin go with rope_cos")
+    if rope_cos is not None or _norm is not None:
         if k_out is None:
             k_out, ldko = k.new_empty(T, Hkv, D), Hkv * D
         else:
@@ -688,13 +726,222 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
                 ldqo = _like(q_out, (T, Hq, D), "q_out")
                 used.append(q_out)
             q_p, qo_p = q.data_ptr(), q_out.data_ptr()
-    elif q is not None or k_out is not None or pos is not None or rope_sin is not None:
-        raise ValueError("q, k_out, pos and rope_sin go with rope_cos")
     if q is None and q_out is not None:
         raise ValueError("q_out goes with q")
+    if _norm is not None:
+        g_k, g_q, eps = _norm
+        gk_p, ldgk = _gain(g_k, Hkv, D, "g_k", used)
+        gq_p, ldgq = _gain(g_q, Hq, D, "g_q", used)
+        _ok(lib().agq_kv_append_norm(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, _ints(slot, T, "slot"), q_p, ldq, Hq, gq_p, ldgq, gk_p, ldgk, eps,
+                                     pos_p, cos_p, sin_p, P, qo_p, ldqo, ko_p, ldko, _stream_of(*used)), "agq_kv_append_norm")
+        return q_out, k_out
     _ok(lib().agq_kv_append(cache, k.data_ptr(), ldk, v.data_ptr(), ldv, T, _ints(slot, T, "slot"), q_p, ldq, Hq, pos_p, cos_p, sin_p, P, qo_p,
                             ldqo, ko_p, ldko, _stream_of(*used)), "agq_kv_append")
     return q_out, k_out
+
+
+def kv_append_norm(k, v, slot, k_cache, v_cache, k_exp, v_exp, g_k, eps, q=None, g_q=None, pos=None, rope_cos=None, rope_sin=None, q_out=None,
+                   k_out=None):
+    """agq_kv_append_norm: kv_append with keys (and queries) normalised per head first; gains fp16 [D] or [heads, D].
+    Returns (q or None, k) as they are after norm and rotation."""
+    if g_k is None or (q is None) != (g_q is None):
+        raise ValueError("g_k, and g_q if q is given, are wanted")
+    return kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q, pos, rope_cos, rope_sin, q_out, k_out, (g_k, g_q, eps))
+
+
+def qk_norm_rope(q, k, g_q=None, g_k=None, eps=1e-6, pos=None, rope_cos=None, rope_sin=None, q_out=None, k_out=None):
+    """agq_qk_norm_rope: q fp16 [T, Hq, D] and k [T, Hkv, D] (either may be None) normalised per head by gains fp16 [D] or
+    [heads, D] (None: not normalised) and rotated (without tables: not rotated).  Returns (q, k) as they are then."""
+    if q is None and k is None:
+        raise ValueError("q or k is wanted")
+    T, _, D = (k if q is None else q).shape
+    used, half = [], []
+    for x, g, out, name in ((q, g_q, q_out, "q"), (k, g_k, k_out, "k")):
+        if x is None:
+            if g is not None or out is not None:
+                raise ValueError("g_%s and %s_out go with %s" % (name, name, name))
+            half.append((None, 0, 0, None, 0, None, 0, None))
+            continue
+        H = x.shape[1]
+        ld = _like(x, (T, H, D), name)
+        used.append(x)
+        if out is None:
+            out, ldo = x.new_empty(T, H, D), H * D
+        else:
+            ldo = _like(out, (T, H, D), name + "_out")
+            used.append(out)
+        g_p, ldg = _gain(g, H, D, "g_" + name, used)
+        half.append((x.data_ptr(), ld, H, g_p, ldg, out.data_ptr(), ldo, out))
+    P, pos_p, cos_p, sin_p = _rope(rope_cos, rope_sin, pos, T, D, used)
+    (q_p, ldq, Hq, gq_p, ldgq, qo_p, ldqo, q_out), (k_p, ldk, Hkv, gk_p, ldgk, ko_p, ldko, k_out) = half
+    _ok(lib().agq_qk_norm_rope(q_p, ldq, Hq, k_p, ldk, Hkv, T, D, gq_p, ldgq, gk_p, ldgk, eps, pos_p, cos_p, sin_p, P, qo_p, ldqo, ko_p, ldko,
+                               _stream_of(*used)), "agq_qk_norm_rope")
+    return q_out, k_out
+
+
+class KvLayers:
+    """The caches of a model's layers as agq_kv_copy_pages and agq_kv_move take them: their addresses, checked and written
+    down once; it keeps the tensors alive."""
+
+    def __init__(self, caches):
+        shapes = {tuple(t.shape for t in c) for c in caches}
+        if len(shapes) > 1:
+            raise ValueError("caches of one shape are wanted")
+        self.tensors = [t for c in caches for t in c]
+        self.n, self.packed = len(caches), b"".join(_kv_cache(*c)[0] for c in caches)
+        devices = {*map(_device_of, self.tensors)}
+        if len(devices) > 1:
+            raise ValueError("caches on one GPU are wanted")
+        self.some = self.tensors[:1]                  # a tensor that says which GPU they are on
+
+
+def kv_layers(caches) -> KvLayers:
+    """caches: [(k_cache, v_cache, k_exp, v_exp), ...], one of each layer"""
+    return KvLayers([tuple(c) for c in caches])
+
+
+class KvFork(NamedTuple):
+    """What kv_fork says (device int32 tensors): lengths [B], table [B, max_pages], further holders of each page [n_pages],
+    the pages to be copied [B] and where to [B], the ring's state [2], and the status [1]."""
+    kv_len: torch.Tensor
+    block_table: torch.Tensor
+    shared: torch.Tensor
+    copy_src: torch.Tensor
+    copy_dst: torch.Tensor
+    free_state: torch.Tensor
+    status: torch.Tensor
+
+
+class KvCompact(NamedTuple):
+    """What kv_compact says (device int32 tensors): lengths [B], table [B, max_pages], further holders of each page [n_pages],
+    what kv_move has to do [kv_moves_ints], the ring's state [2], and the status [1]."""
+    kv_len: torch.Tensor
+    block_table: torch.Tensor
+    shared: torch.Tensor
+    moves: torch.Tensor
+    free_state: torch.Tensor
+    status: torch.Tensor
+
+
+def _new_step(kind, kv_len, B, max_pages, n_pages, sizes):
+    """(a step's tensors, their addresses) in two allocations: the table, and the others"""
+    table = kv_len.new_empty(B, max_pages)
+    buf = kv_len.new_empty(sum(sizes))
+    parts = buf.split_with_sizes(sizes)
+    at = [t.data_ptr() for t in parts]
+    return kind._make((parts[0], table, *parts[1:])), (at[0], table.data_ptr(), *at[1:])
+
+
+def _given_step(out, sizes):
+    return [_ints(t, n, "out." + name) for t, n, name in zip(out, sizes, out._fields)]
+
+
+def kv_fork(kv_len, parent, block_table, page, shared, free_ring, free_state, out: KvFork | None = None) -> KvFork:
+    """agq_kv_fork: request b becomes a copy of what request parent[b] is (-1: nothing).  block_table [B, max_pages], shared
+    and free_ring [n_pages] (the ring is updated).  kv_copy_pages(layers, copy_src, copy_dst) comes next.
+    out: a KvFork to write into (not the tensors that are passed in: a loop swaps two of each)."""
+    B, max_pages = block_table.shape
+    n_pages = free_ring.numel()
+    st = _stream_of(kv_len, parent, block_table, shared, free_ring, free_state, *(out or ()))
+    if out is None:
+        out, to = _new_step(KvFork, kv_len, B, max_pages, n_pages, [B, n_pages, B, B, 2, 1])
+    else:
+        to = _given_step(out, (B, B * max_pages, n_pages, B, B, 2, 1))
+    _ok(lib().agq_kv_fork(_ints(kv_len, B, "kv_len"), _ints(parent, B, "parent"), B, page, _ints(block_table, B * max_pages, "block_table"), max_pages,
+                          _ints(shared, n_pages, "shared"), _ints(free_ring, n_pages, "free_ring"), n_pages, _ints(free_state, 2, "free_state"),
+                          *to, st), "agq_kv_fork")
+    return out
+
+
+def kv_copy_pages(layers: KvLayers, src, dst):
+    """agq_kv_copy_pages: pages src[i] to dst[i] (int32) in the caches of all layers; an i that is not in the cache is left out."""
+    n = src.numel()
+    _ok(lib().agq_kv_copy_pages(layers.packed, layers.n, _ints(src, n, "src"), _ints(dst, n, "dst"), n, _stream_of(src, dst, *layers.some)),
+        "agq_kv_copy_pages")
+
+
+def kv_moves_ints(N, B, page) -> int:
+    return lib().agq_kv_moves_ints(N, B, page)
+
+
+def kv_compact(kv_len, stay, cu_keep, keep, block_table, page, shared, free_ring, free_state, out: KvCompact | None = None) -> KvCompact:
+    """agq_kv_compact: request b keeps its first stay[b] tokens and of the others keep[cu_keep[b]:cu_keep[b+1]].  kv_move(layers,
+    moves, block_table, stay, cu_keep, keep) comes next, with the tensors that were passed in here.  out: as for kv_fork."""
+    B, max_pages = block_table.shape
+    n_pages, N = free_ring.numel(), keep.numel()
+    st = _stream_of(kv_len, stay, cu_keep, keep, block_table, shared, free_ring, free_state, *(out or ()))
+    n_moves = lib().agq_kv_moves_ints(N, B, page)
+    if out is None:                                   # the moves first: they are 16-byte aligned
+        buf = kv_len.new_empty(n_moves + B + n_pages + 3)
+        moves, lens, held, state, status = buf.split_with_sizes([n_moves, B, n_pages, 2, 1])
+        out = KvCompact(lens, kv_len.new_empty(B, max_pages), held, moves, state, status)
+        p = buf.data_ptr()
+        q = p + 4 * n_moves
+        r = q + 4 * (B + n_pages)
+        to = (q, out.block_table.data_ptr(), q + 4 * B, p, r, r + 8)
+    else:
+        to = _given_step(out, (B, B * max_pages, n_pages, n_moves, 2, 1))
+    _ok(lib().agq_kv_compact(_ints(kv_len, B, "kv_len"), _ints(stay, B, "stay"), _ints(cu_keep, B + 1, "cu_keep"), _ints(keep, N, "keep"), N, B, page,
+                             _ints(block_table, B * max_pages, "block_table"), max_pages, _ints(shared, n_pages, "shared"),
+                             _ints(free_ring, n_pages, "free_ring"), n_pages, _ints(free_state, 2, "free_state"), *to, st), "agq_kv_compact")
+    return out
+
+
+def kv_move(layers: KvLayers, moves, block_table, stay, cu_keep, keep):
+    """agq_kv_move: what kv_compact decided, in the caches of all layers; block_table is the one that kv_compact was given."""
+    B, max_pages = block_table.shape
+    N = keep.numel()
+    page = layers.tensors[0].shape[2] if layers.n else 16
+    _ok(lib().agq_kv_move(layers.packed, layers.n, _ints(moves, lib().agq_kv_moves_ints(N, B, page), "moves"),
+                          _ints(block_table, B * max_pages, "block_table"), max_pages, _ints(stay, B, "stay"), _ints(cu_keep, B + 1, "cu_keep"),
+                          _ints(keep, N, "keep"), N, B, _stream_of(moves, block_table, stay, cu_keep, keep, *layers.some)), "agq_kv_move")
+
+
+class Logprobs(NamedTuple):
+    """What logprobs says: log probabilities of the given tokens [T] and entropies [T] (float32; None where not asked for), the
+    likeliest tokens [T, n_top] (int32) and their log probabilities (float32; None if n_top is 0)."""
+    logprob: torch.Tensor | None
+    entropy: torch.Tensor | None
+    top_idx: torch.Tensor | None
+    top_logprob: torch.Tensor | None
+
+
+AGQ_LOGITS_F16, AGQ_LOGITS_F32, AGQ_MAX_TOP = 0, 1, 64
+
+
+def logprobs_workspace_bytes(T, V, kind, n_top) -> int:
+    return lib().agq_logprobs_workspace_bytes(T, V, kind, n_top)
+
+
+def logprobs(logits, tokens=None, n_top=0, scale=1.0, want_entropy=True, out: Logprobs | None = None, workspace=None) -> Logprobs:
+    """agq_logprobs: logits fp16 or float32 [T, V] (rows any distance apart), tokens int32 [T] or None.  out: a Logprobs to
+    write into, with tensors where a result is asked for."""
+    T, V = logits.shape
+    ld, one = logits.stride()
+    kind = AGQ_LOGITS_F16 if logits.dtype is _f16 else AGQ_LOGITS_F32
+    if (kind == AGQ_LOGITS_F32 and logits.dtype is not _f32) or (T and V > 1 and one != 1):
+        raise ValueError("logits: fp16 or float32 [T, V] with contiguous rows is wanted")
+    if T <= 1:
+        ld = V
+    if out is None:
+        e = logits.new_empty
+        out = Logprobs(None if tokens is None else e(T, dtype=_f32), e(T, dtype=_f32) if want_entropy else None,
+                       e(T, n_top, dtype=_i32) if n_top else None, e(T, n_top, dtype=_f32) if n_top else None)
+    elif (out[0] is None) != (tokens is None) or (out[1] is None) == bool(want_entropy) or (out[2] is None) != (not n_top) or (out[3] is None) != (not n_top):
+        raise ValueError("out: a tensor for each result that is asked for is wanted")
+    else:
+        for t, shape, dtype, name in zip(out, ((T,), (T,), (T, n_top), (T, n_top)), (_f32, _f32, _i32, _f32), Logprobs._fields):
+            if t is not None and (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()):
+                raise ValueError("out.%s: a contiguous %s tensor %s is wanted" % (name, dtype, list(shape)))
+    st = _stream_of(*[t for t in (logits, tokens, *out) if t is not None])
+    if workspace is None:
+        need = lib().agq_logprobs_workspace_bytes(T, V, kind, n_top)
+        workspace = logits.new_empty(need, dtype=_i8) if need else None
+    else:
+        _given(workspace, logits)
+    _ok(lib().agq_logprobs(logits.data_ptr(), kind, T, V, ld, scale, None if tokens is None else _ints(tokens, T, "tokens"), n_top, _ptr(out[0]),
+                           _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(workspace), 0 if workspace is None else workspace.nbytes, st), "agq_logprobs")
+    return out
 
 
 def attn_packed_workspace_bytes(Tq, Hq, Tk, Hkv, D, B) -> int:

@@ -381,6 +381,17 @@ struct AgqKvAppend {
     int64_t ldq, ldk, ldv, ldqo, ldko, T, Hq, P;
     const int32_t *pos, *slot;
     const float *rope_cos, *rope_sin;
+    const void *g_q, *g_k;       // gains of normalised heads, or NULL (g_k) where they are not normalised
+    int64_t ldgq, ldgk;
+    double eps;
+};
+struct AgqQkNormRope {
+    const void *q, *k, *g_q, *g_k;
+    void *q_out, *k_out;
+    int64_t ldq, ldk, ldgq, ldgk, ldqo, ldko, T, Hq, Hkv, D, P;
+    const int32_t *pos;
+    const float *rope_cos, *rope_sin;
+    double eps;
 };
 struct AgqAttnPacked {
     const void *q, *k, *v;
@@ -459,6 +470,43 @@ int agq_launch_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, in
                       int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T, int32_t *kv_len_out, int32_t *cu_new,
                       int32_t *pos, int32_t *slot, int32_t *free_state_out, int32_t *status, void *stream);
 int agq_launch_kv_append(const AgqKvAppend &p, void *stream);
+int agq_launch_qk_norm_rope(const AgqQkNormRope &p, void *stream);
+
+// ---- shared pages, forks and compactions (agq_kv_pages.hip)
+struct AgqKvPages {
+    const int32_t *kv_len, *table, *shared, *free_in;
+    int32_t *ring, *kv_len_out, *table_out, *shared_out, *free_out, *status;
+    int64_t B, page, max_pages, n_pages;
+};
+struct AgqKvShape {
+    int64_t n_pages, Hkv, D, page;
+};
+struct AgqKvLayer {
+    int8_t *k, *v, *k_exp, *v_exp;
+};
+#define AGQ_KV_LAYERS 64         // layers of a launch
+#define AGQ_KV_CHECKS 256        // workgroups that check the listed tokens, a word each
+// New pages of a compaction with N listed tokens, at most: a request's first n listed tokens fill n / page of them, the tokens
+// in front of them in the first one and those behind in the last one two more.
+static inline int64_t agq_kv_new_pages(int64_t N, int64_t B, int64_t page) { return N / page + 2 * B; }
+int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy_src, int32_t *copy_dst, void *stream);
+int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int32_t *moves, void *stream);
+int agq_launch_kv_copy_pages(const AgqKvShape &s, const AgqKvLayer *layers, int n_layers, const int32_t *src, const int32_t *dst, int64_t n,
+                             void *stream);
+int agq_launch_kv_move(const AgqKvShape &s, const AgqKvLayer *layers, int n_layers, const int32_t *moves, const int32_t *table, int64_t max_pages,
+                       const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int64_t B, void *stream);
+
+// ---- log probabilities (agq_logprobs.hip)
+struct AgqLogprobs {
+    const void *logits;
+    int kind;
+    int64_t T, V, ld, n_top;
+    float scale;
+    const int32_t *tokens;
+    float *logprob, *entropy, *top_logprob;
+    int32_t *top_idx;
+};
+int agq_launch_logprobs(const AgqLogprobs &p, void *workspace, void *stream);
 // Tiles of 128 queries of B sequences with Tq queries in all: the sum of ceil(n / 128) is not more.  (Workgroups that find no tile
 // take turns with the others in the order in which CUs get them: one spare tile for a single one left half of the CUs without
 // work, 128 queries and 4128 keys of 32 heads 29.8 us.)

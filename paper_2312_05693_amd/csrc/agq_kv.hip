@@ -173,6 +173,10 @@ struct AppendArgs {
     const float *cos_t, *sin_t;
     int8_t *kc, *vc, *ke, *ve;
     int T, Hq, Hkv, D, D_log2, P, page, page_log2, n_pages, chunk, chunks;
+    // normalised heads: gains [D] of head h at g + h * ldg
+    const uint16_t *g_q, *g_k;
+    int64_t ldgq, ldgk;
+    double eps;
 };
 constexpr int kEZero = -30;      // the smallest exponent that a nonzero fp16 value asks for; pages of zeros get it too
 
@@ -206,6 +210,39 @@ __device__ __forceinline__ void rotate8(Half8 &lo, Half8 &hi, const float *cos_t
         hi.v[i] = d2h_odd(h * c + l * s);
     }
 }
+// Eight pairs of a head divided by the head's root mean square, times their gains, and turned (cos_t NULL: not turned), in
+// float64 from fp16 to fp16.  The head's other pairs are the neighbouring lanes' (2^per_log2 of them, all active): their
+// squares are summed across them in pairs, so every lane has the same sum whatever its place.
+__device__ __forceinline__ void norm_rotate8(Half8 &lo, Half8 &hi, const uint16_t *gain, int Dh, int per_log2, double eps, const float *cos_t,
+                                             const float *sin_t) {
+    double l[8], h[8], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        l[i] = h2d(lo.v[i]), h[i] = h2d(hi.v[i]);
+        sum = fma(l[i], l[i], sum);
+        sum = fma(h[i], h[i], sum);
+    }
+    for (int m = 1; m < 1 << per_log2; m <<= 1) sum += __shfl_xor(sum, m);
+    const double inv = 1.0 / sqrt(sum * (Dh == 64 ? 1.0 / 128 : 1.0 / 64) + eps);
+    const Half8 gl = load8(gain), gh = load8(gain + Dh);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l[i] *= h2d(gl.v[i]) * inv, h[i] *= h2d(gh.v[i]) * inv;
+    if (cos_t == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lo.v[i] = d2h_odd(l[i]), hi.v[i] = d2h_odd(h[i]);
+        return;
+    }
+    const float4 c0 = reinterpret_cast<const float4 *>(cos_t)[0], c1 = reinterpret_cast<const float4 *>(cos_t)[1];
+    const float4 s0 = reinterpret_cast<const float4 *>(sin_t)[0], s1 = reinterpret_cast<const float4 *>(sin_t)[1];
+    const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+    const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const double c = (double)cs[i], s = (double)sn[i];
+        lo.v[i] = d2h_odd(l[i] * c - h[i] * s);
+        hi.v[i] = d2h_odd(h[i] * c + l[i] * s);
+    }
+}
 // the largest magnitude of eight fp16 values, as bits; NaN does not count
 __device__ __forceinline__ uint32_t top8(const Half8 &h) {
     uint32_t m = 0;
@@ -228,7 +265,7 @@ __device__ __forceinline__ uint32_t coarser4(uint32_t w, float down) {
 // One run: n tokens from t on into the page `id`, its entries off .. off + n - 1, keys (role 2 h) or values (2 h + 1) of head h.
 // ALONE: a few tokens, by one wavefront, which has at most one work item per lane; else by the whole workgroup, and the
 // fp16 values wait in LDS for the scale.  A work item is eight pairs of a key, or eight of a value.
-template <bool ALONE>
+template <bool ALONE, bool NORM>
 __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t, int n, int64_t id, int off, int tid, int threads, uint16_t *held) {
     const bool values = role & 1;
     const int head = role >> 1, Dh = a.D >> 1, per_log2 = a.D_log2 - (values ? 3 : 4), items = n << per_log2, lane = tid & 63;
@@ -245,10 +282,11 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
         lo = load8(src + i * ld + j);
         if (!values) {
             hi = load8(src + i * ld + j + Dh);
-            if (a.cos_t) {
-                const int64_t p = min(max(a.pos[t + i], 0), a.P - 1);
+            const int64_t p = a.cos_t ? min(max(a.pos[t + i], 0), a.P - 1) : 0;
+            if constexpr (NORM)
+                norm_rotate8(lo, hi, a.g_k + head * a.ldgk + j, Dh, per_log2, a.eps, a.cos_t ? a.cos_t + p * Dh + j : nullptr, a.sin_t + p * Dh + j);
+            else if (a.cos_t)
                 rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
-            }
             if (a.k_out) {
                 uint16_t *dst = a.k_out + (int64_t)(t + i) * a.ldko + head * a.D + j;
                 store8(dst, lo);
@@ -320,14 +358,15 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
 // ROLES = 1: a workgroup takes the runs that begin in its chunk of tokens, for one role (the keys or the values of a head).
 // ROLES = 4: one token and four roles to a workgroup.  A short run, as in a generation step, is that of its first token's
 // workgroup, whose wavefronts have a role each; a long one is shared by the workgroups of its first four tokens, a role each.
-template <int ROLES>
+// NORM: queries and keys are normalised before their rotation.
+template <int ROLES, bool NORM>
 __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint16_t held[];      // [run][D], then one word per wavefront
     const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int slots = a.n_pages << a.page_log2, roles = 2 * a.Hkv, groups = (roles + ROLES - 1) / ROLES;
     const unsigned kv_groups = a.chunks * groups;
-    if (blockIdx.x >= kv_groups) {                                       // queries: rotation only
+    if (blockIdx.x >= kv_groups) {                                       // queries: nothing to store but themselves
         const int per_log2 = a.D_log2 - 4, Dh = a.D >> 1;
         const unsigned item = (blockIdx.x - kv_groups) * threads + tid, th = item >> per_log2;   // below 2^31 (the caller's check)
         const int t = (int)(th / (unsigned)a.Hq), h = (int)th - t * a.Hq, j = (int)(item & ((1u << per_log2) - 1)) * 8;
@@ -335,8 +374,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
         const uint16_t *src = a.q + (int64_t)t * a.ldq + h * a.D + j;
         uint16_t *dst = a.q_out + (int64_t)t * a.ldqo + h * a.D + j;
         Half8 lo = load8(src), hi = load8(src + Dh);
-        const int64_t p = min(max(a.pos[t], 0), a.P - 1);
-        rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
+        const int64_t p = NORM && !a.cos_t ? 0 : min(max(a.pos[t], 0), a.P - 1);
+        if constexpr (NORM)
+            norm_rotate8(lo, hi, a.g_q + h * a.ldgq + j, Dh, per_log2, a.eps, a.cos_t ? a.cos_t + p * Dh + j : nullptr, a.sin_t + p * Dh + j);
+        else
+            rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
         store8(dst, lo);
         store8(dst + Dh, hi);
         return;
@@ -362,9 +404,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
         const int t = c0 - before, role = role0 + (n << (a.D_log2 - 3) <= 64 ? wave : before);
         if (role >= roles) return;
         if (n << (a.D_log2 - 3) <= 64) {
-            if (before == 0) append_run<true>(a, role, t, n, id, off, lane, 64, held);
+            if (before == 0) append_run<true, NORM>(a, role, t, n, id, off, lane, 64, held);
         } else {
-            append_run<false>(a, role, t, n, id, off - before, tid, threads, held);
+            append_run<false, NORM>(a, role, t, n, id, off - before, tid, threads, held);
         }
         return;
     }
@@ -403,12 +445,47 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
             n += 64;
         }
         if (n << (a.D_log2 - 3) <= 64) {
-            if (wave == 0) append_run<true>(a, role0, t, n, id, off, lane, 64, held);
+            if (wave == 0) append_run<true, NORM>(a, role0, t, n, id, off, lane, 64, held);
         } else {
-            append_run<false>(a, role0, t, n, id, off, tid, threads, held);
+            append_run<false, NORM>(a, role0, t, n, id, off, tid, threads, held);
         }
         t += n;
     }
+}
+
+// ---------------------------------------------------------------- normalised and rotated heads, fp16 to fp16
+//
+// An item is eight pairs of a head of q or k; a head is 2^per_log2 lanes.
+struct HeadsArgs {
+    const uint16_t *q, *k, *g_q, *g_k;
+    uint16_t *q_out, *k_out;
+    int64_t ldq, ldk, ldgq, ldgk, ldqo, ldko;
+    const int32_t *pos;
+    const float *cos_t, *sin_t;
+    double eps;
+    int Hq, heads, D, per_log2, P;
+    unsigned rows;               // tokens x heads
+};
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(const HeadsArgs a) {
+    const unsigned item = blockIdx.x * 256u + threadIdx.x, row = item >> a.per_log2;       // below 2^31
+    if (row >= a.rows) return;
+    const int Dh = a.D >> 1, j = (int)(item & ((1u << a.per_log2) - 1)) * 8;
+    const int t = (int)(row / (unsigned)a.heads);
+    int h = (int)row - t * a.heads;
+    const bool keys = h >= a.Hq;
+    h -= keys ? a.Hq : 0;
+    const uint16_t *src = keys ? a.k + (int64_t)t * a.ldk + h * a.D + j : a.q + (int64_t)t * a.ldq + h * a.D + j;
+    uint16_t *dst = keys ? a.k_out + (int64_t)t * a.ldko + h * a.D + j : a.q_out + (int64_t)t * a.ldqo + h * a.D + j;
+    const uint16_t *gain = keys ? a.g_k : a.g_q;
+    Half8 lo = load8(src), hi = load8(src + Dh);
+    const int64_t p = a.cos_t ? min(max(a.pos[t], 0), a.P - 1) : 0;
+    if (gain)
+        norm_rotate8(lo, hi, gain + h * (keys ? a.ldgk : a.ldgq) + j, Dh, a.per_log2, a.eps, a.cos_t ? a.cos_t + p * Dh + j : nullptr,
+                     a.sin_t + p * Dh + j);
+    else if (a.cos_t)
+        rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
+    store8(dst, lo);
+    store8(dst + Dh, hi);
 }
 
 }  // namespace
@@ -432,6 +509,7 @@ int agq_launch_kv_append(const AgqKvAppend &p, void *stream) {
     a.ldq = p.ldq, a.ldk = p.ldk, a.ldv = p.ldv, a.ldqo = p.ldqo, a.ldko = p.ldko;
     a.pos = p.pos, a.slot = p.slot, a.cos_t = p.rope_cos, a.sin_t = p.rope_sin;
     a.kc = p.k_cache, a.vc = p.v_cache, a.ke = p.k_exp, a.ve = p.v_exp;
+    a.g_q = (const uint16_t *)p.g_q, a.g_k = (const uint16_t *)p.g_k, a.ldgq = p.ldgq, a.ldgk = p.ldgk, a.eps = p.eps;
     a.T = (int)p.T, a.Hq = (int)p.Hq, a.Hkv = (int)p.Hkv, a.D = (int)p.D, a.D_log2 = log2_of(p.D), a.P = (int)p.P;
     a.page = p.page, a.page_log2 = log2_of(p.page), a.n_pages = (int)p.n_pages;
     // Chunks: a run of a whole page or more to a workgroup, as those that find none to begin take turns with the others (6000
@@ -448,9 +526,21 @@ int agq_launch_kv_append(const AgqKvAppend &p, void *stream) {
     const int64_t q_groups = (p.T * p.Hq * (p.D / 16) + threads - 1) / threads;
     const int64_t groups = (int64_t)a.chunks * ((2 * p.Hkv + roles - 1) / roles) + q_groups;
     const size_t lds = (size_t)p.page * p.D * 2 + 16;
-    if (roles == 4)
-        kv_append_kernel<4><<<dim3((unsigned)groups), threads, lds, (hipStream_t)stream>>>(a);
-    else
-        kv_append_kernel<1><<<dim3((unsigned)groups), threads, lds, (hipStream_t)stream>>>(a);
+    auto kernel = a.g_k ? (roles == 4 ? kv_append_kernel<4, true> : kv_append_kernel<1, true>)
+                        : (roles == 4 ? kv_append_kernel<4, false> : kv_append_kernel<1, false>);
+    kernel<<<dim3((unsigned)groups), threads, lds, (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
+int agq_launch_qk_norm_rope(const AgqQkNormRope &p, void *stream) {
+    HeadsArgs a;
+    a.q = (const uint16_t *)p.q, a.k = (const uint16_t *)p.k, a.g_q = (const uint16_t *)p.g_q, a.g_k = (const uint16_t *)p.g_k;
+    a.q_out = (uint16_t *)p.q_out, a.k_out = (uint16_t *)p.k_out;
+    a.ldq = p.ldq, a.ldk = p.ldk, a.ldgq = p.ldgq, a.ldgk = p.ldgk, a.ldqo = p.ldqo, a.ldko = p.ldko;
+    a.pos = p.pos, a.cos_t = p.rope_cos, a.sin_t = p.rope_sin, a.eps = p.eps;
+    a.Hq = (int)p.Hq, a.heads = (int)(p.Hq + p.Hkv), a.D = (int)p.D, a.per_log2 = log2_of(p.D) - 4, a.P = (int)p.P;
+    a.rows = (unsigned)(p.T * (p.Hq + p.Hkv));
+    const int64_t groups = (((int64_t)a.rows << a.per_log2) + 255) / 256;
+    qk_norm_rope_kernel<<<dim3((unsigned)groups), 256, 0, (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }

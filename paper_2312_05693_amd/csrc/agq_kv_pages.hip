@@ -1,0 +1,410 @@
+// Pages of the key/value cache that several requests hold: requests that go on as copies of others, requests that lose
+// tokens, pages copied and tokens moved in the caches of all layers.
+#include "agq_device.h"
+#include "agq_internal.h"
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kMaxB = 4096;           // requests: their sums are held in LDS
+
+// Three launches make a step: the holders' counts are copied (and listed tokens checked), every workgroup works out the
+// requests' sums for itself and does its share of the rows, and the pages that nobody holds any more go to the ring.  Counts
+// change by atomic additions of whole numbers, whose order does not matter; the pages given back are found afterwards in the
+// order of their numbers, so the ring does not depend on it either.
+struct ForkArgs {
+    const int32_t *kv_len, *parent, *table, *shared, *ring, *free_in;
+    int32_t *kv_len_out, *table_out, *shared_out, *copy_src, *copy_dst, *free_out, *status;
+    int64_t max_pages;
+    int B, page_log2, n_pages;
+};
+
+__device__ __forceinline__ int ring_at(int head, int64_t i, int n_pages) {       // head and i below n_pages
+    const uint32_t at = (uint32_t)head + (uint32_t)i;
+    return (int)(at >= (uint32_t)n_pages ? at - (uint32_t)n_pages : at);
+}
+
+// the sum over the workgroup's threads before this one, and of all of them
+template <int THREADS>
+__device__ __forceinline__ int block_scan(int v, int *waves, int &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int up = agq_wave_scan(v);
+    __syncthreads();
+    if (lane == 63) waves[wave] = up;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < wave) before += waves[w];
+        total += waves[w];
+    }
+    return before + up - v;
+}
+
+// the largest i in [0, n) with at[i] <= x (at[0] <= x)
+__device__ __forceinline__ int find_row(const int *at, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (at[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(256) void shared_copy_kernel(const int32_t *shared, int32_t *shared_out, int n_pages) {
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n_pages; i += gridDim.x * 256) shared_out[i] = max(shared[i], 0);
+}
+
+__global__ __launch_bounds__(kThreads) void kv_fork_kernel(const ForkArgs a) {
+    __shared__ int n_child[kMaxB], first_child[kMaxB], copy_at[kMaxB];       // copy_at: which of the taken pages, -1: none
+    __shared__ int waves[kThreads / 64];
+    const int tid = threadIdx.x, page1 = (1 << a.page_log2) - 1;
+    const int64_t capacity = a.max_pages << a.page_log2;
+    const int head = a.free_in[0], count = a.free_in[1];
+    const bool lead = blockIdx.x == 0;
+    for (int b = tid; b < a.B; b += kThreads) n_child[b] = 0, first_child[b] = a.B;
+    __syncthreads();
+    bool bad = head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages;
+    for (int b = tid; b < a.B; b += kThreads) {
+        const int p = a.parent[b], L = a.kv_len[b];
+        bad |= p < -1 || p >= a.B || L < 0 || L > capacity;
+        if (p >= 0 && p < a.B) {
+            atomicAdd(&n_child[p], 1);
+            atomicMin(&first_child[p], b);
+        }
+    }
+    bad = __syncthreads_or(bad);
+    auto pages_of = [&](int L) { return (int)(((int64_t)L + page1) >> a.page_log2); };
+    // the page that a request's length ends in, if partly filled: does somebody else hold it too?
+    auto joint = [&](int b, int L) {
+        const int id = a.table[(int64_t)b * a.max_pages + pages_of(L) - 1];
+        return (unsigned)id < (unsigned)a.n_pages && a.shared[id] > 0;
+    };
+    int need = 0;
+    if (!bad)
+        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+            const int b = b0 + tid;
+            int copied = 0;
+            if (b < a.B) {
+                const int p = a.parent[b], L = p >= 0 ? a.kv_len[p] : 0;
+                copied = (L & page1) && (b != first_child[p] || joint(p, L));
+            }
+            int total;
+            const int before = block_scan<kThreads>(copied, waves, total);
+            if (b < a.B) copy_at[b] = copied ? need + before : -1;
+            need += total;
+        }
+    __syncthreads();
+    const bool go = !bad && need <= count;
+    if (lead && tid == 0) {
+        *a.status = bad ? -1 : go ? 0 : need - count;
+        a.free_out[0] = go ? ring_at(head, need, a.n_pages) : head;
+        a.free_out[1] = go ? count - need : count;             // the pages given back come on top
+    }
+    if (lead)
+        for (int b = tid; b < a.B; b += kThreads) {
+            const int p = go ? a.parent[b] : b, L = p >= 0 ? a.kv_len[p] : 0;
+            const bool copied = go && copy_at[b] >= 0;
+            a.kv_len_out[b] = L;
+            a.copy_src[b] = copied ? a.table[(int64_t)p * a.max_pages + pages_of(L) - 1] : -1;
+            a.copy_dst[b] = copied ? a.ring[ring_at(head, copy_at[b], a.n_pages)] : -1;
+        }
+    const int64_t chunks = (a.max_pages + kThreads - 1) / kThreads;
+    for (int64_t item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
+        const int b = (int)(item / chunks), j = (int)(item % chunks) * kThreads + tid;
+        // its pages after the call
+        const int p = go ? a.parent[b] : b;
+        if (p >= 0) {
+            const int L = max(a.kv_len[p], 0), n = (int)min((int64_t)pages_of(L), a.max_pages);
+            if (j < n) {
+                const int at = go && j == n - 1 ? copy_at[b] : -1;
+                a.table_out[(int64_t)b * a.max_pages + j] = at >= 0 ? a.ring[ring_at(head, at, a.n_pages)] : a.table[(int64_t)p * a.max_pages + j];
+            }
+        }
+        if (!go) continue;
+        // the holders of its pages before the call: every copy is one, itself no longer
+        const int L = a.kv_len[b], n = pages_of(L), more = n_child[b] - 1;
+        if (j < n) {
+            const int change = j < L >> a.page_log2 ? more : more < 0 || joint(b, L) ? -1 : 0;
+            const int id = change ? a.table[(int64_t)b * a.max_pages + j] : -1;
+            if ((unsigned)id < (unsigned)a.n_pages) atomicAdd(a.shared_out + id, change);
+        }
+    }
+}
+
+// Pages whose count fell below 0 go behind the free ones, in the order of their numbers.  free_out: {head, free pages so far}.
+__global__ __launch_bounds__(1024) void kv_give_back_kernel(int32_t *shared, int32_t *ring, int32_t *free_out, int n_pages) {
+    __shared__ int waves[16];
+    const int tid = threadIdx.x, head = free_out[0], count = free_out[1];
+    if (head < 0 || head >= n_pages || count < 0 || count > n_pages) return;     // a refused step: nothing has changed
+    int given = 0;
+    for (int i0 = 0; i0 < n_pages; i0 += 4096) {
+        const int i = i0 + tid * 4;
+        bool gone[4];
+        int mine = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) gone[k] = i + k < n_pages && shared[i + k] < 0, mine += gone[k];
+        int total;
+        int at = given + block_scan<1024>(mine, waves, total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (gone[k]) {
+                ring[(int)(((int64_t)head + count + at++) % n_pages)] = i + k;
+                shared[i + k] = 0;
+            }
+        given += total;
+    }
+    if (tid == 0) free_out[1] = min(count + given, n_pages);
+}
+
+// ---------------------------------------------------------------- requests that lose tokens
+struct CompactArgs {
+    const int32_t *kv_len, *stay, *cu, *keep, *table, *shared, *ring, *free_in;
+    int32_t *kv_len_out, *table_out, *shared_out, *moves, *free_out, *status;
+    int64_t max_pages, N;
+    int B, page_log2, n_pages;
+    int32_t *checked;                 // AGQ_KV_CHECKS words behind the new pages in `moves`
+};
+
+// the holders' counts, and whether the listed tokens ascend inside their requests
+__global__ __launch_bounds__(kThreads) void kv_compact_check_kernel(const CompactArgs a) {
+    __shared__ int cu[kMaxB + 1];
+    const int tid = threadIdx.x;
+    for (int i = blockIdx.x * kThreads + tid; i < a.n_pages; i += gridDim.x * kThreads) a.shared_out[i] = max(a.shared[i], 0);
+    for (int b = tid; b <= a.B; b += kThreads) cu[b] = a.cu[b];
+    __syncthreads();
+    bool bad = false;
+    if (a.B > 0)
+        for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < a.N; i += (int64_t)gridDim.x * kThreads) {
+            const int b = find_row(cu, a.B, (int)i);
+            if (i < cu[b] || i >= cu[b + 1]) continue;         // of no request
+            const int x = a.keep[i];
+            bad |= x >= a.kv_len[b] || x < a.stay[b] || (i > cu[b] && x <= a.keep[i - 1]);
+        }
+    bad = __syncthreads_or(bad);
+    if (tid == 0) a.checked[blockIdx.x] = bad;
+}
+
+__global__ __launch_bounds__(kThreads) void kv_compact_kernel(const CompactArgs a, int checked) {
+    __shared__ int need_at[kMaxB], same_of[kMaxB], after_of[kMaxB];      // taken pages before, pages that stay, length after
+    __shared__ int waves[kThreads / 64];
+    const int tid = threadIdx.x, page1 = (1 << a.page_log2) - 1;
+    const int64_t capacity = a.max_pages << a.page_log2;
+    const int head = a.free_in[0], count = a.free_in[1];
+    const bool lead = blockIdx.x == 0;
+    bool bad = head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages;
+    if (tid < checked) bad |= a.checked[tid] != 0;
+    for (int b = tid; b < a.B; b += kThreads) {
+        const int L = a.kv_len[b], c0 = a.cu[b], c1 = a.cu[b + 1];
+        bad |= L < 0 || L > capacity || a.stay[b] < 0 || c0 < 0 || c1 < c0 || c1 > a.N;
+    }
+    bad = __syncthreads_or(bad);
+    auto pages_of = [&](int L) { return (int)(((int64_t)L + page1) >> a.page_log2); };
+    int need = 0;
+    if (!bad)
+        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+            const int b = b0 + tid;
+            int mine = 0;
+            if (b < a.B) {
+                const int L = a.kv_len[b], s = min(a.stay[b], L), n = a.cu[b + 1] - a.cu[b], after = s + n, total = pages_of(after);
+                int same = n > 0 ? s >> a.page_log2 : total;
+                if (n == 0 && after < L && (after & page1)) {            // cut inside a page, which it will write into
+                    const int id = a.table[(int64_t)b * a.max_pages + total - 1];
+                    if ((unsigned)id < (unsigned)a.n_pages && a.shared[id] > 0) same = total - 1;
+                }
+                mine = total - same;
+                same_of[b] = same, after_of[b] = after;
+            }
+            int total;
+            const int before = block_scan<kThreads>(mine, waves, total);
+            if (b < a.B) need_at[b] = need + before;
+            need += total;
+        }
+    __syncthreads();
+    const bool go = !bad && need <= count;
+    if (lead && tid == 0) {
+        *a.status = bad ? -1 : go ? 0 : need - count;
+        a.free_out[0] = go ? ring_at(head, need, a.n_pages) : head;
+        a.free_out[1] = go ? count - need : count;             // the pages given back come on top
+        a.moves[0] = go ? need : 0;
+    }
+    if (lead)
+        for (int b = tid; b < a.B; b += kThreads) a.kv_len_out[b] = go ? after_of[b] : a.kv_len[b];
+    const int64_t chunks = (a.max_pages + kThreads - 1) / kThreads;
+    for (int64_t item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
+        const int b = (int)(item / chunks), j = (int)(item % chunks) * kThreads + tid;
+        const int held = (int)min((int64_t)pages_of(max(a.kv_len[b], 0)), a.max_pages);
+        const int same = go ? same_of[b] : held, after = go ? after_of[b] : 0, total = go ? pages_of(after) : held;
+        const int old = j < held ? a.table[(int64_t)b * a.max_pages + j] : -1;
+        if (j < total) {
+            int id = old;
+            if (j >= same) {
+                const int u = need_at[b] + j - same;
+                id = a.ring[ring_at(head, u, a.n_pages)];
+                reinterpret_cast<int4 *>(a.moves)[1 + u] = make_int4(b, j, id, min(after - (j << a.page_log2), 1 << a.page_log2));
+            }
+            a.table_out[(int64_t)b * a.max_pages + j] = id;
+        }
+        if (j >= same && (unsigned)old < (unsigned)a.n_pages) atomicAdd(a.shared_out + old, -1);
+    }
+}
+
+// ---------------------------------------------------------------- the caches of all layers
+struct Layers {                       // a launch's arguments
+    int8_t *k[AGQ_KV_LAYERS], *v[AGQ_KV_LAYERS], *ke[AGQ_KV_LAYERS], *ve[AGQ_KV_LAYERS];
+};
+
+// A workgroup copies 4 KB of each page (its keys, then its values) of 64 entries of the list, in one layer.
+__global__ __launch_bounds__(256) void kv_copy_pages_kernel(const Layers c, const int32_t *src, const int32_t *dst, int n, int n_pages, int Hkv,
+                                                            int page_bytes) {
+    const int tid = threadIdx.x, lane = tid & 63, layer = blockIdx.y, i = blockIdx.z * 64 + lane;
+    const int from = i < n ? src[i] : -1, to = i < n ? dst[i] : -1;
+    unsigned long long todo = __ballot((unsigned)from < (unsigned)n_pages && (unsigned)to < (unsigned)n_pages);
+    const int64_t at = ((int64_t)blockIdx.x * 256 + tid) * 16;
+    const bool values = at >= page_bytes;
+    int8_t *codes = (values ? c.v[layer] : c.k[layer]) + (values ? at - page_bytes : at);
+    for (; todo; todo &= todo - 1) {
+        const int e = __ffsll((long long)todo) - 1;
+        const int64_t s = __builtin_amdgcn_readlane(from, e), d = __builtin_amdgcn_readlane(to, e);
+        if (at < 2 * (int64_t)page_bytes) *reinterpret_cast<uint4 *>(codes + d * page_bytes) = *reinterpret_cast<const uint4 *>(codes + s * page_bytes);
+        if (blockIdx.x == 0)
+            for (int h = tid; h < Hkv; h += 256) {
+                c.ke[layer][d * Hkv + h] = c.ke[layer][s * Hkv + h];
+                c.ve[layer][d * Hkv + h] = c.ve[layer][s * Hkv + h];
+            }
+    }
+}
+
+// an 8-bit code divided by 2^d, ties to even (down = 2^-d)
+__device__ __forceinline__ uint32_t coarser(uint32_t byte, float down) { return (uint32_t)(int)rintf((float)(int8_t)byte * down) & 0xFFu; }
+
+struct MoveArgs {
+    const int32_t *moves, *table, *stay, *cu, *keep;
+    int64_t max_pages, N;
+    int B, layers, Hkv, D, page, page_log2, n_pages, most;      // most: new pages that `moves` has room for
+};
+
+// An item is a new page of one layer, for one head, keys or values.
+__global__ __launch_bounds__(256) void kv_move_kernel(const Layers c, const MoveArgs a) {
+    __shared__ int page_of[128], slot_of[128], exp_of[128];
+    __shared__ int top_exp;
+    const int tid = threadIdx.x, roles = 2 * a.Hkv;
+    const int64_t items = (int64_t)min(max(a.moves[0], 0), a.most) * a.layers * roles;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int role = (int)(item % roles), layer = (int)(item / roles % a.layers), u = (int)(item / roles / a.layers);
+        const int4 m = reinterpret_cast<const int4 *>(a.moves)[1 + u];      // request, entry, page, tokens
+        const int b = min(max(m.x, 0), a.B - 1), j = m.y, n = min(max(m.w, 0), a.page), head = role >> 1;
+        if ((unsigned)m.z >= (unsigned)a.n_pages) continue;
+        const bool values = role & 1;
+        int8_t *codes = values ? c.v[layer] : c.k[layer], *exps = values ? c.ve[layer] : c.ke[layer];
+        __syncthreads();                                                    // the item before is done with the LDS
+        if (tid == 0) top_exp = -128;
+        __syncthreads();
+        if (tid < a.page) {
+            int id = -1, slot = 0, e = -128;
+            if (tid < n) {
+                const int64_t i = ((int64_t)j << a.page_log2) + tid;
+                const int s = a.stay[b];
+                int64_t old = i;
+                if (i >= s) {
+                    const int64_t at = a.cu[b] + i - s;
+                    old = at >= 0 && at < a.N ? a.keep[at] : -1;
+                }
+                const int64_t entry = old >> a.page_log2;
+                if (old >= 0 && entry < a.max_pages) id = a.table[b * a.max_pages + entry], slot = (int)(old & (a.page - 1));
+                if ((unsigned)id < (unsigned)a.n_pages) {
+                    e = exps[(int64_t)id * a.Hkv + head];
+                    atomicMax(&top_exp, e);
+                } else {
+                    id = -1;
+                }
+            }
+            page_of[tid] = id, slot_of[tid] = slot, exp_of[tid] = e;
+        }
+        __syncthreads();
+        const int e = top_exp;
+        const int64_t stride = (int64_t)a.Hkv * a.page * a.D, mine = (int64_t)head * a.page * a.D;
+        int8_t *to = codes + m.z * stride + mine;
+        if (tid == 0) exps[(int64_t)m.z * a.Hkv + head] = (int8_t)e;
+        for (int w = tid; w < a.page * a.D / 16; w += 256) {
+            uint4 o = make_uint4(0, 0, 0, 0);
+            uint8_t *byte = reinterpret_cast<uint8_t *>(&o);
+            if (!values) {
+                const int t = w / (a.D / 16), d = w % (a.D / 16) * 16;
+                if (page_of[t] >= 0) {
+                    const float down = __builtin_amdgcn_ldexpf(1.0f, exp_of[t] - e);
+                    const uint4 x = *reinterpret_cast<const uint4 *>(codes + page_of[t] * stride + mine + slot_of[t] * a.D + d);
+                    const uint8_t *in = reinterpret_cast<const uint8_t *>(&x);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) byte[k] = (uint8_t)coarser(in[k], down);
+                }
+            } else {
+                const int d = w / (a.page / 16), t0 = w % (a.page / 16) * 16;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const int t = t0 + k;
+                    if (page_of[t] >= 0)
+                        byte[k] = (uint8_t)coarser((uint8_t)codes[page_of[t] * stride + mine + (d << a.page_log2) + slot_of[t]],
+                                                   __builtin_amdgcn_ldexpf(1.0f, exp_of[t] - e));
+                }
+            }
+            *reinterpret_cast<uint4 *>(to + w * 16) = o;
+        }
+    }
+}
+
+int log2_of(int64_t v) { return __builtin_ctzll((unsigned long long)v); }
+unsigned at_most(int64_t n, int64_t most) { return (unsigned)(n < 1 ? 1 : n > most ? most : n); }
+
+}  // namespace
+
+int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy_src, int32_t *copy_dst, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    const ForkArgs a = {p.kv_len, parent, p.table, p.shared, p.ring, p.free_in, p.kv_len_out, p.table_out, p.shared_out, copy_src, copy_dst, p.free_out,
+                        p.status, p.max_pages, (int)p.B, log2_of(p.page), (int)p.n_pages};
+    shared_copy_kernel<<<at_most((p.n_pages + 255) / 256, 256), 256, 0, st>>>(p.shared, p.shared_out, (int)p.n_pages);
+    if (int err = (int)hipGetLastError()) return err;
+    kv_fork_kernel<<<at_most(p.B * ((p.max_pages + kThreads - 1) / kThreads), 256), kThreads, 0, st>>>(a);
+    if (int err = (int)hipGetLastError()) return err;
+    kv_give_back_kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
+    return (int)hipGetLastError();
+}
+
+int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int32_t *moves, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    const CompactArgs a = {p.kv_len, stay, cu, keep, p.table, p.shared, p.ring, p.free_in, p.kv_len_out, p.table_out, p.shared_out, moves, p.free_out,
+                           p.status, p.max_pages, N, (int)p.B, log2_of(p.page), (int)p.n_pages,
+                           moves + 4 + 4 * agq_kv_new_pages(N, p.B, p.page)};
+    const int64_t work = N > p.n_pages ? N : p.n_pages;
+    const unsigned groups = at_most((work + kThreads - 1) / kThreads, AGQ_KV_CHECKS);
+    kv_compact_check_kernel<<<groups, kThreads, 0, st>>>(a);
+    if (int err = (int)hipGetLastError()) return err;
+    kv_compact_kernel<<<at_most(p.B * ((p.max_pages + kThreads - 1) / kThreads), 256), kThreads, 0, st>>>(a, (int)groups);
+    if (int err = (int)hipGetLastError()) return err;
+    kv_give_back_kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
+    return (int)hipGetLastError();
+}
+
+static Layers layers_of(const AgqKvLayer *c, int n) {
+    Layers l = {};
+    for (int i = 0; i < n; ++i) l.k[i] = c[i].k, l.v[i] = c[i].v, l.ke[i] = c[i].k_exp, l.ve[i] = c[i].v_exp;
+    return l;
+}
+
+int agq_launch_kv_copy_pages(const AgqKvShape &s, const AgqKvLayer *layers, int n_layers, const int32_t *src, const int32_t *dst, int64_t n,
+                             void *stream) {
+    const int64_t bytes = s.Hkv * s.page * s.D;
+    const dim3 grid((unsigned)((2 * bytes + 4095) / 4096), (unsigned)n_layers, (unsigned)((n + 63) / 64));
+    kv_copy_pages_kernel<<<grid, 256, 0, (hipStream_t)stream>>>(layers_of(layers, n_layers), src, dst, (int)n, (int)s.n_pages, (int)s.Hkv, (int)bytes);
+    return (int)hipGetLastError();
+}
+
+int agq_launch_kv_move(const AgqKvShape &s, const AgqKvLayer *layers, int n_layers, const int32_t *moves, const int32_t *table, int64_t max_pages,
+                       const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int64_t B, void *stream) {
+    const int64_t most = agq_kv_new_pages(N, B, s.page);
+    const MoveArgs a = {moves, table, stay, cu, keep, max_pages, N, (int)B, n_layers, (int)s.Hkv, (int)s.D, (int)s.page, log2_of(s.page), (int)s.n_pages,
+                        (int)most};
+    kv_move_kernel<<<at_most(most * n_layers * 2 * s.Hkv, 2048), 256, 0, (hipStream_t)stream>>>(layers_of(layers, n_layers), a);
+    return (int)hipGetLastError();
+}
