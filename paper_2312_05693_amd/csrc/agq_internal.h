@@ -506,6 +506,24 @@ struct AgqLogprobs {
     float *logprob, *entropy, *top_logprob;
     int32_t *top_idx;
 };
+// A unit is four 16-byte loads of each lane; a group is a quarter of one of them.  Rows are cut into pieces of four wavefronts
+// until there are about a thousand workgroups.  whole: one workgroup has the row and answers at once; its groups' largest
+// logits fit the LDS.
+#define AGQ_LP_LOADS 4
+#define AGQ_LP_HELD 2048
+struct AgqLpPlan {
+    int units, wave_units, pieces, groups;
+    bool whole;
+};
+static inline AgqLpPlan agq_lp_plan(int64_t T, int64_t V, int kind, int64_t n_top) {
+    const int64_t values = AGQ_LP_LOADS * 64 * (kind ? 4 : 8), units = (V + values - 1) / values, quads = (units + 3) / 4;
+    const int64_t want = T >= 1024 ? 1 : T > 0 ? 1024 / T : 1, each = (quads + want - 1) / want;
+    AgqLpPlan p;
+    p.units = (int)units, p.wave_units = (int)each, p.pieces = (int)((quads + each - 1) / each), p.groups = (int)units * AGQ_LP_LOADS * 4;
+    p.whole = p.pieces == 1 && (n_top == 0 || p.groups <= AGQ_LP_HELD);
+    return p;
+}
+size_t agq_logprobs_workspace(int64_t T, int64_t V, int kind, int64_t n_top);
 int agq_launch_logprobs(const AgqLogprobs &p, void *workspace, void *stream);
 // Tiles of 128 queries of B sequences with Tq queries in all: the sum of ceil(n / 128) is not more.  (Workgroups that find no tile
 // take turns with the others in the order in which CUs get them: one spare tile for a single one left half of the CUs without

@@ -241,7 +241,7 @@ int agq_kv_move(const agq_kv_cache *caches, int n_caches, const int32_t *moves, 
 size_t agq_logprobs_workspace_bytes(int64_t T, int64_t V, int kind, int64_t n_top) {
     if (!count_ok(T, (int64_t)1 << 22) || V < 1 || V > kMaxRow || (kind != AGQ_LOGITS_F16 && kind != AGQ_LOGITS_F32)) return 0;
     if (n_top < 0 || n_top > AGQ_MAX_TOP || n_top > V) return 0;
-    return 0;
+    return agq_logprobs_workspace(T, V, kind, n_top);
 }
 
 int agq_logprobs(const void *logits, int kind, int64_t T, int64_t V, int64_t ld, float scale, const int32_t *tokens, int64_t n_top, float *logprob,
