@@ -255,101 +255,180 @@ struct Layers {                       // a launch's arguments
     int8_t *k[AGQ_KV_LAYERS], *v[AGQ_KV_LAYERS], *ke[AGQ_KV_LAYERS], *ve[AGQ_KV_LAYERS];
 };
 
-// A workgroup copies 4 KB of each page (its keys, then its values) of 64 entries of the list, in one layer.
+// A workgroup copies 4 KB of each page (its keys, then its values) of 64 entries of the list, in one layer, eight of them at a
+// time.
 __global__ __launch_bounds__(256) void kv_copy_pages_kernel(const Layers c, const int32_t *src, const int32_t *dst, int n, int n_pages, int Hkv,
                                                             int page_bytes) {
+    constexpr int AT_ONCE = 8;
     const int tid = threadIdx.x, lane = tid & 63, layer = blockIdx.y, i = blockIdx.z * 64 + lane;
     const int from = i < n ? src[i] : -1, to = i < n ? dst[i] : -1;
     unsigned long long todo = __ballot((unsigned)from < (unsigned)n_pages && (unsigned)to < (unsigned)n_pages);
     const int64_t at = ((int64_t)blockIdx.x * 256 + tid) * 16;
-    const bool values = at >= page_bytes;
+    const bool values = at >= page_bytes, mine = at < 2 * (int64_t)page_bytes;
     int8_t *codes = (values ? c.v[layer] : c.k[layer]) + (values ? at - page_bytes : at);
-    for (; todo; todo &= todo - 1) {
-        const int e = __ffsll((long long)todo) - 1;
-        const int64_t s = __builtin_amdgcn_readlane(from, e), d = __builtin_amdgcn_readlane(to, e);
-        if (at < 2 * (int64_t)page_bytes) *reinterpret_cast<uint4 *>(codes + d * page_bytes) = *reinterpret_cast<const uint4 *>(codes + s * page_bytes);
-        if (blockIdx.x == 0)
+    if (blockIdx.x == 0)
+        for (unsigned long long left = todo; left; left &= left - 1) {
+            const int e = __ffsll((long long)left) - 1;
+            const int64_t s = __builtin_amdgcn_readlane(from, e), d = __builtin_amdgcn_readlane(to, e);
             for (int h = tid; h < Hkv; h += 256) {
                 c.ke[layer][d * Hkv + h] = c.ke[layer][s * Hkv + h];
                 c.ve[layer][d * Hkv + h] = c.ve[layer][s * Hkv + h];
             }
+        }
+    if (!mine) return;
+    auto next = [&](const int8_t *&from_at, int8_t *&to_at) {
+        const int e = __ffsll((long long)todo) - 1;
+        todo &= todo - 1;
+        from_at = codes + (int64_t)__builtin_amdgcn_readlane(from, e) * page_bytes;
+        to_at = codes + (int64_t)__builtin_amdgcn_readlane(to, e) * page_bytes;
+    };
+    for (int left = __popcll(todo); left >= AT_ONCE; left -= AT_ONCE) {
+        const int8_t *s[AT_ONCE];
+        int8_t *d[AT_ONCE];
+        agq_v4i x[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) next(s[j], d[j]);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) x[j] = *reinterpret_cast<const agq_v4i *>(s[j]);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) *reinterpret_cast<agq_v4i *>(d[j]) = x[j];
+    }
+    while (todo) {
+        const int8_t *s;
+        int8_t *d;
+        next(s, d);
+        *reinterpret_cast<uint4 *>(d) = *reinterpret_cast<const uint4 *>(s);
     }
 }
 
 // an 8-bit code divided by 2^d, ties to even (down = 2^-d)
 __device__ __forceinline__ uint32_t coarser(uint32_t byte, float down) { return (uint32_t)(int)rintf((float)(int8_t)byte * down) & 0xFFu; }
+__device__ __forceinline__ uint32_t coarser4(uint32_t w, float down) {
+    return coarser(w, down) | coarser(w >> 8, down) << 8 | coarser(w >> 16, down) << 16 | coarser(w >> 24, down) << 24;
+}
 
 struct MoveArgs {
     const int32_t *moves, *table, *stay, *cu, *keep;
     int64_t max_pages, N;
-    int B, layers, Hkv, D, page, page_log2, n_pages, most;      // most: new pages that `moves` has room for
+    int B, layers, Hkv, D, D_log2, page, page_log2, n_pages, most;      // most: new pages that `moves` has room for
 };
 
-// An item is a new page of one layer, for one head, keys or values.
+// An item is a new page of one layer, for one head; a workgroup takes neighbouring items, most of them of one page, whose tokens'
+// old places it looks up once.  Tokens of one old page are neighbours in the new one: a run.  Keys are rows, copied 16 bytes at
+// a time.  Values lie transposed: lanes are rows d, and a wavefront takes sixteen old tokens of 64 rows, of which it puts those
+// that are kept into the new tile in LDS, byte by byte, as which ones they are is the same for all lanes; rows there are an odd
+// number of words apart, so that the lanes' bytes are in different banks.
 __global__ __launch_bounds__(256) void kv_move_kernel(const Layers c, const MoveArgs a) {
-    __shared__ int page_of[128], slot_of[128], exp_of[128];
-    __shared__ int top_exp;
-    const int tid = threadIdx.x, roles = 2 * a.Hkv;
-    const int64_t items = (int64_t)min(max(a.moves[0], 0), a.most) * a.layers * roles;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int role = (int)(item % roles), layer = (int)(item / roles % a.layers), u = (int)(item / roles / a.layers);
-        const int4 m = reinterpret_cast<const int4 *>(a.moves)[1 + u];      // request, entry, page, tokens
-        const int b = min(max(m.x, 0), a.B - 1), j = m.y, n = min(max(m.w, 0), a.page), head = role >> 1;
-        if ((unsigned)m.z >= (unsigned)a.n_pages) continue;
-        const bool values = role & 1;
-        int8_t *codes = values ? c.v[layer] : c.k[layer], *exps = values ? c.ve[layer] : c.ke[layer];
-        __syncthreads();                                                    // the item before is done with the LDS
-        if (tid == 0) top_exp = -128;
-        __syncthreads();
-        if (tid < a.page) {
-            int id = -1, slot = 0, e = -128;
-            if (tid < n) {
-                const int64_t i = ((int64_t)j << a.page_log2) + tid;
-                const int s = a.stay[b];
-                int64_t old = i;
-                if (i >= s) {
-                    const int64_t at = a.cu[b] + i - s;
-                    old = at >= 0 && at < a.N ? a.keep[at] : -1;
+    __shared__ uint32_t run_mask[128][4];                   // which of its tokens a run's old page gives
+    __shared__ int run_page[128], run_first[128], run_exp[2][128], run_of[128], slot_of[128];
+    __shared__ int n_runs, gaps, top_exp[2];             // gaps: tokens whose old page is not in the cache
+    __shared__ uint32_t tile[128 * 33];                     // [D][page + 4] bytes
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t items = (int64_t)min(max(a.moves[0], 0), a.most) * a.layers * a.Hkv, per = (items + gridDim.x - 1) / gridDim.x;
+    const int64_t stride = (int64_t)a.Hkv * a.page << a.D_log2;
+    const int row = a.page + 4;
+    int have = -1, n = 0, to_page = -1;
+    for (int64_t item = blockIdx.x * per; item < min((blockIdx.x + 1) * per, items); ++item) {
+        const int head = (int)(item % a.Hkv), layer = (int)(item / a.Hkv % a.layers), u = (int)(item / a.Hkv / a.layers);
+        if (u != have) {
+            have = u;
+            const int4 m = reinterpret_cast<const int4 *>(a.moves)[1 + u];      // request, entry, page, tokens
+            const int b = min(max(m.x, 0), a.B - 1), j = m.y;
+            n = min(max(m.w, 0), a.page), to_page = m.z;
+            __syncthreads();                                // the items before are done with the runs
+            if (tid < 128) run_mask[tid][0] = run_mask[tid][1] = run_mask[tid][2] = run_mask[tid][3] = 0;
+            __syncthreads();
+            if (wave == 0) {
+                int runs = 0, last = -1, lost = 0;
+                for (int t0 = 0; t0 < n; t0 += 64) {
+                    const int t = t0 + lane;
+                    int id = -1, slot = 0;
+                    if (t < n) {
+                        const int64_t i = ((int64_t)j << a.page_log2) + t;
+                        const int s = a.stay[b];
+                        int64_t old = i;
+                        if (i >= s) {
+                            const int64_t at = a.cu[b] + i - s;
+                            old = at >= 0 && at < a.N ? a.keep[at] : -1;
+                        }
+                        const int64_t entry = old >> a.page_log2;
+                        if (old >= 0 && entry < a.max_pages) id = a.table[b * a.max_pages + entry], slot = (int)(old & (a.page - 1));
+                        if ((unsigned)id >= (unsigned)a.n_pages) id = -1;
+                    }
+                    const int before = __shfl_up(id, 1);
+                    const bool begins = t < n && (lane == 0 ? t0 == 0 || id != last : id != before);
+                    const unsigned long long at = __ballot(begins), upto = at & (~0ull >> (63 - lane));
+                    const int r = runs + __popcll(upto) - 1;
+                    if (begins) run_page[r] = id, run_first[r] = t;
+                    if (t < n) {
+                        run_of[t] = r, slot_of[t] = slot;
+                        atomicOr(&run_mask[r][slot >> 5], 1u << (slot & 31));
+                    }
+                    runs += __popcll(at);
+                    last = __builtin_amdgcn_readlane(id, 63);
+                    lost |= __any(t < n && id < 0);
                 }
-                const int64_t entry = old >> a.page_log2;
-                if (old >= 0 && entry < a.max_pages) id = a.table[b * a.max_pages + entry], slot = (int)(old & (a.page - 1));
-                if ((unsigned)id < (unsigned)a.n_pages) {
-                    e = exps[(int64_t)id * a.Hkv + head];
-                    atomicMax(&top_exp, e);
-                } else {
-                    id = -1;
-                }
+                if (lane == 0) n_runs = runs, gaps = lost;
             }
-            page_of[tid] = id, slot_of[tid] = slot, exp_of[tid] = e;
+            __syncthreads();
+        }
+        if ((unsigned)to_page >= (unsigned)a.n_pages) continue;
+        const int64_t mine = (int64_t)head * a.page << a.D_log2;
+        if (tid < 2) top_exp[tid] = -128;
+        __syncthreads();                                    // and the item before is done with the exponents and the tile
+        const int runs = n_runs;
+        for (int i = tid; i < 2 * runs; i += 256) {
+            const int v = i >= runs, r = i - v * runs, id = run_page[r];
+            const int e = id < 0 ? -128 : (v ? c.ve[layer] : c.ke[layer])[(int64_t)id * a.Hkv + head];
+            run_exp[v][r] = e;
+            atomicMax(&top_exp[v], e);
+        }
+        if (n < a.page || gaps)                             // behind the tokens, and where no old page is
+            for (int w = tid; w < (a.D * row) >> 2; w += 256) tile[w] = 0;
+        __syncthreads();
+        const int e_k = top_exp[0], e_v = top_exp[1];
+        if (tid < 2) (tid ? c.ve[layer] : c.ke[layer])[(int64_t)to_page * a.Hkv + head] = (int8_t)(tid ? e_v : e_k);
+        // values, into the tile
+        const int8_t *from_v = c.v[layer] + mine;
+        const int halves = a.D >> 6, chunks = a.page >> 4, units = runs * chunks * halves;
+        for (int w = wave; w < units; w += 4) {
+            const int half = w & (halves - 1), k0 = (w / halves) & (chunks - 1), r = w / halves / chunks, id = run_page[r];
+            if (id < 0) continue;
+            uint32_t bits = (run_mask[r][k0 >> 1] >> ((k0 & 1) * 16)) & 0xFFFFu;
+            bits = __builtin_amdgcn_readfirstlane(bits);
+            if (bits == 0) continue;
+            int t = run_first[r];
+            for (int q = 0; q < k0; ++q) t += __popc((run_mask[r][q >> 1] >> ((q & 1) * 16)) & 0xFFFFu);
+            t = __builtin_amdgcn_readfirstlane(t);
+            const int d = half * 64 + lane;
+            const uint4 x = *reinterpret_cast<const uint4 *>(from_v + id * stride + (d << a.page_log2) + k0 * 16);
+            const float down = __builtin_amdgcn_ldexpf(1.0f, run_exp[1][r] - e_v);
+            const uint32_t words[4] = {x.x, x.y, x.z, x.w};
+            uint8_t *out = reinterpret_cast<uint8_t *>(tile) + d * row;
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (bits >> k & 1) out[t++] = (uint8_t)coarser(words[k >> 2] >> ((k & 3) * 8), down);
+        }
+        // keys
+        const int8_t *from_k = c.k[layer] + mine;
+        int8_t *to_k = c.k[layer] + to_page * stride + mine, *to_v = c.v[layer] + to_page * stride + mine;
+        const int per_log2 = a.D_log2 - 4;
+        for (int w = tid; w < a.page << per_log2; w += 256) {
+            const int t = w >> per_log2, d = (w & ((1 << per_log2) - 1)) * 16, r = t < n ? run_of[t] : 0, id = t < n ? run_page[r] : -1;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (id >= 0) {
+                x = *reinterpret_cast<const uint4 *>(from_k + id * stride + (slot_of[t] << a.D_log2) + d);
+                const float down = __builtin_amdgcn_ldexpf(1.0f, run_exp[0][r] - e_k);
+                if (down != 1.0f) x = make_uint4(coarser4(x.x, down), coarser4(x.y, down), coarser4(x.z, down), coarser4(x.w, down));
+            }
+            *reinterpret_cast<uint4 *>(to_k + (t << a.D_log2) + d) = x;
         }
         __syncthreads();
-        const int e = top_exp;
-        const int64_t stride = (int64_t)a.Hkv * a.page * a.D, mine = (int64_t)head * a.page * a.D;
-        int8_t *to = codes + m.z * stride + mine;
-        if (tid == 0) exps[(int64_t)m.z * a.Hkv + head] = (int8_t)e;
-        for (int w = tid; w < a.page * a.D / 16; w += 256) {
-            uint4 o = make_uint4(0, 0, 0, 0);
-            uint8_t *byte = reinterpret_cast<uint8_t *>(&o);
-            if (!values) {
-                const int t = w / (a.D / 16), d = w % (a.D / 16) * 16;
-                if (page_of[t] >= 0) {
-                    const float down = __builtin_amdgcn_ldexpf(1.0f, exp_of[t] - e);
-                    const uint4 x = *reinterpret_cast<const uint4 *>(codes + page_of[t] * stride + mine + slot_of[t] * a.D + d);
-                    const uint8_t *in = reinterpret_cast<const uint8_t *>(&x);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) byte[k] = (uint8_t)coarser(in[k], down);
-                }
-            } else {
-                const int d = w / (a.page / 16), t0 = w % (a.page / 16) * 16;
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const int t = t0 + k;
-                    if (page_of[t] >= 0)
-                        byte[k] = (uint8_t)coarser((uint8_t)codes[page_of[t] * stride + mine + (d << a.page_log2) + slot_of[t]],
-                                                   __builtin_amdgcn_ldexpf(1.0f, exp_of[t] - e));
-                }
-            }
-            *reinterpret_cast<uint4 *>(to + w * 16) = o;
+        const int chunk_log2 = a.page_log2 - 4;
+        for (int w = tid; w < a.D << chunk_log2; w += 256) {
+            const int d = w >> chunk_log2, k = w & (chunks - 1);
+            const uint32_t *p = tile + ((d * row) >> 2) + k * 4;
+            *reinterpret_cast<uint4 *>(to_v + w * 16) = make_uint4(p[0], p[1], p[2], p[3]);
         }
     }
 }
@@ -403,8 +482,8 @@ int agq_launch_kv_copy_pages(const AgqKvShape &s, const AgqKvLayer *layers, int 
 int agq_launch_kv_move(const AgqKvShape &s, const AgqKvLayer *layers, int n_layers, const int32_t *moves, const int32_t *table, int64_t max_pages,
                        const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int64_t B, void *stream) {
     const int64_t most = agq_kv_new_pages(N, B, s.page);
-    const MoveArgs a = {moves, table, stay, cu, keep, max_pages, N, (int)B, n_layers, (int)s.Hkv, (int)s.D, (int)s.page, log2_of(s.page), (int)s.n_pages,
-                        (int)most};
-    kv_move_kernel<<<at_most(most * n_layers * 2 * s.Hkv, 2048), 256, 0, (hipStream_t)stream>>>(layers_of(layers, n_layers), a);
+    const MoveArgs a = {moves, table, stay, cu, keep, max_pages, N, (int)B, n_layers, (int)s.Hkv, (int)s.D, log2_of(s.D), (int)s.page, log2_of(s.page),
+                        (int)s.n_pages, (int)most};
+    kv_move_kernel<<<at_most(most * n_layers * s.Hkv, 2048), 256, 0, (hipStream_t)stream>>>(layers_of(layers, n_layers), a);
     return (int)hipGetLastError();
 }

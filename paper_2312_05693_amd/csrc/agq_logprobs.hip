@@ -7,6 +7,7 @@
 // The pass also leaves the largest logit of every group of neighbours (256 bytes of them: sixteen lanes' loads).  The n_top
 // likeliest tokens lie in the n_top groups with the largest of these, equal ones by their place: any other token has one at
 // least as good in front of it in each of those.  So only some groups are looked at again, by one wavefront.
+#include <limits.h>
 #include "agq_device.h"
 #include "agq_internal.h"
 
@@ -52,18 +53,43 @@ __device__ __forceinline__ int row_max(int v) {          // of sixteen lanes
     return max(v, dpp<0x128>(v));
 }
 
-// the values of one 16-byte load
+// One 16-byte load, its values less m, and the largest of them
 template <class E>
 struct Vec;
 template <>
 struct Vec<_Float16> {
     static constexpr int N = 8;
-    _Float16 v[8];
+    uint32_t w[4];
+    // a half of a word as float32, plus -m: one instruction
+    __device__ __forceinline__ float less(int k, float minus_m) const {
+        float d;
+        if (k & 1)
+            asm("v_fma_mix_f32 %0, %1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(w[k >> 1]), "v"(minus_m));
+        else
+            asm("v_fma_mix_f32 %0, %1, 1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d) : "v"(w[k >> 1]), "v"(minus_m));
+        return d;
+    }
+    static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) {      // of two pairs
+        uint32_t r;
+        asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+        return r;
+    }
+    __device__ __forceinline__ float largest() const {
+        const agq_h2v h = __builtin_bit_cast(agq_h2v, max2(max2(w[0], w[1]), max2(w[2], w[3])));
+        return fmaxf((float)h[0], (float)h[1]);
+    }
+    __device__ __forceinline__ void set(int k, _Float16 x) {
+        const uint32_t u = __builtin_bit_cast(uint16_t, x);
+        w[k >> 1] = k & 1 ? (w[k >> 1] & 0xFFFFu) | u << 16 : u;
+    }
 };
 template <>
 struct Vec<float> {
     static constexpr int N = 4;
     float v[4];
+    __device__ __forceinline__ float less(int k, float minus_m) const { return v[k] + minus_m; }
+    __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
+    __device__ __forceinline__ void set(int k, float x) { v[k] = x; }
 };
 template <class E>
 struct Unit {
@@ -90,7 +116,7 @@ __device__ __forceinline__ Unit<E> load_unit(const E *x, int V, int u, int lane)
             continue;
         }
 #pragma unroll
-        for (int k = 0; k < N; ++k) r.d[i].v[k] = e + k < V ? x[e + k] : (E)-kInf;
+        for (int k = 0; k < N; ++k) r.d[i].set(k, e + k < V ? x[e + k] : (E)-kInf);
     }
     return r;
 }
@@ -98,16 +124,26 @@ __device__ __forceinline__ Unit<E> load_unit(const E *x, int V, int u, int lane)
 struct Sums {
     float m, S, E;
 };
+// A unit's values into a lane's sums, relative to m.  Where 2^z is 0 its product with z is to be 0 too, also for z = -infinity:
+// CLAMP keeps z finite there.
+template <class E, bool CLAMP>
+__device__ __forceinline__ void add_values(float &S, float &H, const Unit<E> &u, float m, float c) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int k = 0; k < Vec<E>::N; ++k) {
+            const float z = u.d[i].less(k, -m) * c, e = __builtin_amdgcn_exp2f(z);
+            S += e;
+            H = fmaf(e, CLAMP ? fmaxf(z, -150.0f) : z, H);
+        }
+}
 // a lane's sums taken to a larger m, and a unit's values into them
 template <class E, bool TOP>
 __device__ __forceinline__ void add_unit(Sums &s, const Unit<E> &u, float c, int *tops, int lane) {
-    constexpr int N = Vec<E>::N;
     float top[kLoads], all = s.m;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        top[i] = (float)u.d[i].v[0];
-#pragma unroll
-        for (int k = 1; k < N; ++k) top[i] = fmaxf(top[i], (float)u.d[i].v[k]);
+        top[i] = u.d[i].largest();
         all = fmaxf(all, top[i]);
     }
     if constexpr (TOP) {                                  // lane i of sixteen writes load i's
@@ -119,139 +155,226 @@ __device__ __forceinline__ void add_unit(Sums &s, const Unit<E> &u, float c, int
         }
         if ((lane & 15) < kLoads) tops[(lane & 15) * 4 + (lane >> 4)] = mine;
     }
-    const float d = (s.m - all) * c, f = __builtin_amdgcn_exp2f(d);
-    s.E = f * (s.E + fmaxf(d, -150.0f) * s.S);            // S is 0 where s.m is not a logit yet
-    s.S *= f;
-    s.m = all;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const float z = ((float)u.d[i].v[k] - all) * c, e = __builtin_amdgcn_exp2f(z);
-            s.S += e;
-            s.E = fmaf(e, fmaxf(z, -150.0f), s.E);        // e is 0 there; -infinity times 0 would not be
-        }
+    const float d = fmaxf((s.m - all) * c, -150.0f), f = __builtin_amdgcn_exp2f(d);
+    const float S = f * s.S, H = f * fmaf(d, s.S, s.E);   // S is 0 where s.m is not a logit yet
+    s.m = all, s.S = S, s.E = H;
+    add_values<E, false>(s.S, s.E, u, all, c);
+    if (__any(s.E != s.E)) {                              // -infinity among them, or a NaN (which stays one)
+        s.S = S, s.E = H;
+        add_values<E, true>(s.S, s.E, u, all, c);
+    }
 }
 
 struct Row {
     double S, E;
     float m;
 };
-__device__ __forceinline__ Row joined(const Row &a, const Row &b, float c) {
-    Row r;
-    r.m = fmaxf(a.m, b.m);
-    const float da = fmaxf((a.m - r.m) * c, -300.0f), db = fmaxf((b.m - r.m) * c, -300.0f);
-    const double fa = (double)__builtin_amdgcn_exp2f(da), fb = (double)__builtin_amdgcn_exp2f(db);
-    r.S = a.S * fa + b.S * fb;
-    r.E = fa * (a.E + (double)da * a.S) + fb * (b.E + (double)db * b.S);
-    return r;
+__device__ __forceinline__ Row taken_to(const Row &r, float m, float c) {
+    const float d = fmaxf((r.m - m) * c, -300.0f);
+    const double f = (double)__builtin_amdgcn_exp2f(d);
+    return Row{f * r.S, f * (r.E + (double)d * r.S), m};
 }
+__device__ __forceinline__ Row joined(const Row &a, const Row &b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    const Row x = taken_to(a, m, c), y = taken_to(b, m, c);
+    return Row{x.S + y.S, x.E + y.E, m};
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double v) {     // plus another lane's, in the rows that are written; 0 elsewhere
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xF, false);
+    return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double v) {    // in lane 63
+    v = dpp_add<0x111, 0xF>(v);                           // row_shr 1, 2, 4, 8: inside sixteen lanes
+    v = dpp_add<0x112, 0xF>(v);
+    v = dpp_add<0x114, 0xF>(v);
+    v = dpp_add<0x118, 0xF>(v);
+    v = dpp_add<0x142, 0xA>(v);                           // row_bcast 15 and 31
+    return dpp_add<0x143, 0xC>(v);
+}
+// the wavefront's rows joined; S and E in lane 63 only
 __device__ __forceinline__ Row wave_joined(Row r, float c) {
-    for (int s = 1; s < 64; s <<= 1) r = joined(r, Row{__shfl_xor(r.S, s), __shfl_xor(r.E, s), __shfl_xor(r.m, s)}, c);
-    return r;
+    float m = r.m;
+    m = fmaxf(m, __int_as_float(dpp<0x121>(__float_as_int(m))));
+    m = fmaxf(m, __int_as_float(dpp<0x122>(__float_as_int(m))));
+    m = fmaxf(m, __int_as_float(dpp<0x124>(__float_as_int(m))));
+    m = fmaxf(m, __int_as_float(dpp<0x128>(__float_as_int(m))));
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    r = taken_to(r, m, c);
+    return Row{wave_sum(r.S), wave_sum(r.E), m};
+}
+__device__ __forceinline__ double lane_63(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)u, 63));
 }
 
 // ---------------------------------------------------------------- the likeliest tokens, by one wavefront
+constexpr int kBlock = 16;       // groups' largest logits that a lane holds at once
+constexpr int kAtOnce = 16;      // groups that are looked at together
 struct Scratch {
-    Key waiting[128];            // candidates that are not in the list yet
-    int picked[256];             // groups to be looked at
+    Key waiting[64 + 128 * kAtOnce];      // of groups or tokens that are not in the list yet; kBlock * 64 is less
 };
 
-__device__ __forceinline__ Key other(Key k, int x) { return (Key)__shfl_xor((long long)k, x); }
-__device__ __forceinline__ Key better(Key a, Key b) { return a > b ? a : b; }
-__device__ __forceinline__ Key worse(Key a, Key b) { return a > b ? b : a; }
-// the wavefront's keys in descending order
-__device__ __forceinline__ Key sorted(Key k, int lane) {
-#pragma unroll
-    for (int n = 2; n <= 64; n <<= 1)
-#pragma unroll
-        for (int j = n >> 1; j > 0; j >>= 1) {
-            const Key o = other(k, j);
-            k = (((lane & n) == 0) == ((lane & j) == 0)) ? better(k, o) : worse(k, o);
-        }
-    return k;
-}
-// the best 64 of two descending lists, descending
-__device__ __forceinline__ Key merged(Key a, Key b, int lane) {
-    Key k = better(a, (Key)__shfl((long long)b, 63 - lane));
-#pragma unroll
-    for (int j = 32; j > 0; j >>= 1) {
-        const Key o = other(k, j);
-        k = (lane & j) == 0 ? better(k, o) : worse(k, o);
+// the key of lane ^ X, by data-parallel moves
+template <int X>
+__device__ __forceinline__ uint32_t other(uint32_t v, int lane) {
+    if constexpr (X == 1) return (uint32_t)dpp<0xB1>((int)v);             // quad_perm 1 0 3 2
+    if constexpr (X == 2) return (uint32_t)dpp<0x4E>((int)v);             // quad_perm 2 3 0 1
+    if constexpr (X == 4) {                                               // row_ror 4 and 12: four lanes back, four ahead
+        const int back = dpp<0x124>((int)v), ahead = dpp<0x12C>((int)v);
+        return (uint32_t)(lane & 4 ? back : ahead);
     }
+    if constexpr (X == 8) return (uint32_t)dpp<0x128>((int)v);            // row_ror 8
+    if constexpr (X == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return lane & 16 ? r[0] : r[1];
+    }
+    if constexpr (X == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return lane & 32 ? r[0] : r[1];
+    }
+}
+template <int X>
+__device__ __forceinline__ Key other(Key k, int lane) { return (Key)other<X>((uint32_t)(k >> 32), lane) << 32 | other<X>((uint32_t)k, lane); }
+__device__ __forceinline__ Key better(Key a, Key b) { return a > b ? a : b; }
+// a step of a sorting network: the better one of lanes X apart to the lower one if `down`, else to the upper one
+template <int X>
+__device__ __forceinline__ Key step(Key k, int lane, bool down) {
+    const Key o = other<X>(k, lane);
+    return (k > o) == (((lane & X) == 0) == down) ? k : o;
+}
+template <int X>
+__device__ __forceinline__ Key steps(Key k, int lane, bool down) {
+    k = step<X>(k, lane, down);
+    if constexpr (X > 1) k = steps<X / 2>(k, lane, down);
     return k;
 }
+// the wavefront's keys in ascending order
+__device__ __forceinline__ Key sorted(Key k, int lane) {
+    k = steps<1>(k, lane, (lane & 2) != 0);
+    k = steps<2>(k, lane, (lane & 4) != 0);
+    k = steps<4>(k, lane, (lane & 8) != 0);
+    k = steps<8>(k, lane, (lane & 16) != 0);
+    k = steps<16>(k, lane, (lane & 32) != 0);
+    return steps<32>(k, lane, false);
+}
+// the best 64 of a descending and an ascending list, descending
+__device__ __forceinline__ Key merged(Key a, Key b, int lane) { return steps<32>(better(a, b), lane, true); }
 __device__ __forceinline__ Key lane_key(Key k, int lane) {
     return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
+
+// The best n of the keys that come by: those that wait (in LDS) are merged into `list` (descending, lane i has the i-th), 64 at a
+// time, once there are 64 or with ALL; cut: the n-th, below which none counts.
+struct Best {
+    Key list, cut;
+    int waiting, n, lane;
+    Key *wait;
+    __device__ __forceinline__ void fence() const { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+    __device__ __forceinline__ void add(Key k, bool good) {
+        const unsigned long long in = __ballot(good);
+        if (good) wait[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = k;
+        waiting += __popcll(in);
+    }
+    __device__ __forceinline__ void merge(bool all) {
+        fence();
+        int q = 0;
+#pragma unroll 1
+        for (; q + 64 <= waiting || (all && q < waiting); q += 64) {
+            const Key k = q + lane < waiting ? wait[q + lane] : 0;
+            if (!__any(k > cut)) continue;
+            list = merged(list, sorted(k, lane), lane);
+            const Key last = lane_key(list, n - 1);
+            if (last != 0) cut = last;
+        }
+        if (q == 0) return;
+        const Key k = q + lane < waiting ? wait[q + lane] : 0;
+        fence();
+        wait[lane] = k;
+        fence();
+        waiting = max(waiting - q, 0);
+    }
+};
 
 // lane i < n gets the i-th best token's key
 template <class E>
 __device__ __forceinline__ Key likeliest(const E *x, int V, const int *tops, int groups, int n, Scratch &sc, int lane) {
     constexpr int G = 16 * Vec<E>::N, PER = G / 64;
-    // each lane's best group; the n-th best of these lets the n best groups and few others through
+    // every lane's best group; the n-th best of these lets the n best groups and few others through
+    int top[kBlock];
+    auto load_tops = [&](int g0) {
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i) top[i] = tops[min(g0 + 64 * i + lane, groups - 1)];
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i) top[i] = g0 + 64 * i + lane < groups ? top[i] : INT_MIN;
+    };
     Key mine = 0;
-    for (int g = lane; g < groups; g += 64) mine = better(mine, key_of(tops[g], (uint32_t)g));
-    Key bound = 0;
-    if (n <= min(groups, 64)) {
-        int before = 0;
-        for (int l = 0; l < 64; ++l) before += lane_key(mine, l) > mine;
-        bound = lane_key(mine, __ffsll((long long)__ballot(before == n - 1)) - 1);
-    }
-    Key list = 0, cut = bound & ~(Key)0xFFFFFFFFu;       // tokens above it: at first those as large as the bound's
-    int picked = 0, waiting = 0;
-    auto take = [&] {                                     // the first 64 that wait, into the list
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const Key k = lane < waiting ? sc.waiting[lane] : 0, rest = lane + 64 < waiting ? sc.waiting[lane + 64] : 0;
-        list = merged(list, sorted(k, lane), lane);
-        sc.waiting[lane] = rest;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        waiting = max(waiting - 64, 0);
-        const Key last = lane_key(list, n - 1);
-        if (last != 0) cut = last;
-    };
-    auto look = [&] {
-        constexpr int AT_ONCE = 8;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int p0 = 0; p0 < picked; p0 += AT_ONCE) {
-            E v[AT_ONCE][PER];
-            int at[AT_ONCE];
+#pragma unroll 1
+    for (int g0 = 0; g0 < groups; g0 += 64 * kBlock) {
+        load_tops(g0);
+        int best = top[0], at = g0;
 #pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i) {
-                at[i] = p0 + i < picked ? sc.picked[p0 + i] * G + lane : V;
-#pragma unroll
-                for (int k = 0; k < PER; ++k) v[i][k] = at[i] + 64 * k < V ? x[at[i] + 64 * k] : (E)0;
-            }
-#pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i)
-#pragma unroll
-                for (int k = 0; k < PER; ++k) {
-                    const int a = at[i] + 64 * k;
-                    const Key key = a < V ? key_of(order((float)v[i][k]), (uint32_t)a) : 0;
-                    const unsigned long long in = __ballot(key > cut);
-                    if (in == 0) continue;
-                    if (key > cut) sc.waiting[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = key;
-                    waiting += __popcll(in);
-                    if (waiting >= 64) take();
-                }
+        for (int i = 1; i < kBlock; ++i) {
+            at = top[i] > best ? g0 + 64 * i : at;
+            best = max(best, top[i]);
         }
-        picked = 0;
-    };
-    for (int g0 = 0; g0 < groups; g0 += 64) {
-        const int g = g0 + lane;
-        const bool pick = g < groups && key_of(tops[g], (uint32_t)g) >= bound;
-        const unsigned long long in = __ballot(pick);
-        if (pick) sc.picked[picked + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = g;
-        picked += __popcll(in);
-        if (picked > 192) look();
+        if (best != INT_MIN) mine = better(mine, key_of(best, (uint32_t)(at + lane)));
     }
-    look();
-    if (waiting > 0) take();
-    return list;
+    // The n best groups, a lane each (all of them if there are no more).  Where few were let through, these will do.
+    const Key bound = n <= min(groups, 64) ? lane_key(sorted(mine, lane), 64 - n) : 0;
+    Best g = {0, bound ? bound - 1 : 0, 0, n, lane, sc.waiting};
+#pragma unroll 1
+    for (int g0 = 0; g0 < groups; g0 += 64 * kBlock) {
+        if (groups > 64 * kBlock) load_tops(g0);
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i) {
+            if (g0 + 64 * i >= groups) break;
+            const Key k = key_of(top[i], (uint32_t)(g0 + 64 * i + lane));
+            g.add(k, top[i] != INT_MIN && k > g.cut);
+        }
+        if (g.waiting > 64 || groups > 64 * kBlock) g.merge(g0 + 64 * kBlock >= groups);
+    }
+    g.fence();
+    int picked = g.waiting;
+    Key least = bound;
+    if (picked > 0) {
+        g.list = lane < picked ? sc.waiting[lane] : 0;
+    } else {
+        picked = n;
+        least = lane_key(g.list, n - 1);
+    }
+    const int group = (int)~(uint32_t)g.list;
+    // their tokens, from those on that are as large as the n-th group's largest
+    Best b = {0, least & ~(Key)0xFFFFFFFFu, 0, n, lane, sc.waiting};
+    g.fence();
+#pragma unroll 1
+    for (int p0 = 0; p0 < picked; p0 += kAtOnce) {
+        E v[kAtOnce][PER];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int at = (p0 + i < picked ? __builtin_amdgcn_readlane(group, p0 + i) : 0) * G + lane;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) v[i][k] = x[min(at + 64 * k, V - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (p0 + i >= picked) break;
+            const int at = __builtin_amdgcn_readlane(group, p0 + i) * G + lane;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const Key key = key_of(order((float)v[i][k]), (uint32_t)(at + 64 * k));
+                b.add(key, at + 64 * k < V && key > b.cut);
+            }
+        }
+        b.merge(p0 + kAtOnce >= picked);
+    }
+    return b.list;
 }
 
 // what is asked for of a row, by one wavefront
-template <class E>
+template <class E, bool TOP>
 __device__ __forceinline__ void answer(const Args &a, int64_t t, const E *x, const Row &r, const int *tops, Scratch &sc, int lane) {
     const bool none = !(r.S > 0.0);        // no distribution: a NaN, or +infinity (less itself), made it one; -infinity only, 0
     const double nan = __builtin_nan(""), lse = none ? nan : log(r.S), scale = (double)a.scale;
@@ -262,7 +385,7 @@ __device__ __forceinline__ void answer(const Args &a, int64_t t, const E *x, con
         }
         if (a.entropy) a.entropy[t] = (float)(lse - r.E / r.S * (scale / (double)(a.scale * kLog2e)));
     }
-    if (a.n_top == 0) return;
+    if constexpr (!TOP) return;
     const Key k = none ? 0 : likeliest<E>(x, a.V, tops, a.groups, a.n_top, sc, lane);
     if (lane < a.n_top) {
         a.top_idx[t * a.n_top + lane] = none ? -1 : (int)~(uint32_t)k;
@@ -294,19 +417,19 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const Args a) {
         }
     }
     Row r = wave_joined(Row{(double)s.S, (double)s.E, s.m}, c);
-    if (lane == 0) rows[wave] = r;
+    if (lane == 63) rows[wave] = r;
     __syncthreads();
     if (wave > 0) return;
     r = joined(joined(rows[0], rows[1], c), joined(rows[2], rows[3], c), c);
     if constexpr (WHOLE) {
-        answer<E>(a, t, x, r, tops, sc, lane);
+        answer<E, TOP>(a, t, x, r, tops, sc, lane);
     } else if (lane == 0) {
         a.parts[t * a.pieces + piece] = Part{r.S, r.E, r.m, 0};
     }
 }
 
 // the answers of rows whose pieces were several workgroups'
-template <class E>
+template <class E, bool TOP>
 __global__ __launch_bounds__(64) void join_kernel(const Args a) {
     __shared__ Scratch sc;
     const int lane = threadIdx.x;
@@ -318,7 +441,8 @@ __global__ __launch_bounds__(64) void join_kernel(const Args a) {
         r = joined(r, Row{q.S, q.E, q.m}, c);
     }
     r = wave_joined(r, c);
-    answer<E>(a, t, (const E *)a.logits + t * a.ld, r, a.tops + t * a.groups, sc, lane);
+    r.S = lane_63(r.S), r.E = lane_63(r.E);
+    answer<E, TOP>(a, t, (const E *)a.logits + t * a.ld, r, a.tops + t * a.groups, sc, lane);
 }
 
 template <class E>
@@ -336,7 +460,10 @@ int launch(const Args &a, int64_t T, bool whole, hipStream_t st) {
     else
         logprobs_kernel<E, false, false><<<grid, 256, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
-    join_kernel<E><<<dim3((unsigned)T), 64, 0, st>>>(a);
+    if (a.n_top)
+        join_kernel<E, true><<<dim3((unsigned)T), 64, 0, st>>>(a);
+    else
+        join_kernel<E, false><<<dim3((unsigned)T), 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
