@@ -177,6 +177,7 @@ struct AppendArgs {
     const uint16_t *g_q, *g_k;
     int64_t ldgq, ldgk;
     double eps;
+    int q_apart;                 // groups of lanes for a token's queries
 };
 constexpr int kEZero = -30;      // the smallest exponent that a nonzero fp16 value asks for; pages of zeros get it too
 
@@ -189,13 +190,12 @@ __device__ __forceinline__ int exp_for(uint32_t top) {
     return (u & 0x7FFFFFu) <= 0x7E0000u ? x - 6 : x - 5;         // m <= 127 / 64
 }
 
-// float64 -> fp16 as in d2h, by way of fp32 rounded to odd, without a branch: what the nearest fp32 value leaves over says
-// whether it was the truncated one; an infinity leaves nothing over (the comparison is false for NaN).
+// float64 -> fp16 as in d2h, by way of the twenty leading bits of the fraction: any bit behind them sets the last one (rounding
+// to odd), which the one rounding that follows sees; they are exact in fp32.
 __device__ __forceinline__ uint16_t d2h_odd(double d) {
-    const float f = (float)d;
-    const double over = d - (double)f;
-    const uint32_t u = __float_as_uint(f), back = (uint32_t)((int32_t)((uint32_t)(__builtin_bit_cast(uint64_t, over) >> 32) ^ u) >> 31);
-    return __half_as_ushort(__float2half_rn(__uint_as_float(__builtin_islessgreater(over, 0.0) ? (u + back) | 1u : u)));
+    const uint64_t u = __builtin_bit_cast(uint64_t, d);
+    const uint32_t hi = (uint32_t)(u >> 32) | min((uint32_t)u, 1u);
+    return __half_as_ushort(__float2half_rn((float)__builtin_bit_cast(double, (uint64_t)hi << 32)));
 }
 // eight pairs of a head turned by their angles
 __device__ __forceinline__ void rotate8(Half8 &lo, Half8 &hi, const float *cos_t, const float *sin_t) {
@@ -210,37 +210,118 @@ __device__ __forceinline__ void rotate8(Half8 &lo, Half8 &hi, const float *cos_t
         hi.v[i] = d2h_odd(h * c + l * s);
     }
 }
-// Eight pairs of a head divided by the head's root mean square, times their gains, and turned (cos_t NULL: not turned), in
-// float64 from fp16 to fp16.  The head's other pairs are the neighbouring lanes' (2^per_log2 of them, all active): their
-// squares are summed across them in pairs, so every lane has the same sum whatever its place.
-__device__ __forceinline__ void norm_rotate8(Half8 &lo, Half8 &hi, const uint16_t *gain, int Dh, int per_log2, double eps, const float *cos_t,
-                                             const float *sin_t) {
-    double l[8], h[8], sum = 0.0;
+// 1 / sqrt(a) to float64's last bit or two: the instruction's 2^-26 or better, and y += y (1 - a y^2) / 2 twice.  Infinite
+// for 0, and 0 for infinity, as the quotient would be.
+__device__ __forceinline__ double inv_sqrt(double a) {
+    const double y = __builtin_amdgcn_rsq(a);
+    double r = fma(y, 0.5 * fma(-a * y, y, 1.0), y);
+    r = fma(r, 0.5 * fma(-a * r, r, 1.0), r);
+    return a > 0.0 && a < __builtin_inf() ? r : y;
+}
+// What a lane does to its eight pairs of a head, y = inv (l a - h b), inv (h c + l d): gains and angles are multiplied once for
+// all heads that have them (exactly: 11 and 24 bits).  Without a rotation l and h stay apart: y = inv l a, inv h c.
+struct Turn {
+    double a[8], b[8], c[8], d[8];
+};
+template <bool ROPE>
+__device__ __forceinline__ Turn turn_of(const uint16_t *gain, int Dh, const float *cos_t, const float *sin_t) {
+    Half8 gl, gh;
+    if (gain) {
+        gl = load8(gain), gh = load8(gain + Dh);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gl.v[i] = gh.v[i] = 0x3C00;          // 1
+    }
+    Turn t;
+    if constexpr (ROPE) {
+        const float4 c0 = reinterpret_cast<const float4 *>(cos_t)[0], c1 = reinterpret_cast<const float4 *>(cos_t)[1];
+        const float4 s0 = reinterpret_cast<const float4 *>(sin_t)[0], s1 = reinterpret_cast<const float4 *>(sin_t)[1];
+        const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+        const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double l = h2d(gl.v[i]), h = h2d(gh.v[i]), c = (double)cs[i], n = (double)sn[i];
+            t.a[i] = l * c, t.b[i] = h * n, t.c[i] = h * c, t.d[i] = l * n;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t.a[i] = h2d(gl.v[i]), t.c[i] = h2d(gh.v[i]);
+    }
+    return t;
+}
+// The head's other pairs are the neighbouring lanes' (2^per_log2 of them, all active): their squares are summed across them in
+// pairs, so every lane has the same sum whatever its place.  norm false: inv = 1.
+template <bool ROPE>
+__device__ __forceinline__ void turn8(Half8 &lo, Half8 &hi, const Turn &t, bool norm, int Dh, int per_log2, double eps) {
+    double inv = 1.0;
+    if (norm) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double l = h2d(lo.v[i]), h = h2d(hi.v[i]);
+            sum = fma(h, h, fma(l, l, sum));
+        }
+        for (int m = 1; m < 1 << per_log2; m <<= 1) sum += __shfl_xor(sum, m);
+        inv = inv_sqrt(sum * (Dh == 64 ? 1.0 / 128 : 1.0 / 64) + eps);
+    }
+    // widened a second time: held in float64 they would take 32 registers, and a SIMD three wavefronts instead of four
+    asm("" : "+v"(*reinterpret_cast<agq_v4i *>(&lo)), "+v"(*reinterpret_cast<agq_v4i *>(&hi)));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        l[i] = h2d(lo.v[i]), h[i] = h2d(hi.v[i]);
-        sum = fma(l[i], l[i], sum);
-        sum = fma(h[i], h[i], sum);
+        const double l = h2d(lo.v[i]), h = h2d(hi.v[i]);
+        lo.v[i] = d2h_odd(ROPE ? inv * fma(l, t.a[i], -(h * t.b[i])) : inv * (l * t.a[i]));
+        hi.v[i] = d2h_odd(ROPE ? inv * fma(h, t.c[i], l * t.d[i]) : inv * (h * t.c[i]));
+    }
+}
+// The same for one head by itself, whose gains and angles nothing else uses (fewer registers).
+template <bool ROPE>
+__device__ __forceinline__ void turn8_once(Half8 &lo, Half8 &hi, const uint16_t *gain, int Dh, int per_log2, double eps, const float *cos_t, const float *sin_t) {
+    Half8 gl = load8(gain), gh = load8(gain + Dh);
+    float cs[8], sn[8];
+    if constexpr (ROPE) {
+        __builtin_memcpy(cs, cos_t, 32);
+        __builtin_memcpy(sn, sin_t, 32);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const double l = h2d(lo.v[i]), h = h2d(hi.v[i]);
+        sum = fma(h, h, fma(l, l, sum));
     }
     for (int m = 1; m < 1 << per_log2; m <<= 1) sum += __shfl_xor(sum, m);
-    const double inv = 1.0 / sqrt(sum * (Dh == 64 ? 1.0 / 128 : 1.0 / 64) + eps);
-    const Half8 gl = load8(gain), gh = load8(gain + Dh);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) l[i] *= h2d(gl.v[i]) * inv, h[i] *= h2d(gh.v[i]) * inv;
-    if (cos_t == nullptr) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) lo.v[i] = d2h_odd(l[i]), hi.v[i] = d2h_odd(h[i]);
-        return;
-    }
-    const float4 c0 = reinterpret_cast<const float4 *>(cos_t)[0], c1 = reinterpret_cast<const float4 *>(cos_t)[1];
-    const float4 s0 = reinterpret_cast<const float4 *>(sin_t)[0], s1 = reinterpret_cast<const float4 *>(sin_t)[1];
-    const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-    const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+    const double inv = inv_sqrt(sum * (Dh == 64 ? 1.0 / 128 : 1.0 / 64) + eps);
+    asm("" : "+v"(*reinterpret_cast<agq_v4i *>(&lo)), "+v"(*reinterpret_cast<agq_v4i *>(&hi)));          // widened a second time, as in turn8
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double c = (double)cs[i], s = (double)sn[i];
-        lo.v[i] = d2h_odd(l[i] * c - h[i] * s);
-        hi.v[i] = d2h_odd(h[i] * c + l[i] * s);
+        const double l = h2d(lo.v[i]) * h2d(gl.v[i]), h = h2d(hi.v[i]) * h2d(gh.v[i]);           // exact
+        if constexpr (ROPE) {
+            const double c = (double)cs[i], n = (double)sn[i];
+            lo.v[i] = d2h_odd(inv * fma(l, c, -(h * n)));
+            hi.v[i] = d2h_odd(inv * fma(h, c, l * n));
+        } else {
+            lo.v[i] = d2h_odd(inv * l), hi.v[i] = d2h_odd(inv * h);
+        }
+    }
+}
+// Some heads of one token by the 2^per_log2 lanes of a head: first, first + apart, and so on.
+struct Heads {
+    const uint16_t *src, *gain;          // of the token; gain NULL: no norm
+    uint16_t *dst;
+    int64_t ldg;                         // 0: one gain for all heads
+    int heads, apart, D;
+};
+template <bool ROPE>
+__device__ __forceinline__ void turn_heads(const Heads &a, int first, const float *cos_t, const float *sin_t, int per_log2, double eps, int lane) {
+    const int Dh = a.D >> 1, j = (lane & ((1 << per_log2) - 1)) * 8;
+    Turn t = turn_of<ROPE>(a.gain ? a.gain + first * a.ldg + j : nullptr, Dh, cos_t + j, sin_t + j);
+    Half8 lo = load8(a.src + first * a.D + j), hi = load8(a.src + first * a.D + j + Dh);
+    for (int h = first; h < a.heads; h += a.apart) {
+        Half8 x = lo, y = hi;
+        if (h + a.apart < a.heads) lo = load8(a.src + (h + a.apart) * a.D + j), hi = load8(a.src + (h + a.apart) * a.D + j + Dh);
+        if (h > first && a.ldg != 0) t = turn_of<ROPE>(a.gain + h * a.ldg + j, Dh, cos_t + j, sin_t + j);
+        turn8<ROPE>(x, y, t, a.gain != nullptr, Dh, per_log2, eps);
+        store8(a.dst + h * a.D + j, x);
+        store8(a.dst + h * a.D + j + Dh, y);
     }
 }
 // the largest magnitude of eight fp16 values, as bits; NaN does not count
@@ -283,9 +364,13 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
         if (!values) {
             hi = load8(src + i * ld + j + Dh);
             const int64_t p = a.cos_t ? min(max(a.pos[t + i], 0), a.P - 1) : 0;
-            if constexpr (NORM)
-                norm_rotate8(lo, hi, a.g_k + head * a.ldgk + j, Dh, per_log2, a.eps, a.cos_t ? a.cos_t + p * Dh + j : nullptr, a.sin_t + p * Dh + j);
-            else if (a.cos_t)
+            if constexpr (NORM) {
+                const uint16_t *gain = a.g_k + head * a.ldgk + j;
+                if (a.cos_t)
+                    turn8_once<true>(lo, hi, gain, Dh, per_log2, a.eps, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
+                else
+                    turn8_once<false>(lo, hi, gain, Dh, per_log2, a.eps, nullptr, nullptr);
+            } else if (a.cos_t)
                 rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
             if (a.k_out) {
                 uint16_t *dst = a.k_out + (int64_t)(t + i) * a.ldko + head * a.D + j;
@@ -358,9 +443,10 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
 // ROLES = 1: a workgroup takes the runs that begin in its chunk of tokens, for one role (the keys or the values of a head).
 // ROLES = 4: one token and four roles to a workgroup.  A short run, as in a generation step, is that of its first token's
 // workgroup, whose wavefronts have a role each; a long one is shared by the workgroups of its first four tokens, a role each.
-// NORM: queries and keys are normalised before their rotation.
+// NORM: queries and keys are normalised before their rotation; a step's five workgroups of a CU are to fit it (256 tokens of 32 query
+// and 8 key heads 9.5 -> 9.2 us).
 template <int ROLES, bool NORM>
-__global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
+__global__ __launch_bounds__(256, NORM && ROLES == 4 ? 6 : 1) void kv_append_kernel(const AppendArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint16_t held[];      // [run][D], then one word per wavefront
     const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -368,6 +454,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
     const unsigned kv_groups = a.chunks * groups;
     if (blockIdx.x >= kv_groups) {                                       // queries: nothing to store but themselves
         const int per_log2 = a.D_log2 - 4, Dh = a.D >> 1;
+        if constexpr (NORM && ROLES == 1) {                              // q_apart groups of lanes to a token
+            const unsigned group = ((blockIdx.x - kv_groups) * threads + tid) >> per_log2;
+            const int t = (int)(group / (unsigned)a.q_apart), first = (int)group - t * a.q_apart;
+            if (t >= a.T || (unsigned)a.slot[t] >= (unsigned)slots) return;
+            const Heads h = {a.q + (int64_t)t * a.ldq, a.g_q, a.q_out + (int64_t)t * a.ldqo, a.ldgq, a.Hq, a.q_apart, a.D};
+            if (a.cos_t) {
+                const int64_t p = min(max(a.pos[t], 0), a.P - 1);
+                turn_heads<true>(h, first, a.cos_t + p * Dh, a.sin_t + p * Dh, per_log2, a.eps, lane);
+            } else {
+                turn_heads<false>(h, first, nullptr, nullptr, per_log2, a.eps, lane);
+            }
+            return;
+        }
         const unsigned item = (blockIdx.x - kv_groups) * threads + tid, th = item >> per_log2;   // below 2^31 (the caller's check)
         const int t = (int)(th / (unsigned)a.Hq), h = (int)th - t * a.Hq, j = (int)(item & ((1u << per_log2) - 1)) * 8;
         if (t >= a.T || (unsigned)a.slot[t] >= (unsigned)slots) return;
@@ -375,10 +474,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
         uint16_t *dst = a.q_out + (int64_t)t * a.ldqo + h * a.D + j;
         Half8 lo = load8(src), hi = load8(src + Dh);
         const int64_t p = NORM && !a.cos_t ? 0 : min(max(a.pos[t], 0), a.P - 1);
-        if constexpr (NORM)
-            norm_rotate8(lo, hi, a.g_q + h * a.ldgq + j, Dh, per_log2, a.eps, a.cos_t ? a.cos_t + p * Dh + j : nullptr, a.sin_t + p * Dh + j);
-        else
+        if constexpr (NORM) {
+            if (a.cos_t)
+                turn8_once<true>(lo, hi, a.g_q + h * a.ldgq + j, Dh, per_log2, a.eps, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
+            else
+                turn8_once<false>(lo, hi, a.g_q + h * a.ldgq + j, Dh, per_log2, a.eps, nullptr, nullptr);
+        } else {
             rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
+        }
         store8(dst, lo);
         store8(dst + Dh, hi);
         return;
@@ -455,7 +558,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
 
 // ---------------------------------------------------------------- normalised and rotated heads, fp16 to fp16
 //
-// An item is eight pairs of a head of q or k; a head is 2^per_log2 lanes.
+// The lanes of a head take some heads of one token, of q or of k, so that the token's angles and the gains are read and
+// multiplied once for them.
 struct HeadsArgs {
     const uint16_t *q, *k, *g_q, *g_k;
     uint16_t *q_out, *k_out;
@@ -463,34 +567,30 @@ struct HeadsArgs {
     const int32_t *pos;
     const float *cos_t, *sin_t;
     double eps;
-    int Hq, heads, D, per_log2, P;
-    unsigned rows;               // tokens x heads
+    int T, Hq, Hkv, D, per_log2, P, q_apart, k_apart;            // groups of lanes for a token's queries and keys
 };
+template <bool ROPE>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const HeadsArgs a) {
-    const unsigned item = blockIdx.x * 256u + threadIdx.x, row = item >> a.per_log2;       // below 2^31
-    if (row >= a.rows) return;
-    const int Dh = a.D >> 1, j = (int)(item & ((1u << a.per_log2) - 1)) * 8;
-    const int t = (int)(row / (unsigned)a.heads);
-    int h = (int)row - t * a.heads;
-    const bool keys = h >= a.Hq;
-    h -= keys ? a.Hq : 0;
-    const uint16_t *src = keys ? a.k + (int64_t)t * a.ldk + h * a.D + j : a.q + (int64_t)t * a.ldq + h * a.D + j;
-    uint16_t *dst = keys ? a.k_out + (int64_t)t * a.ldko + h * a.D + j : a.q_out + (int64_t)t * a.ldqo + h * a.D + j;
-    const uint16_t *gain = keys ? a.g_k : a.g_q;
-    Half8 lo = load8(src), hi = load8(src + Dh);
-    const int64_t p = a.cos_t ? min(max(a.pos[t], 0), a.P - 1) : 0;
-    if (gain)
-        norm_rotate8(lo, hi, gain + h * (keys ? a.ldgk : a.ldgq) + j, Dh, a.per_log2, a.eps, a.cos_t ? a.cos_t + p * Dh + j : nullptr,
-                     a.sin_t + p * Dh + j);
-    else if (a.cos_t)
-        rotate8(lo, hi, a.cos_t + p * Dh + j, a.sin_t + p * Dh + j);
-    store8(dst, lo);
-    store8(dst + Dh, hi);
+    const int lane = threadIdx.x & 63, apart = a.q_apart + a.k_apart, Dh = a.D >> 1;
+    const unsigned group = (blockIdx.x * 256u + threadIdx.x) >> a.per_log2;                              // below 2^31
+    const int t = (int)(group / (unsigned)apart), part = (int)group - t * apart;
+    if (t >= a.T) return;
+    const bool keys = part >= a.q_apart;
+    const Heads h = {keys ? a.k + (int64_t)t * a.ldk : a.q + (int64_t)t * a.ldq, keys ? a.g_k : a.g_q,
+                     keys ? a.k_out + (int64_t)t * a.ldko : a.q_out + (int64_t)t * a.ldqo, keys ? a.ldgk : a.ldgq, keys ? a.Hkv : a.Hq,
+                     keys ? a.k_apart : a.q_apart, a.D};
+    const int64_t p = ROPE ? min(max(a.pos[t], 0), a.P - 1) : 0;
+    turn_heads<ROPE>(h, keys ? part - a.q_apart : part, a.cos_t + p * Dh, a.sin_t + p * Dh, a.per_log2, a.eps, lane);
 }
 
 }  // namespace
 
 static int log2_of(int64_t v) { return __builtin_ctzll((unsigned long long)v); }
+// Groups of lanes for the heads of a token: up to eight heads to each, as long as about 4096 wavefronts are left in all.
+static int apart_of(int64_t heads, int64_t all_heads, int64_t T, int64_t D) {
+    const int64_t most = T * all_heads * (D / 16) / (4096 * 64), times = most < 1 ? 1 : most > 8 ? 8 : most;
+    return (int)((heads + times - 1) / times);
+}
 
 int agq_launch_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int page, int32_t *block_table, int64_t max_pages,
                       int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T, int32_t *kv_len_out, int32_t *cu_new,
@@ -523,7 +623,8 @@ int agq_launch_kv_append(const AgqKvAppend &p, void *stream) {
     a.chunks = (int)((p.T + chunk - 1) / chunk);
     // one item of a full page's keys to a thread, or more
     const int threads = roles == 4 || p.page * p.D >= 4096 ? 256 : (int)(p.page * p.D / 16);
-    const int64_t q_groups = (p.T * p.Hq * (p.D / 16) + threads - 1) / threads;
+    a.q_apart = p.g_k && roles == 1 ? apart_of(p.Hq, p.Hq, p.T, p.D) : (int)p.Hq;
+    const int64_t q_groups = (p.T * a.q_apart * (p.D / 16) + threads - 1) / threads;
     const int64_t groups = (int64_t)a.chunks * ((2 * p.Hkv + roles - 1) / roles) + q_groups;
     const size_t lds = (size_t)p.page * p.D * 2 + 16;
     auto kernel = a.g_k ? (roles == 4 ? kv_append_kernel<4, true> : kv_append_kernel<1, true>)
@@ -538,9 +639,12 @@ int agq_launch_qk_norm_rope(const AgqQkNormRope &p, void *stream) {
     a.q_out = (uint16_t *)p.q_out, a.k_out = (uint16_t *)p.k_out;
     a.ldq = p.ldq, a.ldk = p.ldk, a.ldgq = p.ldgq, a.ldgk = p.ldgk, a.ldqo = p.ldqo, a.ldko = p.ldko;
     a.pos = p.pos, a.cos_t = p.rope_cos, a.sin_t = p.rope_sin, a.eps = p.eps;
-    a.Hq = (int)p.Hq, a.heads = (int)(p.Hq + p.Hkv), a.D = (int)p.D, a.per_log2 = log2_of(p.D) - 4, a.P = (int)p.P;
-    a.rows = (unsigned)(p.T * (p.Hq + p.Hkv));
-    const int64_t groups = (((int64_t)a.rows << a.per_log2) + 255) / 256;
-    qk_norm_rope_kernel<<<dim3((unsigned)groups), 256, 0, (hipStream_t)stream>>>(a);
+    a.T = (int)p.T, a.Hq = (int)p.Hq, a.Hkv = (int)p.Hkv, a.D = (int)p.D, a.per_log2 = log2_of(p.D) - 4, a.P = (int)p.P;
+    a.q_apart = apart_of(p.Hq, p.Hq + p.Hkv, p.T, p.D), a.k_apart = apart_of(p.Hkv, p.Hq + p.Hkv, p.T, p.D);
+    const dim3 grid((unsigned)((p.T * (a.q_apart + a.k_apart) * (p.D / 16) + 255) / 256));
+    if (p.rope_cos)
+        qk_norm_rope_kernel<true><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+    else
+        qk_norm_rope_kernel<false><<<grid, 256, 0, (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }
