@@ -489,6 +489,15 @@ struct AgqKvLayer {
 // New pages of a compaction with N listed tokens, at most: a request's first n listed tokens fill n / page of them, the tokens
 // in front of them in the first one and those behind in the last one two more.
 static inline int64_t agq_kv_new_pages(int64_t N, int64_t B, int64_t page) { return N / page + 2 * B; }
+#define AGQ_KV_MAX_B 4096
+// Steps that one workgroup does in one launch: requests, pages (their holders' counts are in LDS), entries of the table, listed tokens.
+#define AGQ_KV_ONE_B 1024
+#define AGQ_KV_ONE_PAGES 8192
+#define AGQ_KV_ONE_ENTRIES 8192
+#define AGQ_KV_ONE_LISTED 4096
+static inline bool agq_kv_one(int64_t B, int64_t max_pages, int64_t n_pages, int64_t N) {
+    return B <= AGQ_KV_ONE_B && n_pages <= AGQ_KV_ONE_PAGES && B * max_pages <= AGQ_KV_ONE_ENTRIES && N <= AGQ_KV_ONE_LISTED;
+}
 int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy_src, int32_t *copy_dst, void *stream);
 int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int32_t *moves, void *stream);
 int agq_launch_kv_copy_pages(const AgqKvShape &s, const AgqKvLayer *layers, int n_layers, const int32_t *src, const int32_t *dst, int64_t n,

@@ -5,16 +5,20 @@
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kMaxB = 4096;           // requests: their sums are held in LDS
+constexpr int kMaxB = AGQ_KV_MAX_B;   // requests: their sums are held in LDS
 
 // Three launches make a step: the holders' counts are copied (and listed tokens checked), every workgroup works out the
 // requests' sums for itself and does its share of the rows, and the pages that nobody holds any more go to the ring.  Counts
 // change by atomic additions of whole numbers, whose order does not matter; the pages given back are found afterwards in the
 // order of their numbers, so the ring does not depend on it either.
+// Small steps (agq_kv_one) are ONE launch of one workgroup, with the counts in LDS: all of it is waiting for memory and for launches.
+template <bool ONE>
+struct Sizes {
+    static constexpr int THREADS = ONE ? 1024 : 512, B = ONE ? AGQ_KV_ONE_B : kMaxB, PAGES = ONE ? AGQ_KV_ONE_PAGES : 1;
+};
 struct ForkArgs {
-    const int32_t *kv_len, *parent, *table, *shared, *ring, *free_in;
-    int32_t *kv_len_out, *table_out, *shared_out, *copy_src, *copy_dst, *free_out, *status;
+    const int32_t *kv_len, *parent, *table, *shared, *free_in;
+    int32_t *ring, *kv_len_out, *table_out, *shared_out, *copy_src, *copy_dst, *free_out, *status;
     int64_t max_pages;
     int B, page_log2, n_pages;
 };
@@ -52,150 +56,197 @@ __device__ __forceinline__ int find_row(const int *at, int n, int x) {
     return lo;
 }
 
+// This workgroup's part of a table: f(request, entry).  One workgroup: thread by thread over rows and entries; else a row's
+// next entries to a workgroup.
+template <bool ONE, class F>
+__device__ __forceinline__ void over_table(int B, int64_t max_pages, F f) {
+    constexpr int THREADS = Sizes<ONE>::THREADS;
+    if constexpr (ONE) {
+        const unsigned most = (unsigned)max_pages, n = (unsigned)B * most;       // some thousands
+        for (unsigned i = threadIdx.x; i < n; i += THREADS) f((int)(i / most), (int)(i % most));
+    } else {
+        const int64_t chunks = (max_pages + THREADS - 1) / THREADS;
+        for (int64_t item = blockIdx.x; item < B * chunks; item += gridDim.x) f((int)(item / chunks), (int)(item % chunks) * THREADS + (int)threadIdx.x);
+    }
+}
+
+// Pages whose count fell below 0 go behind the free ones, in the order of their numbers: n counts from number `first` on, of
+// which they are the `given`-th and following.  The counts are written to out, 0 for those.
+template <int THREADS>
+__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n, int32_t *ring, int n_pages, int64_t behind, int *waves) {
+    int given = 0;
+    for (int i0 = 0; i0 < n; i0 += 4 * THREADS) {
+        const int i = i0 + threadIdx.x * 4;
+        int c[4], mine = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c[k] = i + k < n ? counts[i + k] : 0, mine += c[k] < 0;
+        int total;
+        int at = given + block_scan<THREADS>(mine, waves, total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (c[k] < 0) ring[(int)((behind + at++) % n_pages)] = i + k;
+            if (i + k < n && (c[k] < 0 || out != counts)) out[i + k] = max(c[k], 0);
+        }
+        given += total;
+    }
+    return given;
+}
+
 __global__ __launch_bounds__(256) void shared_copy_kernel(const int32_t *shared, int32_t *shared_out, int n_pages) {
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n_pages; i += gridDim.x * 256) shared_out[i] = max(shared[i], 0);
 }
 
-__global__ __launch_bounds__(kThreads) void kv_fork_kernel(const ForkArgs a) {
-    __shared__ int n_child[kMaxB], first_child[kMaxB], copy_at[kMaxB];       // copy_at: which of the taken pages, -1: none
-    __shared__ int waves[kThreads / 64];
+// free_out: {head, free pages so far}
+__global__ __launch_bounds__(1024) void kv_give_back_kernel(int32_t *shared, int32_t *ring, int32_t *free_out, int n_pages) {
+    __shared__ int waves[16];
+    const int head = free_out[0], count = free_out[1];
+    if (head < 0 || head >= n_pages || count < 0 || count > n_pages) return;     // a refused step: nothing has changed
+    const int given = give_back<1024>(shared, shared, n_pages, ring, n_pages, (int64_t)head + count, waves);
+    if (threadIdx.x == 0) free_out[1] = min(count + given, n_pages);
+}
+
+template <bool ONE>
+__global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_fork_kernel(const ForkArgs a) {
+    constexpr int THREADS = Sizes<ONE>::THREADS;
+    __shared__ int n_child[Sizes<ONE>::B], first_child[Sizes<ONE>::B], copy_at[Sizes<ONE>::B];   // copy_at: which of the taken pages, -1: none
+    __shared__ uint8_t end[Sizes<ONE>::B];      // the page that a request's length ends in: 0 full, 1 partly filled, 2 and held by another one too
+    __shared__ int counts[Sizes<ONE>::PAGES], len_held[ONE ? Sizes<ONE>::B : 1], parent_held[ONE ? Sizes<ONE>::B : 1];
+    __shared__ int waves[THREADS / 64];
     const int tid = threadIdx.x, page1 = (1 << a.page_log2) - 1;
     const int64_t capacity = a.max_pages << a.page_log2;
     const int head = a.free_in[0], count = a.free_in[1];
     const bool lead = blockIdx.x == 0;
-    for (int b = tid; b < a.B; b += kThreads) n_child[b] = 0, first_child[b] = a.B;
+    auto len_of = [&](int b) { return ONE ? len_held[b] : a.kv_len[b]; };
+    auto parent_of = [&](int b) { return ONE ? parent_held[b] : a.parent[b]; };
+    auto pages_of = [&](int L) { return (int)(((int64_t)L + page1) >> a.page_log2); };
+    for (int b = tid; b < a.B; b += THREADS) {
+        n_child[b] = 0, first_child[b] = a.B;
+        if constexpr (ONE) len_held[b] = a.kv_len[b], parent_held[b] = a.parent[b];
+    }
+    if constexpr (ONE)
+        for (int i = tid; i < a.n_pages; i += THREADS) counts[i] = max(a.shared[i], 0);
     __syncthreads();
     bool bad = head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages;
-    for (int b = tid; b < a.B; b += kThreads) {
-        const int p = a.parent[b], L = a.kv_len[b];
-        bad |= p < -1 || p >= a.B || L < 0 || L > capacity;
+    for (int b = tid; b < a.B; b += THREADS) {
+        const int p = parent_of(b), L = len_of(b);
+        const bool wrong = L < 0 || L > capacity;
+        bad |= p < -1 || p >= a.B || wrong;
         if (p >= 0 && p < a.B) {
             atomicAdd(&n_child[p], 1);
             atomicMin(&first_child[p], b);
         }
+        int e = 0;
+        if (!wrong && (L & page1)) {
+            const int id = a.table[(int64_t)b * a.max_pages + pages_of(L) - 1];
+            e = (unsigned)id < (unsigned)a.n_pages && (ONE ? counts : a.shared)[id] > 0 ? 2 : 1;
+        }
+        end[b] = (uint8_t)e;
     }
     bad = __syncthreads_or(bad);
-    auto pages_of = [&](int L) { return (int)(((int64_t)L + page1) >> a.page_log2); };
-    // the page that a request's length ends in, if partly filled: does somebody else hold it too?
-    auto joint = [&](int b, int L) {
-        const int id = a.table[(int64_t)b * a.max_pages + pages_of(L) - 1];
-        return (unsigned)id < (unsigned)a.n_pages && a.shared[id] > 0;
-    };
     int need = 0;
     if (!bad)
-        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-            const int b = b0 + tid;
-            int copied = 0;
-            if (b < a.B) {
-                const int p = a.parent[b], L = p >= 0 ? a.kv_len[p] : 0;
-                copied = (L & page1) && (b != first_child[p] || joint(p, L));
-            }
+        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+            const int b = b0 + tid, p = b < a.B ? parent_of(b) : -1;
+            const int copied = p >= 0 && end[p] && (b != first_child[p] || end[p] == 2);
             int total;
-            const int before = block_scan<kThreads>(copied, waves, total);
+            const int before = block_scan<THREADS>(copied, waves, total);
             if (b < a.B) copy_at[b] = copied ? need + before : -1;
             need += total;
         }
     __syncthreads();
     const bool go = !bad && need <= count;
+    const int head_out = go ? ring_at(head, need, a.n_pages) : head, left = go ? count - need : count;
     if (lead && tid == 0) {
         *a.status = bad ? -1 : go ? 0 : need - count;
-        a.free_out[0] = go ? ring_at(head, need, a.n_pages) : head;
-        a.free_out[1] = go ? count - need : count;             // the pages given back come on top
+        a.free_out[0] = head_out;
+        a.free_out[1] = left;                                  // the pages given back come on top
     }
     if (lead)
-        for (int b = tid; b < a.B; b += kThreads) {
-            const int p = go ? a.parent[b] : b, L = p >= 0 ? a.kv_len[p] : 0;
+        for (int b = tid; b < a.B; b += THREADS) {
+            const int p = go ? parent_of(b) : b, L = p >= 0 ? len_of(p) : 0;
             const bool copied = go && copy_at[b] >= 0;
             a.kv_len_out[b] = L;
             a.copy_src[b] = copied ? a.table[(int64_t)p * a.max_pages + pages_of(L) - 1] : -1;
             a.copy_dst[b] = copied ? a.ring[ring_at(head, copy_at[b], a.n_pages)] : -1;
         }
-    const int64_t chunks = (a.max_pages + kThreads - 1) / kThreads;
-    for (int64_t item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
-        const int b = (int)(item / chunks), j = (int)(item % chunks) * kThreads + tid;
+    over_table<ONE>(a.B, a.max_pages, [&](int b, int j) {
         // its pages after the call
-        const int p = go ? a.parent[b] : b;
+        const int p = go ? parent_of(b) : b;
         if (p >= 0) {
-            const int L = max(a.kv_len[p], 0), n = (int)min((int64_t)pages_of(L), a.max_pages);
+            const int L = max(len_of(p), 0), n = (int)min((int64_t)pages_of(L), a.max_pages);
             if (j < n) {
                 const int at = go && j == n - 1 ? copy_at[b] : -1;
                 a.table_out[(int64_t)b * a.max_pages + j] = at >= 0 ? a.ring[ring_at(head, at, a.n_pages)] : a.table[(int64_t)p * a.max_pages + j];
             }
         }
-        if (!go) continue;
+        if (!go) return;
         // the holders of its pages before the call: every copy is one, itself no longer
-        const int L = a.kv_len[b], n = pages_of(L), more = n_child[b] - 1;
+        const int L = len_of(b), n = pages_of(L), more = n_child[b] - 1;
         if (j < n) {
-            const int change = j < L >> a.page_log2 ? more : more < 0 || joint(b, L) ? -1 : 0;
+            const int change = j < L >> a.page_log2 ? more : more < 0 || end[b] == 2 ? -1 : 0;
             const int id = change ? a.table[(int64_t)b * a.max_pages + j] : -1;
-            if ((unsigned)id < (unsigned)a.n_pages) atomicAdd(a.shared_out + id, change);
+            if ((unsigned)id < (unsigned)a.n_pages) atomicAdd((ONE ? counts : a.shared_out) + id, change);
         }
+    });
+    if constexpr (ONE) {
+        __syncthreads();
+        const int given = give_back<THREADS>(counts, a.shared_out, a.n_pages, a.ring, a.n_pages, (int64_t)head_out + left, waves);
+        if (tid == 0) a.free_out[1] = go ? min(left + given, a.n_pages) : left;
     }
-}
-
-// Pages whose count fell below 0 go behind the free ones, in the order of their numbers.  free_out: {head, free pages so far}.
-__global__ __launch_bounds__(1024) void kv_give_back_kernel(int32_t *shared, int32_t *ring, int32_t *free_out, int n_pages) {
-    __shared__ int waves[16];
-    const int tid = threadIdx.x, head = free_out[0], count = free_out[1];
-    if (head < 0 || head >= n_pages || count < 0 || count > n_pages) return;     // a refused step: nothing has changed
-    int given = 0;
-    for (int i0 = 0; i0 < n_pages; i0 += 4096) {
-        const int i = i0 + tid * 4;
-        bool gone[4];
-        int mine = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) gone[k] = i + k < n_pages && shared[i + k] < 0, mine += gone[k];
-        int total;
-        int at = given + block_scan<1024>(mine, waves, total);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (gone[k]) {
-                ring[(int)(((int64_t)head + count + at++) % n_pages)] = i + k;
-                shared[i + k] = 0;
-            }
-        given += total;
-    }
-    if (tid == 0) free_out[1] = min(count + given, n_pages);
 }
 
 // ---------------------------------------------------------------- requests that lose tokens
 struct CompactArgs {
-    const int32_t *kv_len, *stay, *cu, *keep, *table, *shared, *ring, *free_in;
-    int32_t *kv_len_out, *table_out, *shared_out, *moves, *free_out, *status;
+    const int32_t *kv_len, *stay, *cu, *keep, *table, *shared, *free_in;
+    int32_t *ring, *kv_len_out, *table_out, *shared_out, *moves, *free_out, *status;
     int64_t max_pages, N;
     int B, page_log2, n_pages;
     int32_t *checked;                 // AGQ_KV_CHECKS words behind the new pages in `moves`
 };
 
-// the holders' counts, and whether the listed tokens ascend inside their requests
-__global__ __launch_bounds__(kThreads) void kv_compact_check_kernel(const CompactArgs a) {
+// do the listed tokens ascend inside their requests?  (cu in LDS)
+__device__ __forceinline__ bool listed_wrongly(const CompactArgs &a, const int *cu, int64_t i) {
+    const int b = find_row(cu, a.B, (int)i);
+    if (i < cu[b] || i >= cu[b + 1]) return false;         // of no request
+    const int x = a.keep[i];
+    return x >= a.kv_len[b] || x < a.stay[b] || (i > cu[b] && x <= a.keep[i - 1]);
+}
+
+// the holders' counts, and the check
+__global__ __launch_bounds__(512) void kv_compact_check_kernel(const CompactArgs a) {
     __shared__ int cu[kMaxB + 1];
     const int tid = threadIdx.x;
-    for (int i = blockIdx.x * kThreads + tid; i < a.n_pages; i += gridDim.x * kThreads) a.shared_out[i] = max(a.shared[i], 0);
-    for (int b = tid; b <= a.B; b += kThreads) cu[b] = a.cu[b];
+    for (int i = blockIdx.x * 512 + tid; i < a.n_pages; i += gridDim.x * 512) a.shared_out[i] = max(a.shared[i], 0);
+    for (int b = tid; b <= a.B; b += 512) cu[b] = a.cu[b];
     __syncthreads();
     bool bad = false;
     if (a.B > 0)
-        for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < a.N; i += (int64_t)gridDim.x * kThreads) {
-            const int b = find_row(cu, a.B, (int)i);
-            if (i < cu[b] || i >= cu[b + 1]) continue;         // of no request
-            const int x = a.keep[i];
-            bad |= x >= a.kv_len[b] || x < a.stay[b] || (i > cu[b] && x <= a.keep[i - 1]);
-        }
+        for (int64_t i = (int64_t)blockIdx.x * 512 + tid; i < a.N; i += (int64_t)gridDim.x * 512) bad |= listed_wrongly(a, cu, i);
     bad = __syncthreads_or(bad);
     if (tid == 0) a.checked[blockIdx.x] = bad;
 }
 
-__global__ __launch_bounds__(kThreads) void kv_compact_kernel(const CompactArgs a, int checked) {
-    __shared__ int need_at[kMaxB], same_of[kMaxB], after_of[kMaxB];      // taken pages before, pages that stay, length after
-    __shared__ int waves[kThreads / 64];
+template <bool ONE>
+__global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_compact_kernel(const CompactArgs a, int checked) {
+    constexpr int THREADS = Sizes<ONE>::THREADS;
+    __shared__ int need_at[Sizes<ONE>::B + 1], same_of[Sizes<ONE>::B], after_of[Sizes<ONE>::B];  // taken pages before, pages that stay, length after
+    __shared__ int counts[Sizes<ONE>::PAGES];
+    __shared__ int waves[THREADS / 64];
     const int tid = threadIdx.x, page1 = (1 << a.page_log2) - 1;
     const int64_t capacity = a.max_pages << a.page_log2;
     const int head = a.free_in[0], count = a.free_in[1];
     const bool lead = blockIdx.x == 0;
     bool bad = head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages;
-    if (tid < checked) bad |= a.checked[tid] != 0;
-    for (int b = tid; b < a.B; b += kThreads) {
+    if constexpr (ONE) {
+        for (int i = tid; i < a.n_pages; i += THREADS) counts[i] = max(a.shared[i], 0);
+        for (int b = tid; b <= a.B; b += THREADS) need_at[b] = a.cu[b];          // for the check
+        __syncthreads();
+        if (a.B > 0)
+            for (int64_t i = tid; i < a.N; i += THREADS) bad |= listed_wrongly(a, need_at, i);
+    } else if (tid < checked) {
+        bad |= a.checked[tid] != 0;
+    }
+    for (int b = tid; b < a.B; b += THREADS) {
         const int L = a.kv_len[b], c0 = a.cu[b], c1 = a.cu[b + 1];
         bad |= L < 0 || L > capacity || a.stay[b] < 0 || c0 < 0 || c1 < c0 || c1 > a.N;
     }
@@ -203,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void kv_compact_kernel(const CompactArgs 
     auto pages_of = [&](int L) { return (int)(((int64_t)L + page1) >> a.page_log2); };
     int need = 0;
     if (!bad)
-        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
             const int b = b0 + tid;
             int mine = 0;
             if (b < a.B) {
@@ -217,23 +268,22 @@ __global__ __launch_bounds__(kThreads) void kv_compact_kernel(const CompactArgs 
                 same_of[b] = same, after_of[b] = after;
             }
             int total;
-            const int before = block_scan<kThreads>(mine, waves, total);
+            const int before = block_scan<THREADS>(mine, waves, total);
             if (b < a.B) need_at[b] = need + before;
             need += total;
         }
     __syncthreads();
     const bool go = !bad && need <= count;
+    const int head_out = go ? ring_at(head, need, a.n_pages) : head, left = go ? count - need : count;
     if (lead && tid == 0) {
         *a.status = bad ? -1 : go ? 0 : need - count;
-        a.free_out[0] = go ? ring_at(head, need, a.n_pages) : head;
-        a.free_out[1] = go ? count - need : count;             // the pages given back come on top
+        a.free_out[0] = head_out;
+        a.free_out[1] = left;                                  // the pages given back come on top
         a.moves[0] = go ? need : 0;
     }
     if (lead)
-        for (int b = tid; b < a.B; b += kThreads) a.kv_len_out[b] = go ? after_of[b] : a.kv_len[b];
-    const int64_t chunks = (a.max_pages + kThreads - 1) / kThreads;
-    for (int64_t item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
-        const int b = (int)(item / chunks), j = (int)(item % chunks) * kThreads + tid;
+        for (int b = tid; b < a.B; b += THREADS) a.kv_len_out[b] = go ? after_of[b] : a.kv_len[b];
+    over_table<ONE>(a.B, a.max_pages, [&](int b, int j) {
         const int held = (int)min((int64_t)pages_of(max(a.kv_len[b], 0)), a.max_pages);
         const int same = go ? same_of[b] : held, after = go ? after_of[b] : 0, total = go ? pages_of(after) : held;
         const int old = j < held ? a.table[(int64_t)b * a.max_pages + j] : -1;
@@ -246,7 +296,12 @@ __global__ __launch_bounds__(kThreads) void kv_compact_kernel(const CompactArgs 
             }
             a.table_out[(int64_t)b * a.max_pages + j] = id;
         }
-        if (j >= same && (unsigned)old < (unsigned)a.n_pages) atomicAdd(a.shared_out + old, -1);
+        if (j >= same && (unsigned)old < (unsigned)a.n_pages) atomicAdd((ONE ? counts : a.shared_out) + old, -1);
+    });
+    if constexpr (ONE) {
+        __syncthreads();
+        const int given = give_back<THREADS>(counts, a.shared_out, a.n_pages, a.ring, a.n_pages, (int64_t)head_out + left, waves);
+        if (tid == 0) a.free_out[1] = go ? min(left + given, a.n_pages) : left;
     }
 }
 
@@ -440,11 +495,15 @@ unsigned at_most(int64_t n, int64_t most) { return (unsigned)(n < 1 ? 1 : n > mo
 
 int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy_src, int32_t *copy_dst, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    const ForkArgs a = {p.kv_len, parent, p.table, p.shared, p.ring, p.free_in, p.kv_len_out, p.table_out, p.shared_out, copy_src, copy_dst, p.free_out,
+    const ForkArgs a = {p.kv_len, parent, p.table, p.shared, p.free_in, p.ring, p.kv_len_out, p.table_out, p.shared_out, copy_src, copy_dst, p.free_out,
                         p.status, p.max_pages, (int)p.B, log2_of(p.page), (int)p.n_pages};
+    if (agq_kv_one(p.B, p.max_pages, p.n_pages, 0)) {
+        kv_fork_kernel<true><<<1, 1024, 0, st>>>(a);
+        return (int)hipGetLastError();
+    }
     shared_copy_kernel<<<at_most((p.n_pages + 255) / 256, 256), 256, 0, st>>>(p.shared, p.shared_out, (int)p.n_pages);
     if (int err = (int)hipGetLastError()) return err;
-    kv_fork_kernel<<<at_most(p.B * ((p.max_pages + kThreads - 1) / kThreads), 256), kThreads, 0, st>>>(a);
+    kv_fork_kernel<false><<<at_most(p.B * ((p.max_pages + 511) / 512), 256), 512, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
     kv_give_back_kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
     return (int)hipGetLastError();
@@ -452,14 +511,18 @@ int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy
 
 int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int32_t *moves, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    const CompactArgs a = {p.kv_len, stay, cu, keep, p.table, p.shared, p.ring, p.free_in, p.kv_len_out, p.table_out, p.shared_out, moves, p.free_out,
+    const CompactArgs a = {p.kv_len, stay, cu, keep, p.table, p.shared, p.free_in, p.ring, p.kv_len_out, p.table_out, p.shared_out, moves, p.free_out,
                            p.status, p.max_pages, N, (int)p.B, log2_of(p.page), (int)p.n_pages,
                            moves + 4 + 4 * agq_kv_new_pages(N, p.B, p.page)};
+    if (agq_kv_one(p.B, p.max_pages, p.n_pages, N)) {
+        kv_compact_kernel<true><<<1, 1024, 0, st>>>(a, 0);
+        return (int)hipGetLastError();
+    }
     const int64_t work = N > p.n_pages ? N : p.n_pages;
-    const unsigned groups = at_most((work + kThreads - 1) / kThreads, AGQ_KV_CHECKS);
-    kv_compact_check_kernel<<<groups, kThreads, 0, st>>>(a);
+    const unsigned groups = at_most((work + 511) / 512, AGQ_KV_CHECKS);
+    kv_compact_check_kernel<<<groups, 512, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
-    kv_compact_kernel<<<at_most(p.B * ((p.max_pages + kThreads - 1) / kThreads), 256), kThreads, 0, st>>>(a, (int)groups);
+    kv_compact_kernel<false><<<at_most(p.B * ((p.max_pages + 511) / 512), 256), 512, 0, st>>>(a, (int)groups);
     if (int err = (int)hipGetLastError()) return err;
     kv_give_back_kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
     return (int)hipGetLastError();

@@ -162,6 +162,7 @@ int agq_attn_kv(const agq_kv_cache *cache, const void *q, int64_t ldq, int64_t T
     return hip_status(agq_launch_attn_kv(a, s, workspace, stream));
 }
 
+static_assert(AGQ_KV_MAX_FORK == AGQ_KV_MAX_B, "the kernels hold that many requests' sums");
 // what agq_kv_fork and agq_kv_compact have in common
 static bool pages_ok(const AgqKvPages &p) {
     if (!count_ok(p.B, AGQ_KV_MAX_FORK) || !page_ok(p.page)) return false;
