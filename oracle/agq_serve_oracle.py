@@ -315,7 +315,9 @@ def logprobs(x, tokens, n_top, scale=1.0):
         if 0 <= tok < V:
             r["logprob"][t] = lp[tok]
             r["logprob_bound"][t] = 0 if np.isinf(z[tok]) else at(z[tok])
-        order = np.argsort(-(y + 0.0), kind="stable")[:n_top]
+        last = np.partition(-y, n_top - 1)[n_top - 1] if n_top else -np.inf
+        among = np.flatnonzero(-y <= last) if n_top else np.zeros(0, dtype=np.int64)
+        order = among[np.argsort(-(y[among] + 0.0), kind="stable")][:n_top]
         r["top_idx"][t], r["top_logprob"][t] = order, lp[order]
         fin = np.isfinite(z[order])
         r["top_bound"][t, fin] = at(z[order][fin])

@@ -609,9 +609,7 @@ def _ints(t, n, name):
 
 
 def _rope(rope_cos, rope_sin, pos, T, D, used):
-    """(rows, pos, cos, sin) of the rotary tables, or none of them"""
-    if rope_cos is None and rope_sin is None and pos is None:
-        return 0, None, None, None
+    """(rows, pos, cos, sin) of the rotary tables"""
     if rope_cos is None or rope_sin is None or pos is None:
         raise ValueError("rope_cos, rope_sin and pos go together")
     P = rope_cos.shape[0]
@@ -755,25 +753,39 @@ def qk_norm_rope(q, k, g_q=None, g_k=None, eps=1e-6, pos=None, rope_cos=None, ro
     if q is None and k is None:
         raise ValueError("q or k is wanted")
     T, _, D = (k if q is None else q).shape
-    used, half = [], []
-    for x, g, out, name in ((q, g_q, q_out, "q"), (k, g_k, k_out, "k")):
-        if x is None:
-            if g is not None or out is not None:
-                raise ValueError("g_%s and %s_out go with %s" % (name, name, name))
-            half.append((None, 0, 0, None, 0, None, 0, None))
-            continue
-        H = x.shape[1]
-        ld = _like(x, (T, H, D), name)
-        used.append(x)
-        if out is None:
-            out, ldo = x.new_empty(T, H, D), H * D
+    used = []
+    Hq = Hkv = ldq = ldk = ldqo = ldko = ldgq = ldgk = P = 0
+    q_p = k_p = qo_p = ko_p = gq_p = gk_p = pos_p = cos_p = sin_p = None
+    if q is not None:
+        Hq = q.shape[1]
+        ldq, q_p = _like(q, (T, Hq, D), "q"), q.data_ptr()
+        used.append(q)
+        if g_q is not None:
+            gq_p, ldgq = _gain(g_q, Hq, D, "g_q", used)
+        if q_out is None:
+            q_out, ldqo = q.new_empty(T, Hq, D), Hq * D
         else:
-            ldo = _like(out, (T, H, D), name + "_out")
-            used.append(out)
-        g_p, ldg = _gain(g, H, D, "g_" + name, used)
-        half.append((x.data_ptr(), ld, H, g_p, ldg, out.data_ptr(), ldo, out))
-    P, pos_p, cos_p, sin_p = _rope(rope_cos, rope_sin, pos, T, D, used)
-    (q_p, ldq, Hq, gq_p, ldgq, qo_p, ldqo, q_out), (k_p, ldk, Hkv, gk_p, ldgk, ko_p, ldko, k_out) = half
+            ldqo = _like(q_out, (T, Hq, D), "q_out")
+            used.append(q_out)
+        qo_p = q_out.data_ptr()
+    elif g_q is not None or q_out is not None:
+        raise ValueError("g_q and q_out go with q")
+    if k is not None:
+        Hkv = k.shape[1]
+        ldk, k_p = _like(k, (T, Hkv, D), "k"), k.data_ptr()
+        used.append(k)
+        if g_k is not None:
+            gk_p, ldgk = _gain(g_k, Hkv, D, "g_k", used)
+        if k_out is None:
+            k_out, ldko = k.new_empty(T, Hkv, D), Hkv * D
+        else:
+            ldko = _like(k_out, (T, Hkv, D), "k_out")
+            used.append(k_out)
+        ko_p = k_out.data_ptr()
+    elif g_k is not None or k_out is not None:
+        raise ValueError("g_k and k_out go with k")
+    if rope_cos is not None or rope_sin is not None or pos is not None:
+        P, pos_p, cos_p, sin_p = _rope(rope_cos, rope_sin, pos, T, D, used)
     _ok(lib().agq_qk_norm_rope(q_p, ldq, Hq, k_p, ldk, Hkv, T, D, gq_p, ldgq, gk_p, ldgk, eps, pos_p, cos_p, sin_p, P, qo_p, ldqo, ko_p, ldko,
                                _stream_of(*used)), "agq_qk_norm_rope")
     return q_out, k_out
@@ -891,10 +903,12 @@ def kv_move(layers: KvLayers, moves, block_table, stay, cu_keep, keep):
     """agq_kv_move: what kv_compact decided, in the caches of all layers; block_table is the one that kv_compact was given."""
     B, max_pages = block_table.shape
     N = keep.numel()
-    page = layers.tensors[0].shape[2] if layers.n else 16
-    _ok(lib().agq_kv_move(layers.packed, layers.n, _ints(moves, lib().agq_kv_moves_ints(N, B, page), "moves"),
+    st = _stream_of(moves, block_table, stay, cu_keep, keep, *layers.some)
+    if layers.n == 0:
+        return
+    _ok(lib().agq_kv_move(layers.packed, layers.n, _ints(moves, lib().agq_kv_moves_ints(N, B, layers.tensors[0].shape[2]), "moves"),
                           _ints(block_table, B * max_pages, "block_table"), max_pages, _ints(stay, B, "stay"), _ints(cu_keep, B + 1, "cu_keep"),
-                          _ints(keep, N, "keep"), N, B, _stream_of(moves, block_table, stay, cu_keep, keep, *layers.some)), "agq_kv_move")
+                          _ints(keep, N, "keep"), N, B, st), "agq_kv_move")
 
 
 class Logprobs(NamedTuple):
@@ -921,26 +935,44 @@ def logprobs(logits, tokens=None, n_top=0, scale=1.0, want_entropy=True, out: Lo
     kind = AGQ_LOGITS_F16 if logits.dtype is _f16 else AGQ_LOGITS_F32
     if (kind == AGQ_LOGITS_F32 and logits.dtype is not _f32) or (T and V > 1 and one != 1):
         raise ValueError("logits: fp16 or float32 [T, V] with contiguous rows is wanted")
+    if n_top < 0:
+        raise ValueError("n_top: 0 or more is wanted")
     if T <= 1:
         ld = V
+    need = lib().agq_logprobs_workspace_bytes(T, V, kind, n_top) if workspace is None else 0
+    ws_p, ws_bytes = None, 0
     if out is None:
-        e = logits.new_empty
-        out = Logprobs(None if tokens is None else e(T, dtype=_f32), e(T, dtype=_f32) if want_entropy else None,
-                       e(T, n_top, dtype=_i32) if n_top else None, e(T, n_top, dtype=_f32) if n_top else None)
-    elif (out[0] is None) != (tokens is None) or (out[1] is None) == bool(want_entropy) or (out[2] is None) != (not n_top) or (out[3] is None) != (not n_top):
-        raise ValueError("out: a tensor for each result that is asked for is wanted")
+        # one allocation, cut up: log probabilities, entropies, alternatives, and a workspace that is small
+        inside = need if need <= 65536 else 0
+        sizes = [inside >> 2, T * n_top, T * n_top, T if want_entropy else 0, T if tokens is not None else 0]
+        buf = logits.new_empty(sum(sizes), dtype=_f32)
+        ws, idx, best, entropy, logprob = buf.split_with_sizes(sizes)
+        if inside:
+            ws_p, ws_bytes = buf.data_ptr(), inside
+        out = Logprobs(logprob if tokens is not None else None, entropy if want_entropy else None, idx.view(_i32).view(T, n_top) if n_top else None,
+                       best.view(T, n_top) if n_top else None)
+        used = [buf, logits]
     else:
+        if (out[0] is None) != (tokens is None) or (out[1] is None) == bool(want_entropy) or (out[2] is None) != (not n_top) or (out[3] is None) != (not n_top):
+            raise ValueError("out: a tensor for each result that is asked for is wanted")
+        used = [logits]
         for t, shape, dtype, name in zip(out, ((T,), (T,), (T, n_top), (T, n_top)), (_f32, _f32, _i32, _f32), Logprobs._fields):
-            if t is not None and (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()):
-                raise ValueError("out.%s: a contiguous %s tensor %s is wanted" % (name, dtype, list(shape)))
-    st = _stream_of(*[t for t in (logits, tokens, *out) if t is not None])
-    if workspace is None:
-        need = lib().agq_logprobs_workspace_bytes(T, V, kind, n_top)
-        workspace = logits.new_empty(need, dtype=_i8) if need else None
-    else:
+            if t is not None:
+                if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+                    raise ValueError("out.%s: a contiguous %s tensor %s is wanted" % (name, dtype, list(shape)))
+                used.append(t)
+    if tokens is not None:
+        used.append(tokens)
+    st = _stream_of(*used)
+    if workspace is not None:
         _given(workspace, logits)
-    _ok(lib().agq_logprobs(logits.data_ptr(), kind, T, V, ld, scale, None if tokens is None else _ints(tokens, T, "tokens"), n_top, _ptr(out[0]),
-                           _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(workspace), 0 if workspace is None else workspace.nbytes, st), "agq_logprobs")
+    elif need and ws_p is None:
+        workspace = logits.new_empty(need, dtype=_i8)
+    if workspace is not None:
+        ws_p, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    logprob, entropy, idx, best = out
+    _ok(lib().agq_logprobs(logits.data_ptr(), kind, T, V, ld, scale, None if tokens is None else _ints(tokens, T, "tokens"), n_top, _ptr(logprob),
+                           _ptr(entropy), _ptr(idx), _ptr(best), ws_p, ws_bytes, st), "agq_logprobs")
     return out
 
 

@@ -515,21 +515,30 @@ struct AgqLogprobs {
     float *logprob, *entropy, *top_logprob;
     int32_t *top_idx;
 };
-// A unit is four 16-byte loads of each lane; a group is a quarter of one of them.  Rows are cut into pieces of four wavefronts
-// until there are about a thousand workgroups.  whole: one workgroup has the row and answers at once; its groups' largest
-// logits fit the LDS.
+// A unit is four 16-byte loads of each lane; a group is a quarter of one of them.  A row is one workgroup's (its groups' largest
+// logits in LDS, the answers in the same launch), or is cut into pieces of four wavefronts until there are about a thousand
+// workgroups, which a second launch joins.  Measured in a replayed graph, pieces against whole rows of sixteen wavefronts, 0 and 20
+// alternatives:
+//   a unit to a wavefront or less: whole (fp16, 1 x 32000 5.7, 13.3 and 4.8, 13.6 us; 64 x 16000 6.0, 14.1 and 4.5, 13.1; 256 x 32000
+//     8.2, 17.1 and 5.9, 15.3), as the host takes 3 us for a launch
+//   more of them: pieces, as one CU reads a row slowly (1 x 128000 5.6, 14.4 and 10.3, 21.0; 64 x 128000 7.7, 17.3 and 11.0, 22.2;
+//     500 x 128000 26.3, 37.8 and 27.0, 42.3), but for one row to each of most CUs (256 x 128000 16.9, 27.3 and 15.5, 25.7; float32,
+//     256 x 50000 13.7, 21.3 and 9.8, 16.9)
+//   more than 512 rows: whole, with four wavefronts (1024 x 32000 15.6, 24.4; pieces 18.2, 27.9 and sixteen 19.2, 33.7 for 1000)
 #define AGQ_LP_LOADS 4
 #define AGQ_LP_HELD 2048
 struct AgqLpPlan {
-    int units, wave_units, pieces, groups;
+    int units, wave_units, pieces, groups, waves;
     bool whole;
 };
 static inline AgqLpPlan agq_lp_plan(int64_t T, int64_t V, int kind, int64_t n_top) {
-    const int64_t values = AGQ_LP_LOADS * 64 * (kind ? 4 : 8), units = (V + values - 1) / values, quads = (units + 3) / 4;
-    const int64_t want = T >= 1024 ? 1 : T > 0 ? 1024 / T : 1, each = (quads + want - 1) / want;
+    const int64_t values = AGQ_LP_LOADS * 64 * (kind ? 4 : 8), units = (V + values - 1) / values;
     AgqLpPlan p;
-    p.units = (int)units, p.wave_units = (int)each, p.pieces = (int)((quads + each - 1) / each), p.groups = (int)units * AGQ_LP_LOADS * 4;
-    p.whole = p.pieces == 1 && (n_top == 0 || p.groups <= AGQ_LP_HELD);
+    p.units = (int)units, p.groups = (int)units * AGQ_LP_LOADS * 4;
+    p.whole = (p.groups <= AGQ_LP_HELD || n_top == 0) && (units <= 16 || T > 512 || (T > 128 && T <= 256));
+    p.waves = p.whole && T <= 512 && units > 4 ? 16 : 4;
+    const int64_t parts = (units + p.waves - 1) / p.waves, want = p.whole || T > 512 ? 1 : T > 0 ? 1024 / T : 1, each = (parts + want - 1) / want;
+    p.wave_units = (int)each, p.pieces = (int)((parts + each - 1) / each);
     return p;
 }
 size_t agq_logprobs_workspace(int64_t T, int64_t V, int kind, int64_t n_top);

@@ -70,24 +70,55 @@ __device__ __forceinline__ void over_table(int B, int64_t max_pages, F f) {
     }
 }
 
-// Pages whose count fell below 0 go behind the free ones, in the order of their numbers: n counts from number `first` on, of
-// which they are the `given`-th and following.  The counts are written to out, 0 for those.
-template <int THREADS>
-__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n, int32_t *ring, int n_pages, int64_t behind, int *waves) {
+// Pages whose count fell below 0 go behind the free ones (`behind`, below 2 n_pages), in the order of their numbers; their number.
+// The counts are written to out, 0 for those.  A thread has four neighbours of each of TILES tiles at once, whose loads are on
+// their way before the first is looked at (a million pages in memory 240 us, 450 without; one tile where they are in LDS).
+template <int THREADS, int TILES>
+__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n_pages, int32_t *ring, int64_t behind) {
+    constexpr int WAVES = THREADS / 64, TILE = 4 * THREADS;
+    __shared__ int waves[TILES][WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t first = (uint32_t)(behind >= n_pages ? behind - n_pages : behind);
     int given = 0;
-    for (int i0 = 0; i0 < n; i0 += 4 * THREADS) {
-        const int i = i0 + threadIdx.x * 4;
-        int c[4], mine = 0;
+#pragma unroll 1
+    for (int64_t i0 = 0; i0 < n_pages; i0 += TILES * TILE) {
+        int c[TILES][4], up[TILES];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) c[k] = i + k < n ? counts[i + k] : 0, mine += c[k] < 0;
-        int total;
-        int at = given + block_scan<THREADS>(mine, waves, total);
+        for (int k = 0; k < TILES; ++k) {
+            const int64_t i = i0 + k * TILE + threadIdx.x * 4;
+            if (i + 4 <= n_pages) {
+                __builtin_memcpy(c[k], counts + i, 16);
+            } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (c[k] < 0) ring[(int)((behind + at++) % n_pages)] = i + k;
-            if (i + k < n && (c[k] < 0 || out != counts)) out[i + k] = max(c[k], 0);
+                for (int j = 0; j < 4; ++j) c[k][j] = i + j < n_pages ? counts[i + j] : 0;
+            }
         }
-        given += total;
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) up[k] = agq_wave_scan((c[k][0] < 0) + (c[k][1] < 0) + (c[k][2] < 0) + (c[k][3] < 0));
+        __syncthreads();
+        if (lane == 63)
+#pragma unroll
+            for (int k = 0; k < TILES; ++k) waves[k][wave] = up[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) {
+            const int64_t i = i0 + k * TILE + threadIdx.x * 4;
+            int at = given + up[k] - ((c[k][0] < 0) + (c[k][1] < 0) + (c[k][2] < 0) + (c[k][3] < 0));
+#pragma unroll 4
+            for (int w = 0; w < WAVES; ++w) {
+                const int x = waves[k][w];
+                at += w < wave ? x : 0;
+                given += x;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (c[k][j] < 0) {
+                    const uint32_t r = first + (uint32_t)at++;
+                    ring[r >= (uint32_t)n_pages ? r - (uint32_t)n_pages : r] = (int)i + j;
+                }
+                if (i + j < n_pages && (c[k][j] < 0 || out != counts)) out[i + j] = max(c[k][j], 0);
+            }
+        }
     }
     return given;
 }
@@ -98,10 +129,9 @@ __global__ __launch_bounds__(256) void shared_copy_kernel(const int32_t *shared,
 
 // free_out: {head, free pages so far}
 __global__ __launch_bounds__(1024) void kv_give_back_kernel(int32_t *shared, int32_t *ring, int32_t *free_out, int n_pages) {
-    __shared__ int waves[16];
     const int head = free_out[0], count = free_out[1];
     if (head < 0 || head >= n_pages || count < 0 || count > n_pages) return;     // a refused step: nothing has changed
-    const int given = give_back<1024>(shared, shared, n_pages, ring, n_pages, (int64_t)head + count, waves);
+    const int given = give_back<1024, 4>(shared, shared, n_pages, ring, (int64_t)head + count);
     if (threadIdx.x == 0) free_out[1] = min(count + given, n_pages);
 }
 
@@ -190,7 +220,7 @@ __global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_fork_kernel(const Fork
     });
     if constexpr (ONE) {
         __syncthreads();
-        const int given = give_back<THREADS>(counts, a.shared_out, a.n_pages, a.ring, a.n_pages, (int64_t)head_out + left, waves);
+        const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, (int64_t)head_out + left);
         if (tid == 0) a.free_out[1] = go ? min(left + given, a.n_pages) : left;
     }
 }
@@ -300,7 +330,7 @@ __global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_compact_kernel(const C
     });
     if constexpr (ONE) {
         __syncthreads();
-        const int given = give_back<THREADS>(counts, a.shared_out, a.n_pages, a.ring, a.n_pages, (int64_t)head_out + left, waves);
+        const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, (int64_t)head_out + left);
         if (tid == 0) a.free_out[1] = go ? min(left + given, a.n_pages) : left;
     }
 }

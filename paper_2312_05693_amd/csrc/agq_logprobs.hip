@@ -393,11 +393,11 @@ __device__ __forceinline__ void answer(const Args &a, int64_t t, const E *x, con
     }
 }
 
-// A workgroup to a piece of a row: wave_units units of each of its four wavefronts.  WHOLE: the piece is the row, and the
-// answers follow here.
-template <class E, bool TOP, bool WHOLE>
-__global__ __launch_bounds__(256) void logprobs_kernel(const Args a) {
-    __shared__ Row rows[4];
+// A workgroup to a piece of a row: wave_units units of each of its wavefronts.  WHOLE: the piece is the row, and the answers
+// follow here.
+template <class E, bool TOP, bool WHOLE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(const Args a) {
+    __shared__ Row rows[WAVES];
     __shared__ int held[WHOLE && TOP ? AGQ_LP_HELD : 1];
     __shared__ Scratch sc;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const Args a) {
     const float c = a.scale * kLog2e;
     int *tops = WHOLE ? held : a.tops + t * a.groups;
     Sums s = {-3.402823466e38f, 0.0f, 0.0f};
-    const int u0 = (piece * 4 + wave) * a.wave_units, u1 = min(u0 + a.wave_units, a.units);
+    const int u0 = (piece * WAVES + wave) * a.wave_units, u1 = min(u0 + a.wave_units, a.units);
     if (u0 < u1) {
         Unit<E> next = load_unit(x, a.V, u0, lane);
         for (int u = u0; u < u1; ++u) {
@@ -420,7 +420,12 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const Args a) {
     if (lane == 63) rows[wave] = r;
     __syncthreads();
     if (wave > 0) return;
-    r = joined(joined(rows[0], rows[1], c), joined(rows[2], rows[3], c), c);
+    if constexpr (WAVES == 4) {
+        r = joined(joined(rows[0], rows[1], c), joined(rows[2], rows[3], c), c);
+    } else {
+        r = wave_joined(lane < WAVES ? rows[lane] : Row{0.0, 0.0, -3.402823466e38f}, c);
+        r.S = lane_63(r.S), r.E = lane_63(r.E);
+    }
     if constexpr (WHOLE) {
         answer<E, TOP>(a, t, x, r, tops, sc, lane);
     } else if (lane == 0) {
@@ -445,25 +450,19 @@ __global__ __launch_bounds__(64) void join_kernel(const Args a) {
     answer<E, TOP>(a, t, (const E *)a.logits + t * a.ld, r, a.tops + t * a.groups, sc, lane);
 }
 
-template <class E>
-int launch(const Args &a, int64_t T, bool whole, hipStream_t st) {
-    const dim3 grid((unsigned)(T * a.pieces));
-    if (whole) {
-        if (a.n_top)
-            logprobs_kernel<E, true, true><<<grid, 256, 0, st>>>(a);
+template <class E, bool TOP>
+int launch(const Args &a, int64_t T, const AgqLpPlan &p, hipStream_t st) {
+    const dim3 grid((unsigned)(T * p.pieces));
+    if (p.whole) {
+        if (p.waves == 16)
+            logprobs_kernel<E, TOP, true, 16><<<grid, 1024, 0, st>>>(a);
         else
-            logprobs_kernel<E, false, true><<<grid, 256, 0, st>>>(a);
+            logprobs_kernel<E, TOP, true, 4><<<grid, 256, 0, st>>>(a);
         return (int)hipGetLastError();
     }
-    if (a.n_top)
-        logprobs_kernel<E, true, false><<<grid, 256, 0, st>>>(a);
-    else
-        logprobs_kernel<E, false, false><<<grid, 256, 0, st>>>(a);
+    logprobs_kernel<E, TOP, false, 4><<<grid, 256, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
-    if (a.n_top)
-        join_kernel<E, true><<<dim3((unsigned)T), 64, 0, st>>>(a);
-    else
-        join_kernel<E, false><<<dim3((unsigned)T), 64, 0, st>>>(a);
+    join_kernel<E, TOP><<<dim3((unsigned)T), 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -479,5 +478,7 @@ int agq_launch_logprobs(const AgqLogprobs &p, void *workspace, void *stream) {
     Part *parts = (Part *)workspace;
     const Args a = {p.logits, p.ld, (int)p.V, (int)p.n_top, plan.units, plan.wave_units, plan.pieces, plan.groups, p.scale, p.tokens, p.logprob, p.entropy,
                     p.top_logprob, p.top_idx, parts, plan.whole ? nullptr : (int32_t *)(parts + p.T * plan.pieces)};
-    return p.kind ? launch<float>(a, p.T, plan.whole, (hipStream_t)stream) : launch<_Float16>(a, p.T, plan.whole, (hipStream_t)stream);
+    hipStream_t st = (hipStream_t)stream;
+    if (p.kind) return p.n_top ? launch<float, true>(a, p.T, plan, st) : launch<float, false>(a, p.T, plan, st);
+    return p.n_top ? launch<_Float16, true>(a, p.T, plan, st) : launch<_Float16, false>(a, p.T, plan, st);
 }

@@ -65,7 +65,7 @@ def test_sizes(agq, kind, V, T, n_top):
 
 @pytest.mark.parametrize("kind", ["fp16", "fp32"])
 @pytest.mark.parametrize("T,V,n_top", [(1, 131072, 20), (5, 128000, 64), (40, 50001, 8), (300, 4001, 10), (1500, 1000, 3), (700, 32000, 20),
-                                       (2, 1 << 20, 33)])
+                                       (2, 1 << 20, 33), (200, 70001, 20), (256, 128000, 0), (130, 300001, 7), (600, 300001, 2), (257, 32769, 64)])
 def test_large(agq, kind, T, V, n_top):
     r = np.random.default_rng([V, T])
     check(agq, draw(r, T, V, kind), r.integers(0, V, T), n_top)
