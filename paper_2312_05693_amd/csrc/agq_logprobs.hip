@@ -6,7 +6,7 @@
 // and the entropy ln S - E / S (scale / c), of the row's joined sums in float64.
 // The pass also leaves the largest logit of every group of neighbours (256 bytes of them: sixteen lanes' loads).  The n_top
 // likeliest tokens lie in the n_top groups with the largest of these, equal ones by their place: any other token has one at
-// least as good in front of it in each of those.  So only some groups are looked at again, by one wavefront.
+// least as good in front of it in each of those.  So only some groups are looked at again.
 #include <limits.h>
 #include "agq_device.h"
 #include "agq_internal.h"
@@ -210,11 +210,15 @@ __device__ __forceinline__ double lane_63(double v) {
     return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)u, 63));
 }
 
-// ---------------------------------------------------------------- the likeliest tokens, by one wavefront
+// ---------------------------------------------------------------- the likeliest tokens, by four wavefronts
 constexpr int kBlock = 16;       // groups' largest logits that a lane holds at once
-constexpr int kAtOnce = 16;      // groups that are looked at together
+constexpr int kAtOnce = 4;       // groups that a wavefront looks at together
+constexpr int kWaiting = 64 + 128 * kAtOnce;
 struct Scratch {
-    Key waiting[64 + 128 * kAtOnce];      // of groups or tokens that are not in the list yet; kBlock * 64 is less
+    Key waiting[4 * kWaiting];   // of tokens that are not in a list yet, a quarter to each wavefront; before that of groups
+    Key best[4][64];             // the wavefronts' lists
+    int group[64], picked;       // groups to be looked at
+    Key cut;
 };
 
 // the key of lane ^ X, by data-parallel moves
@@ -298,10 +302,9 @@ struct Best {
     }
 };
 
-// lane i < n gets the i-th best token's key
+// The first wavefront finds the groups.
 template <class E>
-__device__ __forceinline__ Key likeliest(const E *x, int V, const int *tops, int groups, int n, Scratch &sc, int lane) {
-    constexpr int G = 16 * Vec<E>::N, PER = G / 64;
+__device__ __forceinline__ void find_groups(const int *tops, int groups, int n, Scratch &sc, int lane) {
     // every lane's best group; the n-th best of these lets the n best groups and few others through
     int top[kBlock];
     auto load_tops = [&](int g0) {
@@ -340,56 +343,86 @@ __device__ __forceinline__ Key likeliest(const E *x, int V, const int *tops, int
     int picked = g.waiting;
     Key least = bound;
     if (picked > 0) {
-        g.list = lane < picked ? sc.waiting[lane] : 0;
+        g.list = lane < picked ? g.wait[lane] : 0;
     } else {
         picked = n;
         least = lane_key(g.list, n - 1);
     }
-    const int group = (int)~(uint32_t)g.list;
-    // their tokens, from those on that are as large as the n-th group's largest
-    Best b = {0, least & ~(Key)0xFFFFFFFFu, 0, n, lane, sc.waiting};
-    g.fence();
-#pragma unroll 1
-    for (int p0 = 0; p0 < picked; p0 += kAtOnce) {
-        E v[kAtOnce][PER];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const int at = (p0 + i < picked ? __builtin_amdgcn_readlane(group, p0 + i) : 0) * G + lane;
-#pragma unroll
-            for (int k = 0; k < PER; ++k) v[i][k] = x[min(at + 64 * k, V - 1)];
-        }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (p0 + i >= picked) break;
-            const int at = __builtin_amdgcn_readlane(group, p0 + i) * G + lane;
-#pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                const Key key = key_of(order((float)v[i][k]), (uint32_t)(at + 64 * k));
-                b.add(key, at + 64 * k < V && key > b.cut);
-            }
-        }
-        b.merge(p0 + kAtOnce >= picked);
-    }
-    return b.list;
+    sc.group[lane] = (int)~(uint32_t)g.list;
+    if (lane == 0) sc.picked = picked, sc.cut = least & ~(Key)0xFFFFFFFFu;       // tokens as large as the n-th group's largest
 }
 
-// what is asked for of a row, by one wavefront
-template <class E, bool TOP>
-__device__ __forceinline__ void answer(const Args &a, int64_t t, const E *x, const Row &r, const int *tops, Scratch &sc, int lane) {
-    const bool none = !(r.S > 0.0);        // no distribution: a NaN, or +infinity (less itself), made it one; -infinity only, 0
-    const double nan = __builtin_nan(""), lse = none ? nan : log(r.S), scale = (double)a.scale;
-    if (lane == 0) {
-        if (a.logprob) {
-            const int v = a.tokens[t];
-            a.logprob[t] = (float)((unsigned)v < (unsigned)a.V ? ((double)(float)x[v] - (double)r.m) * scale - lse : nan);
+// Each of four wavefronts looks at a quarter of them; the first one joins what they found.  Lane i < n of it gets the i-th best
+// token's key.  Called by the whole workgroup, behind a barrier.
+template <class E>
+__device__ __forceinline__ Key likeliest(const E *x, int V, int n, Scratch &sc, int wave, int lane) {
+    constexpr int G = 16 * Vec<E>::N, PER = G / 64;
+    static_assert(4 * kWaiting >= 64 + 64 * kBlock, "a block of groups may wait");
+    if (wave < 4) {
+        const int picked = sc.picked;
+        Best b = {0, sc.cut, 0, n, lane, sc.waiting + wave * kWaiting};
+#pragma unroll 1
+        for (int p0 = wave; p0 < picked; p0 += 4 * kAtOnce) {
+            E v[kAtOnce][PER];
+            int at[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                at[i] = p0 + 4 * i < picked ? __builtin_amdgcn_readfirstlane(sc.group[p0 + 4 * i]) * G + lane : V;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) v[i][k] = x[min(at[i] + 64 * k, V - 1)];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) {
+                    const Key key = key_of(order((float)v[i][k]), (uint32_t)(at[i] + 64 * k));
+                    b.add(key, at[i] + 64 * k < V && key > b.cut);
+                }
+            b.merge(p0 + 4 * kAtOnce >= picked);
         }
-        if (a.entropy) a.entropy[t] = (float)(lse - r.E / r.S * (scale / (double)(a.scale * kLog2e)));
+        sc.best[wave][lane] = b.list;
     }
-    if constexpr (!TOP) return;
-    const Key k = none ? 0 : likeliest<E>(x, a.V, tops, a.groups, a.n_top, sc, lane);
-    if (lane < a.n_top) {
-        a.top_idx[t * a.n_top + lane] = none ? -1 : (int)~(uint32_t)k;
-        a.top_logprob[t * a.n_top + lane] = (float)(((double)number((int)((uint32_t)(k >> 32) ^ 0x80000000u)) - (double)r.m) * scale - lse);
+    __syncthreads();
+    Key list = 0;
+    if (wave == 0) {
+        list = sc.best[0][lane];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) list = merged(list, sc.best[w][63 - lane], lane);
+    }
+    return list;
+}
+
+// What is asked for of a row, by a workgroup.  r and tops are the first wavefront's.
+template <class E, bool TOP>
+__device__ __forceinline__ void answer(const Args &a, int64_t t, const E *x, const Row &r, const int *tops, Scratch &sc, int wave, int lane) {
+    const double scale = (double)a.scale;
+    double lse = 0.0;
+    if (wave == 0) {
+        const bool none = !(r.S > 0.0);    // no distribution: a NaN, or +infinity (less itself), made it one; -infinity only, 0
+        lse = none ? __builtin_nan("") : log(r.S);
+        if (lane == 0) {
+            if (a.logprob) {
+                const int v = a.tokens[t];
+                a.logprob[t] = (float)((unsigned)v < (unsigned)a.V ? ((double)(float)x[v] - (double)r.m) * scale - lse : __builtin_nan(""));
+            }
+            if (a.entropy) a.entropy[t] = (float)(lse - r.E / r.S * (scale / (double)(a.scale * kLog2e)));
+        }
+        if constexpr (TOP) {
+            if (none) {
+                if (lane == 0) sc.picked = 0;
+            } else {
+                find_groups<E>(tops, a.groups, a.n_top, sc, lane);
+            }
+        }
+    }
+    if constexpr (TOP) {
+        __syncthreads();
+        const Key k = likeliest<E>(x, a.V, a.n_top, sc, wave, lane);
+        if (wave == 0 && lane < a.n_top) {
+            const bool none = lse != lse;
+            a.top_idx[t * a.n_top + lane] = none ? -1 : (int)~(uint32_t)k;
+            a.top_logprob[t * a.n_top + lane] = (float)(((double)number((int)((uint32_t)(k >> 32) ^ 0x80000000u)) - (double)r.m) * scale - lse);
+        }
     }
 }
 
@@ -419,15 +452,16 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(const Args a) {
     Row r = wave_joined(Row{(double)s.S, (double)s.E, s.m}, c);
     if (lane == 63) rows[wave] = r;
     __syncthreads();
-    if (wave > 0) return;
-    if constexpr (WAVES == 4) {
+    if (wave > 0) {
+        if constexpr (!(WHOLE && TOP)) return;
+    } else if constexpr (WAVES == 4) {
         r = joined(joined(rows[0], rows[1], c), joined(rows[2], rows[3], c), c);
     } else {
         r = wave_joined(lane < WAVES ? rows[lane] : Row{0.0, 0.0, -3.402823466e38f}, c);
         r.S = lane_63(r.S), r.E = lane_63(r.E);
     }
     if constexpr (WHOLE) {
-        answer<E, TOP>(a, t, x, r, tops, sc, lane);
+        answer<E, TOP>(a, t, x, r, tops, sc, wave, lane);
     } else if (lane == 0) {
         a.parts[t * a.pieces + piece] = Part{r.S, r.E, r.m, 0};
     }
@@ -435,19 +469,21 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(const Args a) {
 
 // the answers of rows whose pieces were several workgroups'
 template <class E, bool TOP>
-__global__ __launch_bounds__(64) void join_kernel(const Args a) {
+__global__ __launch_bounds__(TOP ? 256 : 64) void join_kernel(const Args a) {
     __shared__ Scratch sc;
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = blockIdx.x;
     const float c = a.scale * kLog2e;
     Row r = {0.0, 0.0, -3.402823466e38f};
-    for (int p = lane; p < a.pieces; p += 64) {
-        const Part q = a.parts[t * a.pieces + p];
-        r = joined(r, Row{q.S, q.E, q.m}, c);
+    if (wave == 0) {
+        for (int p = lane; p < a.pieces; p += 64) {
+            const Part q = a.parts[t * a.pieces + p];
+            r = joined(r, Row{q.S, q.E, q.m}, c);
+        }
+        r = wave_joined(r, c);
+        r.S = lane_63(r.S), r.E = lane_63(r.E);
     }
-    r = wave_joined(r, c);
-    r.S = lane_63(r.S), r.E = lane_63(r.E);
-    answer<E, TOP>(a, t, (const E *)a.logits + t * a.ld, r, a.tops + t * a.groups, sc, lane);
+    answer<E, TOP>(a, t, (const E *)a.logits + t * a.ld, r, a.tops + t * a.groups, sc, wave, lane);
 }
 
 template <class E, bool TOP>
@@ -462,7 +498,7 @@ int launch(const Args &a, int64_t T, const AgqLpPlan &p, hipStream_t st) {
     }
     logprobs_kernel<E, TOP, false, 4><<<grid, 256, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
-    join_kernel<E, TOP><<<dim3((unsigned)T), 64, 0, st>>>(a);
+    join_kernel<E, TOP><<<dim3((unsigned)T), TOP ? 256 : 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
