@@ -517,14 +517,15 @@ struct AgqLogprobs {
 };
 // A unit is four 16-byte loads of each lane; a group is a quarter of one of them.  A row is one workgroup's (its groups' largest
 // logits in LDS, the answers in the same launch), or is cut into pieces of four wavefronts until there are about a thousand
-// workgroups, which a second launch joins.  Measured in a replayed graph, pieces against whole rows of sixteen wavefronts, 0 and 20
-// alternatives:
-//   a unit to a wavefront or less: whole (fp16, 1 x 32000 5.7, 13.3 and 4.8, 13.6 us; 64 x 16000 6.0, 14.1 and 4.5, 13.1; 256 x 32000
-//     8.2, 17.1 and 5.9, 15.3), as the host takes 3 us for a launch
-//   more of them: pieces, as one CU reads a row slowly (1 x 128000 5.6, 14.4 and 10.3, 21.0; 64 x 128000 7.7, 17.3 and 11.0, 22.2;
-//     500 x 128000 26.3, 37.8 and 27.0, 42.3), but for one row to each of most CUs (256 x 128000 16.9, 27.3 and 15.5, 25.7; float32,
-//     256 x 50000 13.7, 21.3 and 9.8, 16.9)
-//   more than 512 rows: whole, with four wavefronts (1024 x 32000 15.6, 24.4; pieces 18.2, 27.9 and sixteen 19.2, 33.7 for 1000)
+// workgroups, which a second launch joins.  Measured in a replayed graph with 0 and 20 alternatives: pieces, whole rows with
+// sixteen wavefronts and with four:
+//   more than a row to a CU: whole, four wavefronts, so that a CU has several (500 x 32000 11.9, 18.4; 10.0, 20.8; 8.8, 16.2 us;
+//     1000 x 128000 46.9, 54.9; 47.4, 77.1; 43.9, 53.1; float32, 500 x 50000 20.5, 27.7; 18.3, 30.2; 16.6, 22.9; but 300 x 128000
+//     20.2, 29.1; 23.6, 37.7; 19.7, 30.9)
+//   a row to most CUs, or a unit to each of sixteen wavefronts: whole, sixteen, as the host takes 3 us for a launch too (256 x 32000
+//     8.3, 13.7; 5.9, 11.2; 6.1, 11.8; 1 x 32000 5.7, 11.1; 4.9, 10.4; 5.6, 11.3; float32, 200 x 50000 10.9, 18.0; 8.1, 14.1; 8.8, 15.2)
+//   else pieces, as one CU reads a row slowly (1 x 128000 5.7, 11.9; 10.4, 17.9; 11.5, 19.6; 64 x 128000 7.7, 14.5; 10.9, 18.5; 12.2,
+//     20.4)
 #define AGQ_LP_LOADS 4
 #define AGQ_LP_HELD 2048
 struct AgqLpPlan {
@@ -535,8 +536,8 @@ static inline AgqLpPlan agq_lp_plan(int64_t T, int64_t V, int kind, int64_t n_to
     const int64_t values = AGQ_LP_LOADS * 64 * (kind ? 4 : 8), units = (V + values - 1) / values;
     AgqLpPlan p;
     p.units = (int)units, p.groups = (int)units * AGQ_LP_LOADS * 4;
-    p.whole = (p.groups <= AGQ_LP_HELD || n_top == 0) && (units <= 16 || T > 512 || (T > 128 && T <= 256));
-    p.waves = p.whole && T <= 512 && units > 4 ? 16 : 4;
+    p.whole = (p.groups <= AGQ_LP_HELD || n_top == 0) && (units <= 16 || T >= 128);
+    p.waves = p.whole && T <= 256 && units > 4 ? 16 : 4;
     const int64_t parts = (units + p.waves - 1) / p.waves, want = p.whole || T > 512 ? 1 : T > 0 ? 1024 / T : 1, each = (parts + want - 1) / want;
     p.wave_units = (int)each, p.pieces = (int)((parts + each - 1) / each);
     return p;
