@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kMapThreads) void kv_map_kernel(const MapArgs a) {
 // even code.  Keys lie [token, D] in a page; values [D, token], which is the order in which the attention's matrix
 // instructions take them, so it reads both straight into registers.
 // The rotation is float64, in which products of fp16 and fp32 numbers are exact, rounded once.  Bound: long runs by memory and
-// the float64 arithmetic beside it (6000 tokens of 40 heads of 128: 372 MB in 100 us, 3.7 TB/s; a copy reaches 4.9),
+// the float64 arithmetic beside it (6000 tokens of 40 heads of 128: 372 MB in 96 us, 3.9 TB/s; a copy reaches 4.9),
 // a step's tokens by latency (one of 32 heads 4.3 us, 256 of 32 query and 8 key heads 8.0: 12.0 MB written for
 // 3.1, as a token's values are a byte in each of D rows).
 struct AppendArgs {
@@ -195,7 +195,9 @@ __device__ __forceinline__ int exp_for(uint32_t top) {
 __device__ __forceinline__ uint16_t d2h_odd(double d) {
     const uint64_t u = __builtin_bit_cast(uint64_t, d);
     const uint32_t hi = (uint32_t)(u >> 32) | min((uint32_t)u, 1u);
-    return __half_as_ushort(__float2half_rn((float)__builtin_bit_cast(double, (uint64_t)hi << 32)));
+    float f = (float)__builtin_bit_cast(double, (uint64_t)hi << 32);
+    asm("" : "+v"(f));                  // else the compiler makes one conversion of the two, of some thirty instructions
+    return __half_as_ushort(__float2half_rn(f));
 }
 // eight pairs of a head turned by their angles
 __device__ __forceinline__ void rotate8(Half8 &lo, Half8 &hi, const float *cos_t, const float *sin_t) {
