@@ -127,11 +127,12 @@ __global__ __launch_bounds__(256) void shared_copy_kernel(const int32_t *shared,
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n_pages; i += gridDim.x * 256) shared_out[i] = max(shared[i], 0);
 }
 
-// free_out: {head, free pages so far}
+// free_out: {head, free pages so far}.  One tile for a few thousand pages, as the code of four is slow to come (2.6 us, 4.8).
+template <int TILES>
 __global__ __launch_bounds__(1024) void kv_give_back_kernel(int32_t *shared, int32_t *ring, int32_t *free_out, int n_pages) {
     const int head = free_out[0], count = free_out[1];
     if (head < 0 || head >= n_pages || count < 0 || count > n_pages) return;     // a refused step: nothing has changed
-    const int given = give_back<1024, 4>(shared, shared, n_pages, ring, (int64_t)head + count);
+    const int given = give_back<1024, TILES>(shared, shared, n_pages, ring, (int64_t)head + count);
     if (threadIdx.x == 0) free_out[1] = min(count + given, n_pages);
 }
 
@@ -526,6 +527,12 @@ unsigned at_most(int64_t n, int64_t most) { return (unsigned)(n < 1 ? 1 : n > mo
 
 }  // namespace
 
+static int launch_give_back(const AgqKvPages &p, hipStream_t st) {
+    auto kernel = p.n_pages <= 16384 ? kv_give_back_kernel<1> : kv_give_back_kernel<4>;
+    kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
+    return (int)hipGetLastError();
+}
+
 int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy_src, int32_t *copy_dst, void *stream) {
     hipStream_t st = (hipStream_t)stream;
     const ForkArgs a = {p.kv_len, parent, p.table, p.shared, p.free_in, p.ring, p.kv_len_out, p.table_out, p.shared_out, copy_src, copy_dst, p.free_out,
@@ -538,8 +545,7 @@ int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy
     if (int err = (int)hipGetLastError()) return err;
     kv_fork_kernel<false><<<at_most(p.B * ((p.max_pages + 511) / 512), 256), 512, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
-    kv_give_back_kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
-    return (int)hipGetLastError();
+    return launch_give_back(p, st);
 }
 
 int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int32_t *moves, void *stream) {
@@ -557,8 +563,7 @@ int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_
     if (int err = (int)hipGetLastError()) return err;
     kv_compact_kernel<false><<<at_most(p.B * ((p.max_pages + 511) / 512), 256), 512, 0, st>>>(a, (int)groups);
     if (int err = (int)hipGetLastError()) return err;
-    kv_give_back_kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
-    return (int)hipGetLastError();
+    return launch_give_back(p, st);
 }
 
 static Layers layers_of(const AgqKvLayer *c, int n) {
