@@ -96,6 +96,18 @@ def test_fork_long_requests(agq):
     assert check_fork(agq, pool, lens, [0, 1, 2, 3, 4], 16)[-1] == 0
 
 
+@pytest.mark.parametrize("spare", [9000, 40001, 70000])
+def test_fork_and_compact_in_large_pools(agq, spare):
+    """holders' counts by the ten thousand, pages given back from all over them"""
+    r = rng_of(spare)
+    lens, common = families(r, 30, 3, 900, 16)
+    pool = Pool(r, lens, 16, 70, spare, common=common)
+    parent = np.where(r.random(30) < 0.4, -1, np.arange(30) // 3 * 3)
+    assert check_fork(agq, pool, lens, parent, 16)[-1] == 0
+    stay, kept = losses(r, lens, 16, "all")
+    assert check_compact(agq, r, pool, lens, stay, kept, 16, 64, 1)[5] == 0
+
+
 @pytest.mark.parametrize("what", ["short", "none to spare", "parent", "minus2", "negative", "long", "head", "count"])
 def test_fork_leaves_a_step_out(agq, what):
     r = rng_of(2)
@@ -264,7 +276,8 @@ def losses(r, lens, page, what):
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
-@pytest.mark.parametrize("B,longest,what", [(1, 1, "drop"), (1, 700, "drop"), (7, 400, "all"), (60, 200, "cut"), (70, 100, "all"), (600, 40, "all")])
+@pytest.mark.parametrize("B,longest,what", [(1, 1, "drop"), (1, 700, "drop"), (7, 400, "all"), (60, 200, "cut"), (70, 100, "all"), (600, 40, "all"),
+                                             (1500, 20, "all")])
 def test_compact(agq, page, B, longest, what):
     r = rng_of(page, B, longest)
     lens, common = families(r, B, 3, longest, page)
@@ -282,6 +295,73 @@ def test_compact_layers_and_scales(agq, page, D, Hkv, layers):
     stay, kept = losses(r, lens, page, "drop")
     for lo, hi in ((-128, 127), (-9, -2)):
         assert check_compact(agq, r, pool, lens, stay, kept, page, D, Hkv, layers, lo, hi)[5] == 0
+
+
+def test_compact_beyond_32_bits(agq):
+    """pages whose codes lie more than 4 GB into the cache, old ones and new ones"""
+    n_pages, Hkv, page, D = 70000, 4, 128, 128
+    k = torch.empty(n_pages, Hkv, page, D, dtype=torch.int8, device="cuda")
+    v = torch.empty(n_pages, Hkv, D, page, dtype=torch.int8, device="cuda")
+    e = torch.zeros(n_pages, Hkv, dtype=torch.int8, device="cuda")
+    r = rng_of(20)
+    for p in (69999, 2):
+        k[p], v[p] = dev(r.integers(-127, 128, (Hkv, page, D)).astype(np.int8)), dev(r.integers(-127, 128, (Hkv, D, page)).astype(np.int8))
+    keep = np.arange(1, 256, 3)
+    table, stay, cu, d_keep = i32([[2, 69999]]), i32([1]), i32([0, len(keep)]), i32(keep)
+    ring = np.full(n_pages, 5)
+    ring[0] = 69998
+    c = agq.kv_compact(i32([256]), stay, cu, d_keep, table, page, i32(np.zeros(n_pages)), i32(ring), i32([0, 9]))
+    agq.kv_move(agq.kv_layers([(k, v, e, e.clone())]), c.moves, table, stay, cu, d_keep)
+    tokens = np.concatenate([[0], keep])
+    old_k, old_v = torch.cat([k[2], k[69999]], 1), torch.cat([v[2], v[69999]], 2)
+    at = torch.from_numpy(tokens).cuda()
+    n = len(tokens)
+    assert host(c.status)[0] == 0 and host(c.block_table)[0, 0] == 69998 and host(c.kv_len)[0] == n
+    assert torch.equal(k[69998][:, :n], old_k[:, at]) and torch.equal(v[69998][:, :, :n], old_v[:, :, at])
+    assert not k[69998][:, n:].any() and not v[69998][:, :, n:].any()
+
+
+def test_two_streams_at_once(agq):
+    """two pools, forked and compacted on streams of their own"""
+    jobs = []
+    for seed in (1, 2):
+        r = rng_of(30, seed)
+        lens, common = families(r, 24, 4, 300, 16)
+        pool = Pool(r, lens, 16, 24, 400, common=common)
+        parent = np.arange(24) // 4 * 4
+        caches, d, handle = layers_of(agq, r, 2, pool.n_pages, 4, 16, 128)
+        stay, kept = losses(r, lens[parent], 16, "all")
+        cu, keep = np.concatenate([[0], np.cumsum([len(k) for k in kept])]), np.concatenate([np.asarray(k, np.int64) for k in kept])
+        want = so.kv_fork(lens, parent, 16, pool.table, pool.shared, pool.ring, pool.state, np.full_like(pool.table, -1))
+        after = so.kv_compact(want[0], stay, cu, keep, 16, want[1], want[2], want[5], want[6], np.full_like(pool.table, -1))
+        assert want[-1] == 0 and after[5] == 0
+        codes = []
+        for c in caches:
+            for i, turned in ((0, False), (1, True)):
+                a, b = c[i].copy(), c[2 + i].copy()
+                for x, y in zip(want[3], want[4]):
+                    if y >= 0:
+                        a[y], b[y] = a[x], b[x]
+                codes.append(so.kv_move(a, b, after[6], turned))
+        jobs.append((pool, d, handle, [i32(x) for x in (lens, parent, pool.table, pool.shared, pool.ring, pool.state, np.minimum(stay, 2 ** 31 - 1), cu, keep)],
+                     after, codes))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for i, (s, (pool, d, handle, (lens, parent, table, shared, ring, state, stay, cu, keep), _, _)) in enumerate(zip(streams, jobs)):
+        with torch.cuda.stream(s):
+            f = agq.kv_fork(lens, parent, table, 16, shared, ring, state)
+            agq.kv_copy_pages(handle, f.copy_src, f.copy_dst)
+            c = agq.kv_compact(f.kv_len, stay, cu, keep, f.block_table, 16, f.shared, ring, f.free_state)
+            agq.kv_move(handle, c.moves, f.block_table, stay, cu, keep)
+            got[i] = (f, c)
+    torch.cuda.synchronize()
+    for (f, c), (pool, d, handle, args, after, codes) in zip(got, jobs):
+        equal((c.kv_len, c.shared, args[4], c.free_state, c.status), (after[0], after[2], after[3], after[4], [after[5]]), ("kv_len", "shared", "ring", "free_state", "status"))
+        at = 0
+        for layer in d:
+            for i in (0, 1):
+                assert np.array_equal(host(layer[i]), codes[at][0]) and np.array_equal(host(layer[2 + i]), codes[at][1])
+                at += 1
 
 
 def test_compact_long(agq):
@@ -361,11 +441,12 @@ def test_compact_odd_requests(agq):
     assert not k[new, :, 4].any() and np.array_equal(np.delete(k, new, 0), np.delete(caches[0][0], new, 0))
 
 
-def test_captured_and_replayed(agq):
+@pytest.mark.parametrize("spare", [120, 9000])
+def test_captured_and_replayed(agq, spare):
     """a fork and a compaction in one graph, replayed with other lengths and parents, against eager calls"""
     r, B, page, most = rng_of(15), 16, 16, 12
     lens, common = families(r, B, 4, 100, page)
-    pool = Pool(r, lens, page, most, 120, common=common)
+    pool = Pool(r, lens, page, most, spare, common=common)
     caches, d, handle = layers_of(agq, r, 3, pool.n_pages, 4, page, 64)
     _, d2, handle2 = layers_of(agq, r, 3, pool.n_pages, 4, page, 64)
     N = 40

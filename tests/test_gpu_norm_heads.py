@@ -56,6 +56,25 @@ def test_norm_rope_many_tokens(agq):
     same(got, so.norm_rotate(x, g, 1e-5, pos, cos, sin))
 
 
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(6000, 30, 10, 64), (3001, 31, 3, 128), (20000, 7, 1, 64), (2500, 40, 40, 128)])
+@pytest.mark.parametrize("own", [False, True])
+def test_norm_rope_several_heads_to_a_lane(agq, T, Hq, Hkv, D, own):
+    """so many tokens that the lanes of a head take two heads and more, which they may not share out evenly"""
+    r = rng_of(T, Hq, own)
+    x, g_q, g_k = (r.standard_normal((T, Hq + Hkv, D)) * 2).astype(np.float16), gains(r, Hq, D, own), gains(r, Hkv, D, own)
+    pos = r.integers(0, 700, T)
+    cos, sin = synth.rope_tables(700, D)
+    d = dev(x)
+    got_q, got_k = agq.qk_norm_rope(d[:, :Hq], d[:, Hq:], dev(g_q), dev(g_k), 1e-6, i32(pos), dev(cos), dev(sin))
+    same(got_q, so.norm_rotate(x[:, :Hq], g_q, 1e-6, pos, cos, sin))
+    same(got_k, so.norm_rotate(x[:, Hq:], g_k, 1e-6, pos, cos, sin))
+    if own:                                           # and without a rotation, in place
+        q = d[:, :Hq]
+        agq.qk_norm_rope(q, None, dev(g_q), None, 1e-6, q_out=q)
+        same(d[:, :Hq].contiguous(), so.norm_rotate(x[:, :Hq], g_q, 1e-6))
+        assert np.array_equal(host(d[:, Hq:]), x[:, Hq:])
+
+
 @pytest.mark.parametrize("what", ["q only", "k only", "norm only", "rotation only", "one gain", "in place", "other rows"])
 def test_norm_rope_forms(agq, what):
     r = rng_of(3)
@@ -164,6 +183,39 @@ def test_append_norm_forms(agq, rope, own, T):
     r = rng_of(T, rope, own)
     slot, pos = random_slots(r, [3, 0], [T // 2, T - T // 2], 32, 60, 0)
     check_append(agq, r, T, 16, 16, 128, 32, slot, pos, 60, rope=rope, own=own, eps=1e-5)
+
+
+@pytest.mark.parametrize("own", [False, True])
+def test_append_norm_several_heads_to_a_lane(agq, own):
+    r = rng_of(77, own)
+    slot, pos = random_slots(r, [0, 40, 3], [2500, 1, 1500], 64, 90, 5)
+    check_append(agq, r, 4006, 33, 3, 128, 64, slot, pos, 90, own=own)
+
+
+def test_append_norm_nan_touches_nothing_else(agq):
+    """a NaN in a head of a key: that head of that token is NaN; the page's other tokens and heads are as they would be"""
+    r = rng_of(78)
+    T, Hkv, D, page, n_pages = 20, 3, 64, 32, 4
+    slot, pos = random_slots(r, [0], [T], page, n_pages, 0)
+    x, g = heads(r, T, 2 * Hkv, D), gains(r, Hkv, D, False)
+    bad = x.copy()
+    bad[7, 1, 9] = np.nan
+    cos, sin = synth.rope_tables(64, D)
+    fresh, got = random_cache(r, n_pages, Hkv, page, D), []
+    for a in (x, bad):
+        d = [dev(c) for c in fresh]
+        _, k = agq.kv_append_norm(dev(a)[:, :Hkv], dev(a)[:, Hkv:], i32(slot), *d, dev(g), 1e-6, pos=i32(pos), rope_cos=dev(cos), rope_sin=dev(sin))
+        got.append([host(t) for t in (k, *d)])
+    (k0, kc0, vc0, ke0, ve0), (k1, kc1, vc1, ke1, ve1) = got
+    assert np.isnan(k1[7, 1]).all() and np.array_equal(np.delete(k1, 7, 0), np.delete(k0, 7, 0)) and np.array_equal(k1[7, [0, 2]], k0[7, [0, 2]])
+    assert np.array_equal(vc0, vc1) and np.array_equal(ve0, ve1) and np.array_equal(kc0[:, [0, 2]], kc1[:, [0, 2]]) and np.array_equal(ke0[:, [0, 2]], ke1[:, [0, 2]])
+    rest = np.delete(x[:, 1:2], 7, 0)                  # the others' scale is theirs alone
+    want = so.norm_rotate(rest, g, 1e-6, np.delete(pos, 7), cos, sin)
+    p = slot[0] // page
+    e = so.exponent(np.abs(want.astype(np.float64)).max())
+    assert ke1[p, 1] == e
+    codes = np.clip(np.rint(want[:, 0].astype(np.float64) * 2.0 ** -e), -128, 127)
+    assert np.array_equal(np.delete(kc1[p, 1, :T], 7, 0), codes)
 
 
 def test_append_norm_is_norm_then_append(agq):
