@@ -1,6 +1,7 @@
 /* agq - the W4A8 / W4A4 quantized linear layer of Agile-Quant (arxiv 2312.05693)
  * and its log2-quantized softmax x V path, with the paged 8-bit key/value cache
- * and the attentions that serving needs, as HIP kernels for gfx950 (MI355X).
+ * (its pages shared and compacted too), the attentions that serving needs and the
+ * log probabilities of its answers, as HIP kernels for gfx950 (MI355X).
  *
  * C ABI.  Conventions that hold for every call unless a comment says otherwise:
  *   - every tensor pointer is a DEVICE pointer owned by the caller; the library
@@ -637,7 +638,7 @@ int agq_qk_norm_rope(const void *q_f16, int64_t ldq, int64_t Hq, const void *k_f
  * agq_kv_compact leave every partly filled page that a request would write into to that request alone.  A length that a
  * program lowers by itself must therefore stay within the last page if that one is not shared; agq_kv_compact takes any.
  * Both calls work from the old lengths, table, counts and ring state to new ones, which must not overlap them (AGQ_EINVAL;
- * a loop swaps two of each), on the device, in three launches; the ring alone is updated in place, behind the free pages.
+ * a loop swaps two of each), on the device, in one launch or three; the ring alone is updated in place, behind the free pages.
  * Pages are taken at the ring's head in the order of requests and entries, as in agq_kv_map; pages that lost their last
  * holder are given back in ascending order, and are not taken again by the same call.  Entries of block_table_out behind a
  * request's pages are left as they are.  *status: 0; or the number of free pages that are missing; or -1 (an impossible

@@ -491,6 +491,8 @@ struct AgqKvLayer {
 static inline int64_t agq_kv_new_pages(int64_t N, int64_t B, int64_t page) { return N / page + 2 * B; }
 #define AGQ_KV_MAX_B 4096
 // Steps that one workgroup does in one launch: requests, pages (their holders' counts are in LDS), entries of the table, listed tokens.
+// One launch against three: 8 beams forked and their pages copied 7.8 against 10.8 us in a replayed graph, 15 against 21 with the host's
+// calls; a compaction with 16000 listed tokens 18 against 11, level at about 4000.
 #define AGQ_KV_ONE_B 1024
 #define AGQ_KV_ONE_PAGES 8192
 #define AGQ_KV_ONE_ENTRIES 8192
