@@ -241,7 +241,7 @@ __device__ __forceinline__ bool listed_wrongly(const CompactArgs &a, const int *
     const int b = find_row(cu, a.B, (int)i);
     if (i < cu[b] || i >= cu[b + 1]) return false;         // of no request
     const int x = a.keep[i];
-    return x >= a.kv_len[b] || x < a.stay[b] || (i > cu[b] && x <= a.keep[i - 1]);
+    return x >= a.kv_len[b] || x < a.stay[b] || (i > max(cu[b], 0) && x <= a.keep[i - 1]);     // a cu may be anything
 }
 
 // the holders' counts, and the check

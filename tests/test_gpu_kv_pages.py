@@ -419,6 +419,16 @@ def test_compact_leaves_a_step_out(agq, what):
     assert want[5] == (2 if what == "short" else -1)
 
 
+@pytest.mark.parametrize("spare", [8, 9000])                        # one launch, three
+@pytest.mark.parametrize("cu", [[-3, 4, 4, 9], [-(1 << 31), -5, 4, 9], [0, -1, 4, 9], [-3, -2, -1, -1], [(1 << 31) - 1] * 4])
+def test_compact_sums_outside(agq, spare, cu):
+    r = rng_of(23)
+    lens, stay = np.array([40, 20, 64]), np.array([10, 20, 33])
+    pool = Pool(r, lens, 16, 4, spare)
+    keep = np.array([12, 20, 21, 39, 35, 40, 41, 50, 63])
+    assert run_compact(agq, r, pool, lens, stay, np.array(cu), keep, 16)[5] == -1
+
+
 def test_compact_odd_requests(agq):
     r = rng_of(14)
     pool = Pool(r, [], 16, 3, 4)
