@@ -697,7 +697,7 @@ int agq_kv_move(const agq_kv_cache *caches, int n_caches, const int32_t *moves, 
  * last.  A row without a distribution (a NaN or +infinity among its logits, or -infinity only) has NaN for logprob, entropy
  * and top_logprob, and -1 for top_idx.
  * 1 <= V <= 2^24, 0 <= T <= 2^22, 0 <= n_top <= min(V, AGQ_MAX_TOP), 2^-24 <= scale <= 2^24, ld <= 2^30; float32 logits times
- * scale have to be finite.  workspace: agq_logprobs_workspace_bytes, 16-byte aligned; contents are scratch.
+ * scale have to be finite (a log probability below float32's range is -infinity).  workspace: agq_logprobs_workspace_bytes, 16-byte aligned; contents are scratch.
  * Exponents, sums and results are float32, the sums of a row in a fixed order: a result's error is about 2^-22 of the largest
  * difference of scaled logits that counts in it.                                                                          */
 enum agq_logit_kind { AGQ_LOGITS_F16 = 0, AGQ_LOGITS_F32 = 1 };

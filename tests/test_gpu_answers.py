@@ -39,6 +39,8 @@ def compare(got, want, n_top, label=""):
             continue
         g, w = host(g).astype(np.float64), want[name]
         assert np.array_equal(np.isnan(g), np.isnan(w)), (label, name)
+        # float32 ends at 2^128 (1 - 2^-24); what is 2^128 (1 - 2^-25) or more rounds to infinity
+        w = np.where(np.abs(w) >= 2.0 ** 128 - 2.0 ** 103, np.copysign(np.inf, w), w)
         inf = np.isinf(w)
         assert np.array_equal(g[inf], w[inf]), (label, name)
         fine = np.isfinite(w)
@@ -139,6 +141,25 @@ def test_scales_and_large_logits(agq, kind, scale):
     x[3] = -65504
     x[4] = x[4] * 1e-4
     check(agq, x, r.integers(0, V, 6), 12, scale)
+
+
+@pytest.mark.parametrize("kind", ["fp16", "fp32"])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+@pytest.mark.parametrize("V", [300, 50001])
+def test_masks_of_the_lowest_value(agq, kind, scale, V):
+    """differences from it, times the scale in bits, are beyond float32"""
+    r = np.random.default_rng([9, V])
+    low = np.finfo(TYPES[kind]).min
+    x = draw(r, 6, V, kind)
+    x[0, r.random(V) < 0.5] = low
+    x[1, 3:] = low                                       # fewer tokens left than are asked for
+    x[2] = low
+    x[3] = low
+    x[3, V // 2] = -np.inf
+    x[4, 7:] = np.where(r.random(V - 7) < 0.5, low, -np.inf)
+    x[5] = low
+    x[5, 7] = -low
+    check(agq, x, [int(np.argmin(x[0])), 2, 0, V // 2, 8, 7], 12, scale)
 
 
 def test_sure_answers(agq):
