@@ -446,7 +446,7 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
 // ROLES = 4: one token and four roles to a workgroup.  A short run, as in a generation step, is that of its first token's
 // workgroup, whose wavefronts have a role each; a long one is shared by the workgroups of its first four tokens, a role each.
 // NORM: queries and keys are normalised before their rotation; a step's five workgroups of a CU are to fit it (256 tokens of 32 query
-// and 8 key heads 9.5 -> 8.9 us).  7001 normalised tokens of 24 and 4 heads: 88 MB in 24 us, 3.6 TB/s.
+// and 8 key heads 9.5 -> 8.9 us).  7001 normalised tokens of 32 and 8 heads of 64: 88 MB in 24 us, 3.6 TB/s.
 template <int ROLES, bool NORM>
 __global__ __launch_bounds__(256, NORM && ROLES == 4 ? 6 : 1) void kv_append_kernel(const AppendArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint16_t held[];      // [run][D], then one word per wavefront
