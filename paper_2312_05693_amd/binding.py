@@ -612,8 +612,9 @@ def _rope(rope_cos, rope_sin, pos, T, D, used):
     """(rows, pos, cos, sin) of the rotary tables"""
     if rope_cos is None or rope_sin is None or pos is None:
         raise ValueError("rope_cos, rope_sin and pos go together")
-    P = rope_cos.shape[0]
-    if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is _f32) \
+    shape = rope_cos.shape
+    P = shape[0]
+    if shape != (P, D // 2) or rope_sin.shape != shape or not (rope_cos.dtype is rope_sin.dtype is _f32) \
             or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
         raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
     used += pos, rope_cos, rope_sin
@@ -624,10 +625,11 @@ def _gain(g, H, D, name, used):
     """(address, elements between heads) of gains [D] or [H, D]"""
     if g is None:
         return None, 0
-    if g.dtype is not _f16 or tuple(g.shape) not in ((D,), (H, D)) or g.stride(-1) != 1:
+    ld, *one = g.stride() or (0,)
+    if g.dtype is not _f16 or g.shape != ((H, D) if one else (D,)) or (one[0] if one else ld) != 1:
         raise ValueError("%s: fp16 [%d] or [%d, %d] is wanted" % (name, D, H, D))
     used.append(g)
-    return g.data_ptr(), (g.stride(0) if g.dim() == 2 and H > 1 else 0)
+    return g.data_ptr(), (ld if one and H > 1 else 0)
 
 
 def _kv_cache(k_cache, v_cache, k_exp, v_exp):
@@ -691,16 +693,17 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     the queries if given, are rotated first: returns (rotated q or None, rotated k), else (None, None)."""
     cache, Hkv, D = _kv_cache(k_cache, v_cache, k_exp, v_exp)
     T = slot.numel()
-    shape = T, Hkv, D
+    like = T, Hkv, D
     used = [k, v, slot, k_cache, v_cache, k_exp, v_exp]
-    ldk, ldv = _like(k, shape, "k"), _like(v, shape, "v")
+    ldk, ldv = _like(k, like, "k"), _like(v, like, "v")
     P = Hq = ldq = ldqo = ldko = 0
     pos_p = cos_p = sin_p = q_p = qo_p = ko_p = None
     if rope_cos is not None:
         if rope_sin is None or pos is None:
             raise ValueError("rope_cos, rope_sin and pos go together")
-        P = rope_cos.shape[0]
-        if rope_cos.shape != (P, D // 2) or rope_sin.shape != (P, D // 2) or not (rope_cos.dtype is rope_sin.dtype is _f32) \
+        shape = rope_cos.shape
+        P = shape[0]
+        if shape != (P, D // 2) or rope_sin.shape != shape or not (rope_cos.dtype is rope_sin.dtype is _f32) \
                 or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
             raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
         pos_p, cos_p, sin_p = _ints(pos, T, "pos"), rope_cos.data_ptr(), rope_sin.data_ptr()
@@ -711,7 +714,7 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
         if k_out is None:
             k_out, ldko = k.new_empty(T, Hkv, D), Hkv * D
         else:
-            ldko = _like(k_out, shape, "k_out")
+            ldko = _like(k_out, like, "k_out")
             used.append(k_out)
         ko_p = k_out.data_ptr()
         if q is not None:
