@@ -564,7 +564,8 @@ __global__ __launch_bounds__(256, NORM && ROLES == 4 ? 6 : 1) void kv_append_ker
 // A lane has sixteen values of a head, eight of each half, which the rotation brings together; the sum of squares is joined over
 // the D / 16 lanes of the head.  They take some heads of one token, of q or of k, one after the other, so that the token's angles
 // and the gains are read and multiplied once for them.  Bound: long prompts by memory (6000 tokens of 40 query and 40 key heads of
-// 128: 249 MB in 55 us, 4.5 TB/s, a copy reaches 4.8); one token of 32 and 32 heads by latency, 3.2 us.
+// 128: 249 MB in 55 us, 4.5 TB/s, a copy reaches 4.8); one token of 32 and 32 heads by latency, 3.2 us.  (Stores past the caches
+// take 51, but the attention that reads the results comes next: both together 153 -> 158.)
 struct HeadsArgs {
     const uint16_t *q, *k, *g_q, *g_k;
     uint16_t *q_out, *k_out;

@@ -104,7 +104,8 @@ struct Unit {
 };
 
 // A lane's loads of unit u: load i holds values from (u kLoads + i) 64 N + lane N on; -infinity behind the row's end.  The rows
-// begin at any element: the loads need not be aligned.
+// begin at any element: the loads need not be aligned.  (Loads that leave nothing in the caches are faster where the logits come from
+// memory, 4096 x 32000 51.0 -> 48.3 us, and slower behind the product that has just made them, 500 x 128000 31.1 -> 33.7.)
 template <class E>
 __device__ __forceinline__ Unit<E> load_unit(const E *x, int V, int u, int lane) {
     constexpr int N = Vec<E>::N;
