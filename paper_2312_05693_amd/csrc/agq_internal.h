@@ -526,6 +526,8 @@ struct AgqLogprobs {
 //     20.2, 29.1; 23.6, 37.7; 19.7, 30.9)
 //   a row to most CUs, or a unit to each of sixteen wavefronts: whole, sixteen, as the host takes 3 us for a launch too (256 x 32000
 //     8.3, 13.7; 5.9, 11.2; 6.1, 11.8; 1 x 32000 5.7, 11.1; 4.9, 10.4; 5.6, 11.3; float32, 200 x 50000 10.9, 18.0; 8.1, 14.1; 8.8, 15.2)
+//   rows of one or two units without alternatives (four wavefronts look for those): as many wavefronts (20000 x 1000 49.6 -> 26.7,
+//     2000 x 1000 7.6 -> 5.8; 5000 x 4000 17.0 -> 15.0)
 //   else pieces, as one CU reads a row slowly (1 x 128000 5.7, 11.9; 10.4, 17.9; 11.5, 19.6; 64 x 128000 7.7, 14.5; 10.9, 18.5; 12.2,
 //     20.4)
 #define AGQ_LP_LOADS 4
@@ -539,7 +541,7 @@ static inline AgqLpPlan agq_lp_plan(int64_t T, int64_t V, int kind, int64_t n_to
     AgqLpPlan p;
     p.units = (int)units, p.groups = (int)units * AGQ_LP_LOADS * 4;
     p.whole = (p.groups <= AGQ_LP_HELD || n_top == 0) && (units <= 16 || T >= 128);
-    p.waves = p.whole && T <= 256 && units > 4 ? 16 : 4;
+    p.waves = p.whole && T <= 256 && units > 4 ? 16 : p.whole && n_top == 0 && units <= 2 ? (int)units : 4;
     const int64_t parts = (units + p.waves - 1) / p.waves, want = p.whole || T > 512 ? 1 : T > 0 ? 1024 / T : 1, each = (parts + want - 1) / want;
     p.wave_units = (int)each, p.pieces = (int)((parts + each - 1) / each);
     return p;

@@ -458,10 +458,16 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(const Args a) {
         }
     }
     Row r = wave_joined(Row{(double)s.S, (double)s.E, s.m}, c);
-    if (lane == 63) rows[wave] = r;
-    __syncthreads();
+    if constexpr (WAVES > 1) {
+        if (lane == 63) rows[wave] = r;
+        __syncthreads();
+    }
     if (wave > 0) {
         if constexpr (!(WHOLE && TOP)) return;
+    } else if constexpr (WAVES == 1) {
+        r.S = lane_63(r.S), r.E = lane_63(r.E);
+    } else if constexpr (WAVES == 2) {
+        r = joined(rows[0], rows[1], c);
     } else if constexpr (WAVES == 4) {
         r = joined(joined(rows[0], rows[1], c), joined(rows[2], rows[3], c), c);
     } else {
@@ -498,10 +504,9 @@ template <class E, bool TOP>
 int launch(const Args &a, int64_t T, const AgqLpPlan &p, hipStream_t st) {
     const dim3 grid((unsigned)(T * p.pieces));
     if (p.whole) {
-        if (p.waves == 16)
-            logprobs_kernel<E, TOP, true, 16><<<grid, 1024, 0, st>>>(a);
-        else
-            logprobs_kernel<E, TOP, true, 4><<<grid, 256, 0, st>>>(a);
+        auto kernel = p.waves == 16 ? logprobs_kernel<E, TOP, true, 16> : logprobs_kernel<E, TOP, true, 4>;
+        if constexpr (!TOP) kernel = p.waves == 1 ? logprobs_kernel<E, false, true, 1> : p.waves == 2 ? logprobs_kernel<E, false, true, 2> : kernel;
+        kernel<<<grid, 64 * p.waves, 0, st>>>(a);
         return (int)hipGetLastError();
     }
     logprobs_kernel<E, TOP, false, 4><<<grid, 256, 0, st>>>(a);
