@@ -698,8 +698,9 @@ int agq_kv_move(const agq_kv_cache *caches, int n_caches, const int32_t *moves, 
  * and top_logprob, and -1 for top_idx.
  * 1 <= V <= 2^24, 0 <= T <= 2^22, 0 <= n_top <= min(V, AGQ_MAX_TOP), 2^-24 <= scale <= 2^24, ld <= 2^30; float32 logits times
  * scale have to be finite (a log probability below float32's range is -infinity).  workspace: agq_logprobs_workspace_bytes, 16-byte aligned; contents are scratch.
- * Exponents, sums and results are float32, the sums of a row in a fixed order: a result's error is about 2^-22 of the largest
- * difference of scaled logits that counts in it.                                                                          */
+ * Exponents and results are float32, sums float32 for a few values and float64 beyond, in a fixed order.  With d = 2^-24, D the
+ * mean and Q the mean square of scale (max x - x) under p, a log probability l is off by at most d (|l| + 8 D + 32), an entropy H by
+ * d (H + 128 + 128 D + 16 Q), whatever V; 1 to 2 d of the result are usual.                                               */
 enum agq_logit_kind { AGQ_LOGITS_F16 = 0, AGQ_LOGITS_F32 = 1 };
 #define AGQ_MAX_TOP 64
 size_t agq_logprobs_workspace_bytes(int64_t T, int64_t V, int kind, int64_t n_top);

@@ -288,10 +288,12 @@ def logprobs(x, tokens, n_top, scale=1.0):
     what float32 arithmetic may be off, in units of d = 2^-24, to first order:
       z = (x - m) c, c = scale log2(e): a difference, a product, c's two roundings: 4 d |z|
       2^z: ln 2 times that, and the exponential's own 2 d, relative
-      S, E: sums of V terms in up to V / 256 + 64 steps in a row
+      S, E: sums of a few terms in 10 steps, the others in float64; z is relative to a logit less than a factor of two below the
+      largest, 1 more than |z|, and is brought to a larger one by a rounded factor (2 d) for every power of two or more, 3 d |z| + 2 d;
+      lanes, wavefronts and pieces are joined by a factor each, 10 d: 24 d and 3 d |z|
       log2 S: 2 d of itself, and S's relative error over ln 2; differences, products and factors: d or two of the result"""
     T, V = x.shape
-    d, ln2, steps = 2.0 ** -24, np.log(2.0), V / 256 + 64
+    d, steps = 2.0 ** -24, 24
     r = dict(logprob=np.full(T, np.nan), entropy=np.full(T, np.nan), top_idx=np.full((T, n_top), -1, dtype=np.int64),
              top_logprob=np.full((T, n_top), np.nan), logprob_bound=np.zeros(T), entropy_bound=np.zeros(T), top_bound=np.zeros((T, n_top)))
     for t in range(T):
@@ -306,11 +308,11 @@ def logprobs(x, tokens, n_top, scale=1.0):
             lp = z - lse
             size = np.where(p > 0, p * np.abs(z), 0.0).sum()
             square = np.where(p > 0, p * z * z, 0.0).sum()
-        S = 4 * size + 2 + steps                                                        # relative error of S over d
+        S = 7 * size + 2 + steps                                                        # relative error of S over d
         log_err = S + 2 * abs(lse)
         at = lambda v: d * (4 * np.abs(v) + log_err + 4 * np.abs(v - lse)) + 2.0 ** -149
         r["entropy"][t] = -(p[p > 0] * lp[p > 0]).sum()
-        r["entropy_bound"][t] = d * (log_err + 4 * square + (steps + 8 + S) * size + 4 * (abs(lse) + size))
+        r["entropy_bound"][t] = d * (log_err + 7 * (square + 2 * size + 1) + (steps + 8 + S) * (size + 1) + 4 * (abs(lse) + size))
         tok = -1 if tokens is None else int(tokens[t])
         if 0 <= tok < V:
             r["logprob"][t] = lp[tok]

@@ -280,3 +280,52 @@ def test_logits_of_the_quantized_layer(agq):
     tokens = np.arange(M) * 100
     got = agq.logprobs(y, dev(tokens.astype(np.int32)), n_top=5)
     compare(got, so.logprobs(host(y), tokens, 5), 5)
+
+
+def even_rows(V, kind):
+    """rows whose logits are nearly equal: a sum of them, one after the other in float32, is off by the same way at every step"""
+    rows, n = [], min(V, 2048)
+    for up in (0.3, 1.0, 2.5):                       # a few larger ones in front of every quarter
+        x = np.zeros(V)
+        for q in range(4):
+            x[q * V // 4:q * V // 4 + n] = up
+        rows.append(x)
+    rows += [np.linspace(0.0, 0.5, V), np.linspace(2.0, 0.0, V), np.linspace(-3.0, 3.0, V), np.full(V, 1.5)]
+    return np.stack(rows).astype(TYPES[kind])
+
+
+def check_even(agq, kind, T, V, n_top, scale):
+    """against float64 within the bounds of include/agq.h, which do not know V"""
+    x = even_rows(V, kind)
+    at = np.arange(T) % len(x)
+    tokens = np.array([0, V - 1, V // 2, V // 3, 0, V - 1, 1], dtype=np.int32)[:len(x)]
+    logits = dev(x)[torch.from_numpy(at).cuda()]
+    got = agq.logprobs(logits, dev(tokens[at]), n_top=n_top, scale=scale)
+    lp, ent, d = host(got.logprob).astype(np.float64), host(got.entropy).astype(np.float64), 2.0 ** -24
+    for i in range(min(T, len(x))):
+        y = x[i].astype(np.float64)
+        z = (y - y.max()) * float(np.float32(scale))
+        lse = np.log(np.exp(z).sum())
+        p = np.exp(z - lse)
+        want, H = z[tokens[i]] - lse, -(p * (z - lse)).sum()
+        D, Q = (p * -z).sum(), (p * z * z).sum()
+        off = abs(lp[i] - want), abs(ent[i] - H)
+        assert off[0] <= d * (abs(want) + 8 * D + 32) and off[1] <= d * (H + 128 + 128 * D + 16 * Q), (i, off, D, Q)
+        assert (lp[at == i] == lp[i]).all() and (ent[at == i] == ent[i]).all()
+        if n_top:
+            best = np.argsort(-y, kind="stable")[:n_top]
+            assert np.array_equal(host(got.top_idx)[i], best)
+            assert (np.abs(host(got.top_logprob)[i] - (z[best] - lse)) <= d * (np.abs(z[best] - lse) + 8 * D + 32)).all()
+
+
+@pytest.mark.parametrize("kind", ["fp16", "fp32"])
+@pytest.mark.parametrize("scale", [1.0, 0.37])
+@pytest.mark.parametrize("T,V,n_top", [(300, 32000, 0), (300, 131072, 0), (600, 131072, 3), (140, 131072, 0), (1, 131072, 2), (7, 1 << 20, 0),
+                                       (300, 1 << 20, 0), (520, 1 << 20, 2)])
+def test_rows_of_nearly_equal_logits(agq, kind, scale, T, V, n_top):
+    check_even(agq, kind, T, V, n_top, scale)
+
+
+def test_long_rows_of_nearly_equal_logits(agq):
+    check_even(agq, "fp16", 513, 1 << 24, 0, 1.0)
+    check_even(agq, "fp16", 2, 1 << 24, 1, 1.0)
