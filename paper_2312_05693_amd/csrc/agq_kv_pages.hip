@@ -17,11 +17,15 @@ template <bool ONE>
 struct Sizes {
     static constexpr int THREADS = ONE ? 1024 : 512, B = ONE ? AGQ_KV_ONE_B : kMaxB, PAGES = ONE ? AGQ_KV_ONE_PAGES : 1;
 };
-struct ForkArgs {
-    const int32_t *kv_len, *parent, *table, *shared, *free_in;
-    int32_t *ring, *kv_len_out, *table_out, *shared_out, *copy_src, *copy_dst, *free_out, *status;
+struct Books {
+    const int32_t *kv_len, *table, *shared, *free_in;
+    int32_t *ring, *kv_len_out, *table_out, *shared_out, *free_out, *status;
+    int32_t *copy_src, *copy_dst, *moves;       // a fork's, a compaction's; else NULL
     int64_t max_pages;
     int B, page_log2, n_pages;
+};
+struct ForkArgs : Books {
+    const int32_t *parent;
 };
 
 __device__ __forceinline__ int ring_at(int head, int64_t i, int n_pages) {       // head and i below n_pages
@@ -71,15 +75,15 @@ __device__ __forceinline__ void over_table(int B, int64_t max_pages, F f) {
     }
 }
 
-// Pages whose count fell below 0 go behind the free ones (`behind`, below 2 n_pages), in the order of their numbers; their number.
-// The counts are written to out, 0 for those.  A thread has four neighbours of each of TILES tiles at once, whose loads are on
+// Pages whose count fell below 0 go behind the `left` free ones that begin at head, in the order of their numbers; their number.
+// If that is more than the ring has room for, what does not fit is not written.  The counts are written to out, 0 for those.  A thread has four neighbours of each of TILES tiles at once, whose loads are on
 // their way before the first is looked at (a million pages in memory 240 us, 450 without; one tile where they are in LDS).
 template <int THREADS, int TILES>
-__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n_pages, int32_t *ring, int64_t behind) {
+__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n_pages, int32_t *ring, int head, int left) {
     constexpr int WAVES = THREADS / 64, TILE = 4 * THREADS;
     __shared__ int waves[TILES][WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t first = (uint32_t)(behind >= n_pages ? behind - n_pages : behind);
+    const uint32_t first = (uint32_t)ring_at(head, left, n_pages);
     int given = 0;
 #pragma unroll 1
     for (int64_t i0 = 0; i0 < n_pages; i0 += TILES * TILE) {
@@ -113,7 +117,7 @@ __device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, in
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (c[k][j] < 0) {
+                if (c[k][j] < 0 && given <= n_pages - left) {
                     const uint32_t r = first + (uint32_t)at++;
                     ring[r >= (uint32_t)n_pages ? r - (uint32_t)n_pages : r] = (int)i + j;
                 }
@@ -128,13 +132,54 @@ __global__ __launch_bounds__(256) void shared_copy_kernel(const int32_t *shared,
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n_pages; i += gridDim.x * 256) shared_out[i] = max(shared[i], 0);
 }
 
+// A step whose pages given back are more than the ring has room for (the books contradict each other) is taken back: copies of the
+// inputs, by one workgroup.  Table entries behind a request's pages and ring entries that are not free have been written by then.
+template <int THREADS>
+__device__ __forceinline__ void take_back(const Books &a) {
+    const int tid = threadIdx.x;
+    if (tid == 0) {
+        *a.status = -1;
+        a.free_out[0] = a.free_in[0], a.free_out[1] = a.free_in[1];
+        if (a.moves) a.moves[0] = 0;
+    }
+    for (int i = tid; i < a.n_pages; i += THREADS) a.shared_out[i] = max(a.shared[i], 0);
+    for (int b = tid; b < a.B; b += THREADS) {
+        a.kv_len_out[b] = a.kv_len[b];
+        if (a.copy_src) a.copy_src[b] = a.copy_dst[b] = -1;
+    }
+    for (int b = 0; b < a.B; ++b) {
+        const int64_t n = min(((int64_t)max(a.kv_len[b], 0) + (1 << a.page_log2) - 1) >> a.page_log2, a.max_pages), row = b * a.max_pages;
+        for (int64_t j = tid; j < n; j += THREADS) a.table_out[row + j] = a.table[row + j];
+    }
+}
 // free_out: {head, free pages so far}.  One tile for a few thousand pages, as the code of four is slow to come (2.6 us, 4.8).
 template <int TILES>
-__global__ __launch_bounds__(1024) void kv_give_back_kernel(int32_t *shared, int32_t *ring, int32_t *free_out, int n_pages) {
-    const int head = free_out[0], count = free_out[1];
-    if (head < 0 || head >= n_pages || count < 0 || count > n_pages) return;     // a refused step: nothing has changed
-    const int given = give_back<1024, TILES>(shared, shared, n_pages, ring, (int64_t)head + count);
-    if (threadIdx.x == 0) free_out[1] = min(count + given, n_pages);
+__global__ __launch_bounds__(1024) void kv_give_back_kernel(const Books a) {
+    const int head = a.free_out[0], left = a.free_out[1];
+    if (head < 0 || head >= a.n_pages || left < 0 || left > a.n_pages) return;     // a refused step: nothing has changed
+    const int given = give_back<1024, TILES>(a.shared_out, a.shared_out, a.n_pages, a.ring, head, left);
+    if (given > a.n_pages - left) {
+        __syncthreads();
+        take_back<1024>(a);
+    } else if (threadIdx.x == 0) {
+        a.free_out[1] = left + given;
+    }
+}
+// the same as the end of a step by one workgroup; go: the step is not refused
+template <int THREADS>
+__device__ __forceinline__ void give_back_here(const Books &a, const int32_t *counts, bool go, int head, int left) {
+    __syncthreads();
+    if (!go) {
+        for (int i = threadIdx.x; i < a.n_pages; i += THREADS) a.shared_out[i] = counts[i];
+        return;
+    }
+    const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, head, left);
+    if (given > a.n_pages - left) {
+        __syncthreads();
+        take_back<THREADS>(a);
+    } else if (threadIdx.x == 0) {
+        a.free_out[1] = left + given;
+    }
 }
 
 template <bool ONE>
@@ -220,19 +265,13 @@ __global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_fork_kernel(const Fork
             if ((unsigned)id < (unsigned)a.n_pages) atomicAdd((ONE ? counts : a.shared_out) + id, change);
         }
     });
-    if constexpr (ONE) {
-        __syncthreads();
-        const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, (int64_t)head_out + left);
-        if (tid == 0) a.free_out[1] = go ? min(left + given, a.n_pages) : left;
-    }
+    if constexpr (ONE) give_back_here<THREADS>(a, counts, go, head_out, left);
 }
 
 // ---------------------------------------------------------------- requests that lose tokens
-struct CompactArgs {
-    const int32_t *kv_len, *stay, *cu, *keep, *table, *shared, *free_in;
-    int32_t *ring, *kv_len_out, *table_out, *shared_out, *moves, *free_out, *status;
-    int64_t max_pages, N;
-    int B, page_log2, n_pages;
+struct CompactArgs : Books {
+    const int32_t *stay, *cu, *keep;
+    int64_t N;
     int32_t *checked;                 // AGQ_KV_CHECKS words behind the new pages in `moves`
 };
 
@@ -330,11 +369,7 @@ __global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_compact_kernel(const C
         }
         if (j >= same && (unsigned)old < (unsigned)a.n_pages) atomicAdd((ONE ? counts : a.shared_out) + old, -1);
     });
-    if constexpr (ONE) {
-        __syncthreads();
-        const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, (int64_t)head_out + left);
-        if (tid == 0) a.free_out[1] = go ? min(left + given, a.n_pages) : left;
-    }
+    if constexpr (ONE) give_back_here<THREADS>(a, counts, go, head_out, left);
 }
 
 // ---------------------------------------------------------------- the caches of all layers
@@ -535,16 +570,19 @@ unsigned at_most(int64_t n, int64_t most) { return (unsigned)(n < 1 ? 1 : n > mo
 
 }  // namespace
 
-static int launch_give_back(const AgqKvPages &p, hipStream_t st) {
-    auto kernel = p.n_pages <= 16384 ? kv_give_back_kernel<1> : kv_give_back_kernel<4>;
-    kernel<<<1, 1024, 0, st>>>(p.shared_out, p.ring, p.free_out, (int)p.n_pages);
+static Books books_of(const AgqKvPages &p, int32_t *copy_src, int32_t *copy_dst, int32_t *moves) {
+    return {p.kv_len, p.table, p.shared, p.free_in, p.ring, p.kv_len_out, p.table_out, p.shared_out, p.free_out, p.status, copy_src, copy_dst, moves,
+            p.max_pages, (int)p.B, log2_of(p.page), (int)p.n_pages};
+}
+static int launch_give_back(const Books &a, hipStream_t st) {
+    auto kernel = a.n_pages <= 16384 ? kv_give_back_kernel<1> : kv_give_back_kernel<4>;
+    kernel<<<1, 1024, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
 int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy_src, int32_t *copy_dst, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    const ForkArgs a = {p.kv_len, parent, p.table, p.shared, p.free_in, p.ring, p.kv_len_out, p.table_out, p.shared_out, copy_src, copy_dst, p.free_out,
-                        p.status, p.max_pages, (int)p.B, log2_of(p.page), (int)p.n_pages};
+    const ForkArgs a = {books_of(p, copy_src, copy_dst, nullptr), parent};
     if (agq_kv_one(p.B, p.max_pages, p.n_pages, 0)) {
         kv_fork_kernel<true><<<1, 1024, 0, st>>>(a);
         return (int)hipGetLastError();
@@ -553,14 +591,12 @@ int agq_launch_kv_fork(const AgqKvPages &p, const int32_t *parent, int32_t *copy
     if (int err = (int)hipGetLastError()) return err;
     kv_fork_kernel<false><<<at_most(p.B * ((p.max_pages + 511) / 512), 256), 512, 0, st>>>(a);
     if (int err = (int)hipGetLastError()) return err;
-    return launch_give_back(p, st);
+    return launch_give_back(a, st);
 }
 
 int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_t *cu, const int32_t *keep, int64_t N, int32_t *moves, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    const CompactArgs a = {p.kv_len, stay, cu, keep, p.table, p.shared, p.free_in, p.ring, p.kv_len_out, p.table_out, p.shared_out, moves, p.free_out,
-                           p.status, p.max_pages, N, (int)p.B, log2_of(p.page), (int)p.n_pages,
-                           moves + 4 + 4 * agq_kv_new_pages(N, p.B, p.page)};
+    const CompactArgs a = {books_of(p, nullptr, nullptr, moves), stay, cu, keep, N, moves + 4 + 4 * agq_kv_new_pages(N, p.B, p.page)};
     if (agq_kv_one(p.B, p.max_pages, p.n_pages, N)) {
         kv_compact_kernel<true><<<1, 1024, 0, st>>>(a, 0);
         return (int)hipGetLastError();
@@ -571,7 +607,7 @@ int agq_launch_kv_compact(const AgqKvPages &p, const int32_t *stay, const int32_
     if (int err = (int)hipGetLastError()) return err;
     kv_compact_kernel<false><<<at_most(p.B * ((p.max_pages + 511) / 512), 256), 512, 0, st>>>(a, (int)groups);
     if (int err = (int)hipGetLastError()) return err;
-    return launch_give_back(p, st);
+    return launch_give_back(a, st);
 }
 
 static Layers layers_of(const AgqKvLayer *c, int n) {

@@ -181,6 +181,69 @@ def test_fork_many_steps(agq):
     assert host(f.free_state)[1] == n_pages and not host(f.shared).any()
 
 
+def check_refused(r, pool, lens, got, ring, copies=()):
+    """a step that is left out for its books: copies of the inputs, and the free pages in the ring as they were"""
+    head, count = pool.state
+    free = (head + np.arange(count)) % pool.n_pages
+    assert host(got.status)[0] == -1 and host(got.free_state).tolist() == [head, count]
+    assert np.array_equal(host(ring)[free], pool.ring[free])
+    assert np.array_equal(host(got.kv_len), lens) and np.array_equal(host(got.shared), pool.shared)
+    for t in copies:
+        assert (host(t) == -1).all()
+    for b, L in enumerate(lens):
+        n = -(-int(L) // 16)
+        assert np.array_equal(host(got.block_table)[b, :n], pool.table[b, :n])
+
+
+@pytest.mark.parametrize("spare", [20, 5000, 9000, 40000])            # one launch (one tile of counts, two), three launches
+@pytest.mark.parametrize("room", [0, 1, 29])
+def test_no_room_in_the_ring(agq, spare, room):
+    """free_state says that more pages are free than can be, as 30 pages go back"""
+    r = rng_of(spare, room)
+    lens = np.array([160, 100, 480, 0, 33])                            # the third one's 30 pages go
+    pool = Pool(r, lens, 16, 40, spare)
+    pool.state[1] = pool.n_pages - room
+    # a ring of other numbers, none of which may change
+    pool.ring[:] = r.integers(0, pool.n_pages, pool.n_pages)
+    new = lambda *s: torch.full(s, -55, dtype=torch.int32, device="cuda")
+    parent = [0, 1, -1, 3, 4]
+    B, most = pool.table.shape
+    assert so.kv_fork(lens, parent, 16, pool.table, pool.shared, pool.ring, pool.state, pool.table)[-1] == -1
+    ring = i32(pool.ring)
+    out = agq.KvFork(new(B), new(B, most), new(pool.n_pages), new(B), new(B), new(2), new(1))
+    got = agq.kv_fork(i32(lens), i32(parent), i32(pool.table), 16, i32(pool.shared), ring, i32(pool.state), out=out)
+    check_refused(r, pool, lens, got, ring, (got.copy_src, got.copy_dst))
+    # the same pages, from a request that is cut to nothing; no token moves
+    stay, cu, keep = np.array([160, 100, 0, 0, 33]), [0] * 6, np.zeros(0, np.int64)
+    assert so.kv_compact(lens, stay, cu, keep, 16, pool.table, pool.shared, pool.ring, pool.state, pool.table)[5] == -1
+    ring = i32(pool.ring)
+    out = agq.KvCompact(new(B), new(B, most), new(pool.n_pages), new(agq.kv_moves_ints(0, B, 16)), new(2), new(1))
+    got = agq.kv_compact(i32(lens), i32(stay), i32(cu), i32(keep), i32(pool.table), 16, i32(pool.shared), ring, i32(pool.state), out=out)
+    check_refused(r, pool, lens, got, ring)
+    assert host(got.moves)[0] == 0
+    # one page of room more than goes back, and exactly as much: taken
+    for spare_room in (31, 30):
+        pool.state[1] = pool.n_pages - spare_room
+        assert check_fork(agq, pool, lens, parent, 16)[-1] == 0
+
+
+def test_no_room_in_the_ring_after_copies(agq):
+    """pages are taken and given back in the refused step; one that took as many as it gave is taken"""
+    r = rng_of(44)
+    lens = np.array([20, 40, 50])
+    pool = Pool(r, lens, 16, 5, 6)
+    pool.state[1] = pool.n_pages
+    new = lambda *s: torch.full(s, -55, dtype=torch.int32, device="cuda")
+    for parent in ([0, 0, 0], [-1, 2, 2]):                             # two pages taken, seven given back; one and five
+        ring = i32(pool.ring)
+        out = agq.KvFork(new(3), new(3, 5), new(pool.n_pages), new(3), new(3), new(2), new(1))
+        got = agq.kv_fork(i32(lens), i32(parent), i32(pool.table), 16, i32(pool.shared), ring, i32(pool.state), out=out)
+        check_refused(r, pool, lens, got, ring, (got.copy_src, got.copy_dst))
+        assert so.kv_fork(lens, parent, 16, pool.table, pool.shared, pool.ring, pool.state, pool.table)[-1] == -1
+    pool.state[1] = pool.n_pages - 5
+    assert check_fork(agq, pool, lens, [0, 0, 0], 16)[-1] == 0
+
+
 # ------------------------------------------------------------------ copies
 
 def layers_of(agq, r, n, n_pages, Hkv, page, D, lo=-7, hi=-4):
