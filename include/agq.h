@@ -637,8 +637,9 @@ int agq_qk_norm_rope(const void *q_f16, int64_t ldq, int64_t Hq, const void *k_f
  * agq_kv_fork.  A request writes only into the page that its length ends in, so full pages can be shared; agq_kv_fork and
  * agq_kv_compact leave every partly filled page that a request would write into to that request alone.  A length that a
  * program lowers by itself must therefore stay within the last page if that one is not shared; agq_kv_compact takes any.
- * Both calls work from the old lengths, table, counts and ring state to new ones, which must not overlap them (AGQ_EINVAL;
- * a loop swaps two of each), on the device, in one launch or three; the ring alone is updated in place, behind the free pages.
+ * Both calls work from the old lengths, table, counts and ring state to new ones (a loop swaps two of each), on the device, in
+ * one launch or three; the ring alone is updated in place, behind the free pages.  No output, the ring and moves among them, may
+ * overlap an input, parents, stay and listed tokens among them, or another output (AGQ_EINVAL).
  * Pages are taken at the ring's head in the order of requests and entries, as in agq_kv_map; pages that lost their last
  * holder are given back in ascending order, and are not taken again by the same call.  Entries of block_table_out behind a
  * request's pages are left as they are.  *status: 0; or the number of free pages that are missing; or -1 (an impossible

@@ -1,5 +1,6 @@
 // The serving calls of include/agq.h: argument checks on the host (before any HIP call), then the launchers.
 #include "../../include/agq.h"
+#include <initializer_list>
 #include "agq_internal.h"
 
 namespace {
@@ -163,16 +164,30 @@ int agq_attn_kv(const agq_kv_cache *cache, const void *q, int64_t ldq, int64_t T
 }
 
 static_assert(AGQ_KV_MAX_FORK == AGQ_KV_MAX_B, "the kernels hold that many requests' sums");
-// what agq_kv_fork and agq_kv_compact have in common
-static bool pages_ok(const AgqKvPages &p) {
+struct Ints {
+    const int32_t *p;
+    int64_t n;
+};
+// what agq_kv_fork and agq_kv_compact have in common, and what they read and write beside it: workgroups write while others read
+static bool pages_ok(const AgqKvPages &p, std::initializer_list<Ints> more_in, std::initializer_list<Ints> more_out) {
     if (!count_ok(p.B, AGQ_KV_MAX_FORK) || !page_ok(p.page)) return false;
     if (p.max_pages < 1 || p.max_pages > kMaxIndex / p.page || p.n_pages < 1 || p.n_pages > kMaxIndex / p.page) return false;
-    if (!ints_ok(p.shared) || !ints_ok(p.shared_out) || !ints_ok(p.ring) || !ints_ok(p.free_in) || !ints_ok(p.free_out) || !ints_ok(p.status)) return false;
-    if (!apart(p.free_in, 8, p.free_out, 8) || !apart(p.shared, 4 * (size_t)p.n_pages, p.shared_out, 4 * (size_t)p.n_pages)) return false;
-    if (p.B == 0) return true;
-    if (!ints_ok(p.kv_len) || !ints_ok(p.kv_len_out) || !ints_ok(p.table) || !ints_ok(p.table_out)) return false;
-    const size_t rows = 4 * (size_t)p.B, entries = rows * (size_t)p.max_pages;
-    return apart(p.kv_len, rows, p.kv_len_out, rows) && apart(p.table, entries, p.table_out, entries);
+    Ints all[16];
+    int n = 0, n_out = 0;
+    bool ok = true;
+    auto take = [&](const Ints &t) {                                      // tensors of no values have no addresses
+        ok &= t.n == 0 || ints_ok(t.p);
+        if (t.n > 0) all[n++] = t;
+    };
+    const int64_t entries = p.B * p.max_pages;
+    for (const Ints &t : {Ints{p.ring, p.n_pages}, {p.kv_len_out, p.B}, {p.table_out, entries}, {p.shared_out, p.n_pages}, {p.free_out, 2}, {p.status, 1}}) take(t);
+    for (const Ints &t : more_out) take(t);
+    n_out = n;
+    for (const Ints &t : {Ints{p.kv_len, p.B}, {p.table, entries}, {p.shared, p.n_pages}, {p.free_in, 2}}) take(t);
+    for (const Ints &t : more_in) take(t);
+    for (int i = 0; i < n_out; ++i)
+        for (int j = i + 1; j < n; ++j) ok &= apart(all[i].p, 4 * (size_t)all[i].n, all[j].p, 4 * (size_t)all[j].n);
+    return ok;
 }
 
 int agq_kv_fork(const int32_t *kv_len, const int32_t *parent, int64_t B, int64_t page, const int32_t *block_table, int64_t max_pages,
@@ -181,7 +196,7 @@ int agq_kv_fork(const int32_t *kv_len, const int32_t *parent, int64_t B, int64_t
                 void *stream) {
     const AgqKvPages p = {kv_len, block_table, shared, free_state, free_ring, kv_len_out, block_table_out, shared_out, free_state_out, status, B, page,
                           max_pages, n_pages};
-    if (!pages_ok(p) || (B > 0 && (!ints_ok(parent) || !ints_ok(copy_src) || !ints_ok(copy_dst)))) return AGQ_EINVAL;
+    if (!pages_ok(p, {{parent, B}}, {{copy_src, B}, {copy_dst, B}})) return AGQ_EINVAL;
     return hip_status(agq_launch_kv_fork(p, parent, copy_src, copy_dst, stream));
 }
 
@@ -196,8 +211,9 @@ int agq_kv_compact(const int32_t *kv_len, const int32_t *stay, const int32_t *cu
                    int32_t *free_state_out, int32_t *status, void *stream) {
     const AgqKvPages p = {kv_len, block_table, shared, free_state, free_ring, kv_len_out, block_table_out, shared_out, free_state_out, status, B, page,
                           max_pages, n_pages};
-    if (!pages_ok(p) || !count_ok(N, kMaxTokens - 1) || !ints_ok(cu_keep) || !aligned(moves, 16)) return AGQ_EINVAL;
-    if ((B > 0 && !ints_ok(stay)) || (N > 0 && !ints_ok(keep))) return AGQ_EINVAL;
+    const int64_t n_moves = (int64_t)agq_kv_moves_ints(N, B, page);
+    if (!count_ok(N, kMaxTokens - 1) || !aligned(moves, 16)) return AGQ_EINVAL;
+    if (!pages_ok(p, {{stay, B}, {cu_keep, B + 1}, {keep, N}}, {{moves, n_moves}})) return AGQ_EINVAL;
     return hip_status(agq_launch_kv_compact(p, stay, cu_keep, keep, N, moves, stream));
 }
 

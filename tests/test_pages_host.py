@@ -77,6 +77,37 @@ def test_compact_refuses(agq):
     assert f(-1, 3, 16) == 0 and f(1 << 30, 3, 16) == 0 and f(4, 4097, 16) == 0 and f(4, 4, 17) == 0
 
 
+def overlaps(outputs, inputs):
+    """every output at the start, at the last and just in front of the end of every input and other output: (name, address)"""
+    for name, (at, n) in outputs.items():
+        for other, (there, m) in {**inputs, **outputs}.items():
+            if other != name:
+                for place in (there, there + m - 4, there - n + 4):
+                    yield name, other, place
+
+
+def test_fork_refuses_outputs_on_other_tensors(agq):
+    """whatever a workgroup writes while another one reads, or both write; addresses that no kernel ever sees"""
+    inputs = dict(kv_len=(far(0), 12), second=(far(1), 12), table=(far(2), 48), shared=(far(3), 36), state=(far(5), 8))
+    outputs = dict(ring=(far(4), 36), kv_len_out=(far(6), 12), table_out=(far(7), 48), shared_out=(far(8), 36), src=(far(9), 12), dst=(far(10), 12),
+                   state_out=(far(11), 8), status=(far(12), 4))
+    ok = pages(**{k: outputs[k][0] for k in list(outputs)[1:]}, stream=None)
+    for name, other, place in overlaps(outputs, inputs):
+        assert agq.lib().agq_kv_fork(*dict(ok, **{name: place}).values()) == EINVAL, (name, other)
+
+
+def test_compact_refuses_outputs_on_other_tensors(agq):
+    moves = 4 * agq.kv_moves_ints(7, 3, 16)
+    inputs = dict(kv_len=(far(0), 12), second=(far(1), 12), cu=(far(13), 16), keep=(far(14), 28), table=(far(2), 48), shared=(far(3), 36), state=(far(5), 8))
+    outputs = dict(ring=(far(4), 36), kv_len_out=(far(6), 12), table_out=(far(7), 48), shared_out=(far(8), 36), moves=(far(9), moves), state_out=(far(11), 8),
+                   status=(far(12), 4))
+    base = pages()
+    ok = dict(kv_len=base["kv_len"], second=base["second"], cu=far(13), keep=far(14), N=7, **{k: base[k] for k in list(base)[2:]},
+              **{k: outputs[k][0] for k in list(outputs)[1:]}, stream=None)
+    for name, other, place in overlaps(outputs, inputs):
+        assert agq.lib().agq_kv_compact(*dict(ok, **{name: place}).values()) == EINVAL, (name, other)
+
+
 def test_layers_refuse(agq):
     import ctypes
     two = lambda **kw: (ctypes.c_int64 * 16)(*cache_of(), *cache_of(**kw))
