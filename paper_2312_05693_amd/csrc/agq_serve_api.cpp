@@ -100,7 +100,7 @@ int agq_qk_norm_rope(const void *q, int64_t ldq, int64_t Hq, const void *k, int6
     if ((q != nullptr) != (q_out != nullptr) || (q != nullptr) != (Hq > 0) || (k != nullptr) != (k_out != nullptr) || (k != nullptr) != (Hkv > 0))
         return AGQ_EINVAL;
     if ((!q && !k) || (g_q && !q) || (g_k && !k) || (!rope && !g_q && !g_k)) return AGQ_EINVAL;
-    if (T * (D / 16) > kMaxIndex / (Hq + Hkv) - 4096) return AGQ_EINVAL;  // work items are counted in 31 bits
+    if (T * (D / 16) > kMaxIndex / (Hq + Hkv)) return AGQ_EINVAL;         // work items are counted in 31 bits
     if (rope && (P < 1 || P > kMaxIndex || !aligned(rope_cos, 16) || !aligned(rope_sin, 16) || !ints_ok(pos))) return AGQ_EINVAL;
     if (q && (!tensor_ok(q, ldq, Hq, D) || !tensor_ok(q_out, ldqo, Hq, D))) return AGQ_EINVAL;
     if (k && (!tensor_ok(k, ldk, Hkv, D) || !tensor_ok(k_out, ldko, Hkv, D))) return AGQ_EINVAL;

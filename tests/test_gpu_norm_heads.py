@@ -267,3 +267,22 @@ def test_norm_captured_and_replayed(agq):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((qo, ko, qn, kn), want)) and torch.equal(qo, qn) and torch.equal(ko, kn)
         assert all(torch.equal(a, b) for a, b in zip(cache, other)), n
+
+
+def test_norm_rope_as_large_as_it_gets(agq):
+    """T * (Hq + Hkv) * D just below 2^35, in place: 4 GB and more between the first token and the last"""
+    r = rng_of(50)
+    T, H, D = 4095, 65536, 64
+    cos, sin = synth.rope_tables(16, D)
+    q, k = (torch.zeros(T, H, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    g_q, g_k = gains(r, H, D, False), gains(r, H, D, False)
+    rows = [0, 1, 2047, 3071, 3500, T - 1]
+    x = [heads(r, len(rows), H, D) for _ in range(2)]
+    pos = np.arange(T) % 20
+    at = torch.tensor(rows, device="cuda")
+    q[at], k[at] = dev(x[0]), dev(x[1])
+    agq.qk_norm_rope(q, k, dev(g_q), dev(g_k), 1e-6, i32(pos), dev(cos), dev(sin), q_out=q, k_out=k)
+    for t, y, g in ((q, x[0], g_q), (k, x[1], g_k)):
+        same(t[at], so.norm_rotate(y, g, 1e-6, pos[rows], cos, sin))
+        t[at] = 0
+        assert not any(bool(part.any()) for part in t.split(256))

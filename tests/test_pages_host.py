@@ -42,6 +42,15 @@ def test_qk_norm_rope_refuses(agq):
     assert call(T=0) == 0 and call(T=0, q=None, k=None) == 0
 
 
+def test_qk_norm_rope_size_limit(agq):
+    """T * (Hq + Hkv) * D < 2^35, to the last token; that the largest one below is taken is a test on the GPU"""
+    for T, Hq, Hkv, D in ((4096, 65536, 65536, 64), (2048, 65536, 65536, 128), ((1 << 28) + 1, 1, 0, 128), (1 << 28, 1, 1, 64), (613566757, 1, 0, 64),
+                          (1 << 22, 100, 100, 64)):
+        k = P if Hkv else None
+        assert agq.lib().agq_qk_norm_rope(P, Hq * D, Hq, k, max(Hkv, 1) * D, Hkv, T, D, P, 0, k, 0, 1e-6, None, None, None, 0, P, Hq * D, k,
+                                          max(Hkv, 1) * D, None) == EINVAL, (T, Hq, Hkv, D)
+
+
 def far(i):
     return Q + (i << 20)
 
