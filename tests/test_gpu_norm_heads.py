@@ -286,3 +286,50 @@ def test_norm_rope_as_large_as_it_gets(agq):
         same(t[at], so.norm_rotate(y, g, 1e-6, pos[rows], cos, sin))
         t[at] = 0
         assert not any(bool(part.any()) for part in t.split(256))
+
+
+def same_bits(got, want):
+    """bit for bit, zeros' signs too: what the definition's zeros are where no head has an infinity"""
+    g, w = host(got), np.asarray(want)
+    assert g.shape == w.shape and not np.isnan(w).any() and np.array_equal(g.view(np.uint16), w.view(np.uint16))
+
+
+@pytest.mark.parametrize("T", [5, 1500])
+@pytest.mark.parametrize("rope", [True, False])
+def test_signs_of_zeros(agq, T, rope):
+    """values, gains and angles of zero of either sign, alone and in whole heads; results too small for fp16"""
+    r = rng_of(T, rope, 60)
+    Hq, Hkv, D, page = 9, 3, 64, 32
+    x = heads(r, T, Hq + 2 * Hkv, D)
+    x[r.random(x.shape) < 0.5] = 0
+    x[:, [0, Hq]] = 0
+    x[:, [1, Hq + 1]] = (x[:, [1, Hq + 1]] * 2.0 ** -18).astype(np.float16)
+    x = np.where(r.random(x.shape) < 0.5, -x, x)
+    g_q, g_k = gains(r, Hq, D, True), gains(r, Hkv, D, True)
+    for g in (g_q, g_k):
+        g[r.random(g.shape) < 0.2] = 0
+        g[r.random(g.shape) < 0.2] *= np.float16(2.0 ** -20)
+        g[r.random(g.shape) < 0.3] *= -1
+    n_pages = T // page + 3
+    slot, pos = random_slots(r, [0], [T], page, n_pages, 0)             # the first token is not turned: sines of 0
+    cos, sin = synth.rope_tables(T, D)
+    tables = dict(pos=i32(pos), rope_cos=dev(cos), rope_sin=dev(sin)) if rope else {}
+    turn = dict(pos=pos, cos=cos, sin=sin) if rope else {}
+    want_q, want_k = so.norm_rotate(x[:, :Hq], g_q, 1e-6, **turn), so.norm_rotate(x[:, Hq:Hq + Hkv], g_k, 1e-6, **turn)
+    assert np.signbit(want_q[want_q == 0]).any() and not np.signbit(want_q[want_q == 0]).all()
+    d = dev(x)
+    q, k = agq.qk_norm_rope(d[:, :Hq], d[:, Hq:Hq + Hkv], dev(g_q), dev(g_k), 1e-6, **tables)
+    same_bits(q, want_q)
+    same_bits(k, want_k)
+    cache = [dev(a) for a in random_cache(r, n_pages, Hkv, page, D)]
+    q, k = agq.kv_append_norm(d[:, Hq:Hq + Hkv], d[:, Hq + Hkv:], i32(slot), *cache, dev(g_k), 1e-6, q=d[:, :Hq], g_q=dev(g_q), **tables)
+    same_bits(q, want_q)
+    same_bits(k, want_k)
+    if rope:                                                            # q turned without a norm, k normalised
+        q, k = agq.qk_norm_rope(d[:, :Hq], d[:, Hq:Hq + Hkv], None, dev(g_k), 1e-6, **tables)
+        same_bits(q, so.rotate(x[:, :Hq], pos, cos, sin))
+        same_bits(k, want_k)
+        cache = [dev(a) for a in random_cache(r, n_pages, Hkv, page, D)]
+        q, k = agq.kv_append(d[:, Hq:Hq + Hkv], d[:, Hq + Hkv:], i32(slot), *cache, q=d[:, :Hq], **tables)
+        same_bits(q, so.rotate(x[:, :Hq], pos, cos, sin))
+        same_bits(k, so.rotate(x[:, Hq:Hq + Hkv], pos, cos, sin))
