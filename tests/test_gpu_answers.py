@@ -329,3 +329,27 @@ def test_rows_of_nearly_equal_logits(agq, kind, scale, T, V, n_top):
 def test_long_rows_of_nearly_equal_logits(agq):
     check_even(agq, "fp16", 513, 1 << 24, 0, 1.0)
     check_even(agq, "fp16", 2, 1 << 24, 1, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["fp16", "fp32"])
+@pytest.mark.parametrize("T,V,n_top", [(3, 300001, 7), (40, 70001, 8), (3, 70001, 0), (600, 600001, 2)])
+def test_workspaces_that_are_needed(agq, kind, T, V, n_top):
+    """rows in pieces: a workspace that is too small, elsewhere or odd is refused, one of the least size is enough, and nothing
+    behind it is written"""
+    need = agq.logprobs_workspace_bytes(T, V, {"fp16": 0, "fp32": 1}[kind], n_top)
+    assert need > 0
+    row = np.random.default_rng([T, V]).standard_normal((2, V)).astype(TYPES[kind])
+    logits = dev(row)[torch.arange(T, device="cuda") % 2]
+    store = torch.full((need + 64,), 85, dtype=torch.int8, device="cuda")
+    for bad, status in ((store[:need - 1], agq.AGQ_ESIZE), (store[8:8 + need], agq.AGQ_EINVAL)):
+        with pytest.raises(agq.AgqError) as e:
+            agq.logprobs(logits, n_top=n_top, workspace=bad)
+        assert e.value.status == status
+    with pytest.raises(ValueError):
+        agq.logprobs(logits, n_top=n_top, workspace=torch.empty(need, dtype=torch.int8))
+    assert (store == 85).all()
+    got = agq.logprobs(logits, dev(np.zeros(T, np.int32)), n_top=n_top, workspace=store[:need])
+    assert (store[need:] == 85).all() and bool((store[:need] != 85).any())
+    want = so.logprobs(row, [0, 0], n_top)
+    at = np.arange(T) % 2
+    compare(got, {k: v[at] for k, v in want.items()}, n_top)

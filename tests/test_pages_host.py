@@ -154,6 +154,18 @@ def test_logprobs_refuses(agq):
         assert call(V=100000, ld=100000, ws=P, wsb=need - 1) == ESIZE
 
 
+def test_logprobs_workspace_sizes(agq):
+    """which shapes need a workspace, and that a smaller one is refused for each of them"""
+    need = agq.logprobs_workspace_bytes
+    for T, V, kind, n_top in ((2, 128000, 0, 20), (40, 70001, 1, 8), (3, 70001, 1, 0), (3, 300001, 0, 0), (600, 600001, 0, 2), (127, 50001, 0, 0)):
+        n = need(T, V, kind, n_top)
+        assert n > 0 and n % 4 == 0, (T, V, kind, n_top)
+        call = lambda ws, size: agq.lib().agq_logprobs(P, kind, T, V, V, 1.0, P, n_top, P, P, P if n_top else None, P if n_top else None, ws, size, None)
+        assert call(P, n - 1) == ESIZE and call(P, 0) == ESIZE and call(None, 0) == EINVAL and call(P + 8, n) == EINVAL
+    for T, V, kind, n_top in ((600, 2000, 0, 5), (1, 32000, 0, 64), (4096, 32000, 0, 0), (300, 1 << 20, 0, 0), (1, 1, 1, 1), (200, 50001, 1, 8)):
+        assert need(T, V, kind, n_top) == 0, (T, V, kind, n_top)
+
+
 def test_binding_refuses_other_tensors(agq):
     h, i, c = tensors()
     kv = (c(6, 2, 16, 64), c(6, 2, 64, 16), c(6, 2), c(6, 2))
