@@ -699,15 +699,7 @@ def kv_append(k, v, slot, k_cache, v_cache, k_exp, v_exp, q=None, pos=None, rope
     P = Hq = ldq = ldqo = ldko = 0
     pos_p = cos_p = sin_p = q_p = qo_p = ko_p = None
     if rope_cos is not None:
-        if rope_sin is None or pos is None:
-            raise ValueError("rope_cos, rope_sin and pos go together")
-        shape = rope_cos.shape
-        P = shape[0]
-        if shape != (P, D // 2) or rope_sin.shape != shape or not (rope_cos.dtype is rope_sin.dtype is _f32) \
-                or not (rope_cos.is_contiguous() and rope_sin.is_contiguous()):
-            raise ValueError("rope tables: contiguous float32 [P, D/2] are wanted")
-        pos_p, cos_p, sin_p = _ints(pos, T, "pos"), rope_cos.data_ptr(), rope_sin.data_ptr()
-        used += pos, rope_cos, rope_sin
+        P, pos_p, cos_p, sin_p = _rope(rope_cos, rope_sin, pos, T, D, used)
     elif pos is not None or rope_sin is not None or (_norm is None and (q is not None or k_out is not None)):
         raise ValueError("q, k_out, pos and rope_sin go with rope_cos")
     if rope_cos is not None or _norm is not None:
