@@ -157,3 +157,22 @@ __device__ __forceinline__ int agq_wave_scan(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);      // row_bcast 31: the thirty-two before
     return v;
 }
+
+// the largest i in [0, n) with at[i] <= x (at[0] <= x)
+__device__ __forceinline__ int agq_find_row(const int *at, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (at[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// an 8-bit code divided by 2^d, ties to even (down = 2^-d)
+__device__ __forceinline__ int8_t agq_coarser(int8_t c, float down) { return (int8_t)(int)rintf((float)c * down); }
+__device__ __forceinline__ uint32_t agq_coarser4(uint32_t w, float down) {
+    uint32_t o = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o |= ((uint32_t)(uint8_t)agq_coarser((int8_t)(w >> (8 * i)), down)) << (8 * i);
+    return o;
+}

@@ -44,16 +44,6 @@ __device__ __forceinline__ MapRow map_row(int past, int add, int page_log2, int6
     return r;
 }
 
-// the largest i in [0, n) with at[i] <= x (at[0] <= x)
-__device__ __forceinline__ int find_row(const int *at, int n, int x) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (at[mid] <= x) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
 __global__ __launch_bounds__(kMapThreads) void kv_map_kernel(const MapArgs a) {
     __shared__ int64_t sums[3][kMapThreads / 64];
     __shared__ int bad_wave[kMapThreads / 64];
@@ -137,18 +127,18 @@ __global__ __launch_bounds__(kMapThreads) void kv_map_kernel(const MapArgs a) {
         __syncthreads();
         // the tokens of these requests that are this workgroup's
         for (int t = max(t0, at_tok[0]) + tid; t < min(t1, done_tok); t += kMapThreads) {
-            const int i = find_row(at_tok, n, t);
+            const int i = agq_find_row(at_tok, n, t);
             const int p = past_of[i] + t - at_tok[i], j = p >> a.page_log2;
             const int id = j < held_of[i] ? a.table[(int64_t)(b0 + i) * a.max_pages + j] : a.ring[ring_at((int64_t)at_need[i] + j - held_of[i])];
             a.pos[t] = p;
             a.slot[t] = (unsigned)id < (unsigned)a.n_pages ? (id << a.page_log2) + (p & ((1 << a.page_log2) - 1)) : -1;
         }
         for (int u = max(n0, at_need[0]) + tid; u < min(n1, done_need); u += kMapThreads) {
-            const int i = find_row(at_need, n, u);
+            const int i = agq_find_row(at_need, n, u);
             a.table[(int64_t)(b0 + i) * a.max_pages + held_of[i] + u - at_need[i]] = a.ring[ring_at(u)];
         }
         for (int u = max(k0, at_back[0]) + tid; u < min(k1, done_back); u += kMapThreads) {
-            const int i = find_row(at_back, n, u);
+            const int i = agq_find_row(at_back, n, u);
             a.ring[ring_at((int64_t)count + u)] = a.table[(int64_t)(b0 + i) * a.max_pages + u - at_back[i]];
         }
     }
@@ -336,14 +326,6 @@ __device__ __forceinline__ uint32_t top8(const Half8 &h) {
     }
     return m;
 }
-// an 8-bit code divided by 2^d, ties to even (down = 2^-d)
-__device__ __forceinline__ int8_t coarser(int8_t c, float down) { return (int8_t)(int)rintf((float)c * down); }
-__device__ __forceinline__ uint32_t coarser4(uint32_t w, float down) {
-    uint32_t o = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o |= ((uint32_t)(uint8_t)coarser((int8_t)(w >> (8 * i)), down)) << (8 * i);
-    return o;
-}
 
 // One run: n tokens from t on into the page `id`, its entries off .. off + n - 1, keys (role 2 h) or values (2 h + 1) of head h.
 // ALONE: a few tokens, by one wavefront, which has at most one work item per lane; else by the whole workgroup, and the
@@ -402,7 +384,7 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
         if (off && e > e_had)
             for (int w = tid; w < off << (a.D_log2 - 2); w += threads) {
                 uint32_t *p = reinterpret_cast<uint32_t *>(codes) + w;
-                *p = coarser4(*p, down);
+                *p = agq_coarser4(*p, down);
             }
         if (ALONE) {
             if (tid < items) {
@@ -436,7 +418,7 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int role, int t,
         }
         if (first < 0 && e > e_had)
 #pragma unroll 1
-            for (int j = 0; j < min(-first, 16); ++j) p[j] = coarser(p[j], down);
+            for (int j = 0; j < min(-first, 16); ++j) p[j] = agq_coarser(p[j], down);
 #pragma unroll 1
         for (int j = max(-first, 0); j < min(n - first, 16); ++j) p[j] = (int8_t)code(j);
     }

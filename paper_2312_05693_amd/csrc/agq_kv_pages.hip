@@ -51,16 +51,6 @@ __device__ __forceinline__ int block_scan(int v, int *waves, int &total) {
     return before + up - v;
 }
 
-// the largest i in [0, n) with at[i] <= x (at[0] <= x)
-__device__ __forceinline__ int find_row(const int *at, int n, int x) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (at[mid] <= x) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
 // This workgroup's part of a table: f(request, entry).  One workgroup: thread by thread over rows and entries; else a row's
 // next entries to a workgroup.
 template <bool ONE, class F>
@@ -277,7 +267,7 @@ struct CompactArgs : Books {
 
 // do the listed tokens ascend inside their requests?  (cu in LDS)
 __device__ __forceinline__ bool listed_wrongly(const CompactArgs &a, const int *cu, int64_t i) {
-    const int b = find_row(cu, a.B, (int)i);
+    const int b = agq_find_row(cu, a.B, (int)i);
     if (i < cu[b] || i >= cu[b + 1]) return false;         // of no request
     const int x = a.keep[i];
     return x >= a.kv_len[b] || x < a.stay[b] || (i > max(cu[b], 0) && x <= a.keep[i - 1]);     // a cu may be anything
@@ -426,12 +416,6 @@ __global__ __launch_bounds__(256) void kv_copy_pages_kernel(const Layers c, cons
     }
 }
 
-// an 8-bit code divided by 2^d, ties to even (down = 2^-d)
-__device__ __forceinline__ uint32_t coarser(uint32_t byte, float down) { return (uint32_t)(int)rintf((float)(int8_t)byte * down) & 0xFFu; }
-__device__ __forceinline__ uint32_t coarser4(uint32_t w, float down) {
-    return coarser(w, down) | coarser(w >> 8, down) << 8 | coarser(w >> 16, down) << 16 | coarser(w >> 24, down) << 24;
-}
-
 // Past the caches: what is moved in all layers is more than they hold when the first layer's attention reads it (8 requests of up to
 // 16384 tokens 50 -> 44 us; with two layers only and their attention right behind 69.6 -> 70.3).
 __device__ __forceinline__ void store_past(int8_t *p, const uint4 &x) { __builtin_nontemporal_store(__builtin_bit_cast(agq_v4i, x), reinterpret_cast<agq_v4i *>(p)); }
@@ -539,7 +523,7 @@ __global__ __launch_bounds__(256) void kv_move_kernel(const Layers c, const Move
             uint8_t *out = reinterpret_cast<uint8_t *>(tile) + d * row;
 #pragma unroll
             for (int k = 0; k < 16; ++k)
-                if (bits >> k & 1) out[t++] = (uint8_t)coarser(words[k >> 2] >> ((k & 3) * 8), down);
+                if (bits >> k & 1) out[t++] = (uint8_t)agq_coarser((int8_t)(words[k >> 2] >> ((k & 3) * 8)), down);
         }
         // keys
         const int8_t *from_k = c.k[layer] + mine;
@@ -551,7 +535,7 @@ __global__ __launch_bounds__(256) void kv_move_kernel(const Layers c, const Move
             if (id >= 0) {
                 x = *reinterpret_cast<const uint4 *>(from_k + id * stride + (slot_of[t] << a.D_log2) + d);
                 const float down = __builtin_amdgcn_ldexpf(1.0f, run_exp[0][r] - e_k);
-                if (down != 1.0f) x = make_uint4(coarser4(x.x, down), coarser4(x.y, down), coarser4(x.z, down), coarser4(x.w, down));
+                if (down != 1.0f) x = make_uint4(agq_coarser4(x.x, down), agq_coarser4(x.y, down), agq_coarser4(x.z, down), agq_coarser4(x.w, down));
             }
             store_past(to_k + (t << a.D_log2) + d, x);
         }
