@@ -643,10 +643,10 @@ int agq_qk_norm_rope(const void *q_f16, int64_t ldq, int64_t Hq, const void *k_f
  * Pages are taken at the ring's head in the order of requests and entries, as in agq_kv_map; pages that lost their last
  * holder are given back in ascending order, and are not taken again by the same call.  Entries of block_table_out behind a
  * request's pages are left as they are.  *status: 0; or the number of free pages that are missing; or -1 (an impossible
- * free_state, a length that is negative or beyond max_pages * page, more pages to be given back than the ring has room for
- * beside the free ones, and what each call adds).  With a status other than 0 nothing happens: the outputs are copies of the
- * inputs, and the calls that follow do nothing (where the ring had no room its entries that are not free, and table entries
- * behind a request's pages, are unspecified; they mean nothing).
+ * free_state, a length that is negative or beyond max_pages * page, more pages to be given back than are not free, and what each
+ * call adds).  With a status other than 0 nothing happens: the outputs are copies of the inputs, and the calls that follow do
+ * nothing (where too many pages were to be given back, ring entries that are not free and table entries behind a request's pages
+ * are unspecified; they mean nothing).
  * 0 <= B <= AGQ_KV_MAX_FORK.  Everything is captured and replayed like the other calls.                                 */
 #define AGQ_KV_MAX_FORK 4096
 

@@ -212,7 +212,7 @@ def kv_fork(kv_len, parent, page, table, shared, ring, state, table_out):
         for q in table[p, :n - 1 if b in copies else n]:
             if there(q):
                 holders[q] += 1
-    if count - len(copies) + (shared + holders < 0).sum() > n_pages:
+    if count + (shared + holders < 0).sum() > n_pages:
         return refused(-1)
     shared = shared + holders
     state = _give_back(shared, ring, head, count, len(copies))
@@ -263,7 +263,7 @@ def kv_compact(kv_len, stay, cu, keep, page, table, shared, ring, state, table_o
         for p in table[b, same:up(kv_len[b])]:
             if 0 <= p < n_pages:
                 held[p] -= 1
-    if count - took + (shared + held < 0).sum() > n_pages:
+    if count + (shared + held < 0).sum() > n_pages:
         return refused(-1)
     shared = shared + held
     state = _give_back(shared, ring, head, count, took)

@@ -65,15 +65,15 @@ __device__ __forceinline__ void over_table(int B, int64_t max_pages, F f) {
     }
 }
 
-// Pages whose count fell below 0 go behind the `left` free ones that begin at head, in the order of their numbers; their number.
-// If that is more than the ring has room for, what does not fit is not written.  The counts are written to out, 0 for those.  A thread has four neighbours of each of TILES tiles at once, whose loads are on
+// Pages whose count fell below 0 go behind the free ones, of which there were `count` from head on before the step, in the order of
+// their numbers; their number.  If that is more than n_pages - count, what does not fit is not written.  The counts are written to out, 0 for those.  A thread has four neighbours of each of TILES tiles at once, whose loads are on
 // their way before the first is looked at (a million pages in memory 240 us, 450 without; one tile where they are in LDS).
 template <int THREADS, int TILES>
-__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n_pages, int32_t *ring, int head, int left) {
+__device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, int n_pages, int32_t *ring, int head, int count) {
     constexpr int WAVES = THREADS / 64, TILE = 4 * THREADS;
     __shared__ int waves[TILES][WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t first = (uint32_t)ring_at(head, left, n_pages);
+    const uint32_t first = (uint32_t)ring_at(head, count, n_pages);
     int given = 0;
 #pragma unroll 1
     for (int64_t i0 = 0; i0 < n_pages; i0 += TILES * TILE) {
@@ -107,9 +107,9 @@ __device__ __forceinline__ int give_back(const int32_t *counts, int32_t *out, in
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (c[k][j] < 0 && given <= n_pages - left) {
-                    const uint32_t r = first + (uint32_t)at++;
-                    ring[r >= (uint32_t)n_pages ? r - (uint32_t)n_pages : r] = (int)i + j;
+                if (c[k][j] < 0) {
+                    const uint32_t r = first + (uint32_t)at;
+                    if (at++ < n_pages - count) ring[r >= (uint32_t)n_pages ? r - (uint32_t)n_pages : r] = (int)i + j;
                 }
                 if (i + j < n_pages && (c[k][j] < 0 || out != counts)) out[i + j] = max(c[k][j], 0);
             }
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void shared_copy_kernel(const int32_t *shared,
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n_pages; i += gridDim.x * 256) shared_out[i] = max(shared[i], 0);
 }
 
-// A step whose pages given back are more than the ring has room for (the books contradict each other) is taken back: copies of the
+// A step that gives back more pages than were not free before it (the books contradict each other) is taken back: copies of the
 // inputs, by one workgroup.  Table entries behind a request's pages and ring entries that are not free have been written by then.
 template <int THREADS>
 __device__ __forceinline__ void take_back(const Books &a) {
@@ -145,10 +145,10 @@ __device__ __forceinline__ void take_back(const Books &a) {
 // free_out: {head, free pages so far}.  One tile for a few thousand pages, as the code of four is slow to come (2.6 us, 4.8).
 template <int TILES>
 __global__ __launch_bounds__(1024) void kv_give_back_kernel(const Books a) {
-    const int head = a.free_out[0], left = a.free_out[1];
-    if (head < 0 || head >= a.n_pages || left < 0 || left > a.n_pages) return;     // a refused step: nothing has changed
-    const int given = give_back<1024, TILES>(a.shared_out, a.shared_out, a.n_pages, a.ring, head, left);
-    if (given > a.n_pages - left) {
+    const int head = a.free_in[0], count = a.free_in[1], left = a.free_out[1];
+    if (head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages) return;   // a refused step: nothing has changed
+    const int given = give_back<1024, TILES>(a.shared_out, a.shared_out, a.n_pages, a.ring, head, count);
+    if (given > a.n_pages - count) {
         __syncthreads();
         take_back<1024>(a);
     } else if (threadIdx.x == 0) {
@@ -157,14 +157,14 @@ __global__ __launch_bounds__(1024) void kv_give_back_kernel(const Books a) {
 }
 // the same as the end of a step by one workgroup; go: the step is not refused
 template <int THREADS>
-__device__ __forceinline__ void give_back_here(const Books &a, const int32_t *counts, bool go, int head, int left) {
+__device__ __forceinline__ void give_back_here(const Books &a, const int32_t *counts, bool go, int head, int count, int left) {
     __syncthreads();
     if (!go) {
         for (int i = threadIdx.x; i < a.n_pages; i += THREADS) a.shared_out[i] = counts[i];
         return;
     }
-    const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, head, left);
-    if (given > a.n_pages - left) {
+    const int given = give_back<THREADS, 1>(counts, a.shared_out, a.n_pages, a.ring, head, count);
+    if (given > a.n_pages - count) {
         __syncthreads();
         take_back<THREADS>(a);
     } else if (threadIdx.x == 0) {
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_fork_kernel(const Fork
             if ((unsigned)id < (unsigned)a.n_pages) atomicAdd((ONE ? counts : a.shared_out) + id, change);
         }
     });
-    if constexpr (ONE) give_back_here<THREADS>(a, counts, go, head_out, left);
+    if constexpr (ONE) give_back_here<THREADS>(a, counts, go, head, count, left);
 }
 
 // ---------------------------------------------------------------- requests that lose tokens
@@ -359,7 +359,7 @@ __global__ __launch_bounds__(Sizes<ONE>::THREADS) void kv_compact_kernel(const C
         }
         if (j >= same && (unsigned)old < (unsigned)a.n_pages) atomicAdd((ONE ? counts : a.shared_out) + old, -1);
     });
-    if constexpr (ONE) give_back_here<THREADS>(a, counts, go, head_out, left);
+    if constexpr (ONE) give_back_here<THREADS>(a, counts, go, head, count, left);
 }
 
 // ---------------------------------------------------------------- the caches of all layers

@@ -227,12 +227,16 @@ def test_no_room_in_the_ring(agq, spare, room):
         assert check_fork(agq, pool, lens, parent, 16)[-1] == 0
 
 
-def test_no_room_in_the_ring_after_copies(agq):
-    """pages are taken and given back in the refused step; one that took as many as it gave is taken"""
-    r = rng_of(44)
+@pytest.mark.parametrize("spare", [6, 8000, 40000])
+@pytest.mark.parametrize("room", [0, 2, 4])
+def test_no_room_in_the_ring_after_copies(agq, spare, room):
+    """pages are taken and given back in the refused step, and the taken ones are free again: the ring's entries that they came from
+    are not written over; in one launch with one tile of counts and two, and in three with several"""
+    r = rng_of(44, spare)
     lens = np.array([20, 40, 50])
-    pool = Pool(r, lens, 16, 5, 6)
-    pool.state[1] = pool.n_pages
+    pool = Pool(r, lens, 16, 5, spare)
+    pool.state[1] = pool.n_pages - room
+    pool.ring[:] = r.integers(0, pool.n_pages, pool.n_pages)
     new = lambda *s: torch.full(s, -55, dtype=torch.int32, device="cuda")
     for parent in ([0, 0, 0], [-1, 2, 2]):                             # two pages taken, seven given back; one and five
         ring = i32(pool.ring)
@@ -240,7 +244,7 @@ def test_no_room_in_the_ring_after_copies(agq):
         got = agq.kv_fork(i32(lens), i32(parent), i32(pool.table), 16, i32(pool.shared), ring, i32(pool.state), out=out)
         check_refused(r, pool, lens, got, ring, (got.copy_src, got.copy_dst))
         assert so.kv_fork(lens, parent, 16, pool.table, pool.shared, pool.ring, pool.state, pool.table)[-1] == -1
-    pool.state[1] = pool.n_pages - 5
+    pool.state[1] = pool.n_pages - 7
     assert check_fork(agq, pool, lens, [0, 0, 0], 16)[-1] == 0
 
 
