@@ -543,7 +543,8 @@ typedef struct agq_kv_cache {
  * are, cu_new is all 0 and every slot -1, so that calls which follow do nothing.
  * kv_len_out and free_state_out must not overlap kv_len and free_state (AGQ_EINVAL): a loop swaps two of each.  Between
  * steps a program may lower a length (a draft's tokens that were not taken) as far as the request keeps its pages;
- * pages behind that would be lost, as nothing gives them back.
+ * pages behind that would be lost, as nothing gives them back.  n_new = -1 gives pages back without a look at other requests
+ * that hold them: where pages are shared (agq_kv_fork, below) a request is ended by agq_kv_fork alone.
  * B <= 2^20; max_pages * page < 2^31; pos and slot may be NULL when T == 0.                                          */
 int agq_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int64_t page, int32_t *block_table,
                int64_t max_pages, int32_t *free_ring, int64_t n_pages, const int32_t *free_state, int64_t T,
@@ -563,7 +564,8 @@ int agq_kv_map(const int32_t *kv_len, const int32_t *n_new, int64_t B, int64_t p
  * stay as they are.
  * k, v: fp16 [T, Hkv, D].  q (may be NULL with q_out NULL, Hq = 0): fp16 [T, Hq, D], rotated into q_out.  k_out (may be
  * NULL): the rotated keys in fp16, for agq_attn_packed.  q_out and k_out may be q and k themselves.
- * rope_cos, rope_sin [P, D/2] float32 and pos [T]; all three NULL: no rotation (q and k_out must be NULL then).        */
+ * rope_cos, rope_sin [P, D/2] float32 and pos [T]; all three NULL: no rotation (q and k_out must be NULL then).
+ * T * D / 16 <= (2^31 - 1) / max(Hq, 2 Hkv) - 4096.                                                                    */
 int agq_kv_append(const agq_kv_cache *cache, const void *k_f16, int64_t ldk, const void *v_f16, int64_t ldv, int64_t T,
                   const int32_t *slot, const void *q_f16, int64_t ldq, int64_t Hq, const int32_t *pos,
                   const float *rope_cos, const float *rope_sin, int64_t P, void *q_out_f16, int64_t ldqo,

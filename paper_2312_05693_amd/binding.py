@@ -671,6 +671,7 @@ class KvStep(NamedTuple):
 
 def kv_map(kv_len, n_new, block_table, page, free_ring, free_state, T, out: KvStep | None = None) -> KvStep:
     """agq_kv_map: pages, slots and positions of one step; block_table [B, max_pages] and free_ring [n_pages] are updated.
+    n_new = -1 looks at no other holders of a page: where pages are shared a request is ended by kv_fork.
     out: a KvStep to write into (not the one whose kv_len and free_state are passed in: a loop swaps two)."""
     B, max_pages = block_table.shape
     n_pages = free_ring.numel()

@@ -12,7 +12,7 @@ constexpr int kMaxB = AGQ_KV_MAX_B;   // requests: their sums are held in LDS
 // change by atomic additions of whole numbers, whose order does not matter; the pages given back are found afterwards in the
 // order of their numbers, so the ring does not depend on it either.
 // Small steps (agq_kv_one) are ONE launch of one workgroup, with the counts in LDS: all of it is waiting for memory and for launches
-// (a fork of 8 requests 4.8 us, of 256 8.8, a compaction of 64 requests 6.7; three launches take 11 to 13).
+// (a fork of 8 requests 4.8 us, of 256 9.0, a compaction of 64 requests 6.4; three launches take 11 to 13).
 template <bool ONE>
 struct Sizes {
     static constexpr int THREADS = ONE ? 1024 : 512, B = ONE ? AGQ_KV_ONE_B : kMaxB, PAGES = ONE ? AGQ_KV_ONE_PAGES : 1;

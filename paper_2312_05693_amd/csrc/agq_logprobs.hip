@@ -5,9 +5,9 @@
 // be off by m c's rounding, which is more than an exponent can take where the logits times scale are large.)  Then
 // log p = (x - m) scale - ln S and the entropy ln S - E / S (scale / c), of the row's joined sums in float64.
 // Sums in float32 are those of the values of a load and of a unit's four loads; units are added in float64, as sums of nearly equal
-// terms are off the same way at every step (rows of 131072 logits, a few larger than the others: log probabilities off by 4.6e-6, 4.4e-7 like this).  m stays
-// where a larger logit is less than a factor of two above it, so that there are no more factors 2^(old m - new m), each rounded, than
-// powers of two between a logit and the largest.  With d = 2^-24 S is off, relatively and to first order, by
+// terms are off the same way at every step (rows of 131072 logits, a few larger than the others: log probabilities off by 4.6e-6,
+// 4.4e-7 like this).  m stays where a larger logit is less than a factor of two above it, so that there are no more factors
+// 2^(old m - new m), each rounded, than powers of two between a logit and the largest.  With d = 2^-24 S is off, relatively and to first order, by
 //   4 d |difference| of z (a subtraction, a product, c's two roundings), 2 d of 2^z, 10 d of the chains, 2 d and 3 d |difference| of the
 //   factors, and 10 d of the joins of lanes, wavefronts and pieces, a factor each.
 // (300 rows of 128000 fp16 logits 19.8 -> 20.6 us against float32 throughout, other sizes 0 to 2 %.  A chain for each load side by
@@ -20,7 +20,7 @@
 //   many rows by memory and the exponentials beside it: 4096 rows of 32000, fp16, 51 us: 262 MB at 5.1 TB/s, where a read alone
 //     reaches 6.05; a lane's 128 logits and its share of the joins take nine instructions a logit, one of them a quarter-rate
 //     exponential, 40 us of arithmetic beside it;
-//   few rows by latency: 1 x 32000 with 20 alternatives 9.8 us, 64 x 128000 15.3, 200 x 50000 of float32 with a mask 16.0, of which
+//   few rows by latency: 1 x 32000 with 20 alternatives 10.8 us, 64 x 128000 15.6, 200 x 50000 of float32 with a mask 16.2, of which
 //     the alternatives are 4 to 5 us: the groups' order, the loads of the best ones, the order of their tokens, one after the other.
 #include <limits.h>
 #include "agq_device.h"
